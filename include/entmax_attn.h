@@ -267,6 +267,80 @@ int entmax_scale_proj_bwd(const entmax_scale_proj_params* p, const void* X, cons
 /* Workspace bytes of entmax_scale_proj_bwd; 0 if the parameters are invalid. Host-only. */
 size_t entmax_scale_proj_workspace_bytes(const entmax_scale_proj_params* p);
 
+/*
+ * Serving: entmax attention of sequences of different lengths, their tokens packed one sequence after the other, with
+ * grouped heads (query head h reads key/value head h / (Hq / Hkv)), and a paged cache for the keys and values.  No
+ * thresholds are returned and there is no backward: training uses entmax_attn_fwd / entmax_attn_bwd.
+ *
+ * Packed rows.  cu_seqlens, int32 [nseq + 1], not decreasing: sequence s owns rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1
+ * of the tensors with T rows.  Rows that no sequence owns (in front, behind the last one) are left as they are.
+ * Paged cache.  K and V are pools of num_pages pages of page_size tokens, [num_pages, Hkv, page_size, D] with strides in
+ * elements.  page_table, int32 [nseq, max_pages] contiguous: token j of sequence s lives in page page_table[s][j / page_size],
+ * place j % page_size.  kv_len, int32 [nseq]: tokens of each sequence, its new ones (the last ones) included.
+ * All of these live in device memory and are read by the kernels only, so that a captured graph serves other lengths and
+ * pages on replay.  Nothing outside the tensors is touched whatever they hold:
+ *   - A sequence is left out (its rows are not written) if cu_seqlens leads out of the T rows or decreases, if it has more than
+ *     max_new new tokens, or more than max_keys keys, or kv_len is negative.
+ *   - A page number outside 0 .. num_pages - 1 is a hole: its keys are visible to no row, and tokens appended there are dropped.
+ *
+ * Attention (entmax_paged_attn_fwd, entmax_packed_attn_fwd): the operation of entmax_attn_fwd.  New token t of a sequence
+ * with n new tokens and L keys sits at position L - n + t; under the causal flag it sees the keys up to its position.  A row
+ * that sees no key (L < n, holes) gets zeros.  Keys that a row does not see do not influence it whatever they hold, infinities and
+ * NaN included; a row that sees a key with such values has no defined result.
+ *   beta, gamma: fp32 [Hq] (scale_layout 1), [Hq, T] (scale_layout 2: what entmax_scale_proj_fwd returns for X [1, T, E]);
+ *   alibi_slopes: NULL or fp32 [Hq], with bias_mode, as in entmax_attn_fwd.  n in (ln n)^gamma: logn_mode 0 the sequence's keys L,
+ *   1 the keys the row sees (holes counted).
+ * Packed: K, V [T, Hkv, D]; every sequence has as many keys as tokens; page_size, num_pages, max_pages and the page strides must be
+ * 0, and max_keys = max_new.
+ * Calls need entmax_seq_workspace_bytes(p) bytes of 256-byte aligned workspace whose contents do not matter; calls that may
+ * overlap in time (two streams, two captured graphs replayed together) need one each.
+ */
+typedef struct {
+  int32_t nseq, T;              /* sequences; rows of Q and O (packed: of K and V too) */
+  int32_t Hq, Hkv, D;           /* Hq a multiple of Hkv; D in {64, 128} */
+  int32_t dtype;                /* ENTMAX_ATTN_BF16 or ENTMAX_ATTN_FP32: type of Q, K, V, O */
+  int32_t causal, scale_layout, logn_mode, bias_mode; /* as in entmax_attn_params */
+  int32_t path;                 /* 0: automatic; 1: tiled kernel only (test aid) */
+  int32_t page_size, num_pages, max_pages; /* page_size: a power of two from 16 to 65536; all 0: packed */
+  int32_t max_new, max_keys;    /* no sequence has more new tokens / keys (max_keys <= max_pages * page_size) */
+  float alpha, delta;
+  int64_t q_stride_t, q_stride_h, o_stride_t, o_stride_h;  /* elements */
+  int64_t k_stride_p, k_stride_h, k_stride_n;              /* page, head, token */
+  int64_t v_stride_p, v_stride_h, v_stride_n;
+} entmax_seq_params;
+
+int entmax_paged_attn_fwd(const entmax_seq_params* p, const void* Q, const void* K, const void* V, const int32_t* cu_seqlens,
+                          const int32_t* kv_len, const int32_t* page_table, const float* beta, const float* gamma,
+                          const float* alibi_slopes, void* O, void* workspace, size_t workspace_bytes, void* hip_stream);
+int entmax_packed_attn_fwd(const entmax_seq_params* p, const void* Q, const void* K, const void* V, const int32_t* cu_seqlens,
+                           const float* beta, const float* gamma, const float* alibi_slopes, void* O, void* workspace,
+                           size_t workspace_bytes, void* hip_stream);
+/* Workspace bytes of either; 0 if the parameters are invalid. Host-only. */
+size_t entmax_seq_workspace_bytes(const entmax_seq_params* p);
+
+/*
+ * Appending to the paged cache, with the position rotation on the way: for every new token (position P = kv_len - n + t)
+ *     Qout = R_P Q,   K page = R_P K,   V page = V
+ * where R_P turns the pairs of the first `rot` features of every head: (x, y) -> (x cos - y sin, y cos + x sin) by the angle
+ * P inv_freq[i].  Pair i is features (i, i + rot / 2), or (2 i, 2 i + 1) if `interleaved`.  Angles are formed in 64 bits.
+ *   Q, Qout: [T, Hq, D], NULL together (Hq = 0) if there is nothing to rotate; Qout may be Q.  K, V: [T, Hkv, D].
+ *   inv_freq: fp32 [rot / 2], ignored (may be NULL) for rot = 0.
+ * A sequence with kv_len < n, or more keys than max_pages * page_size, is left out.  Two tokens with the same place in the
+ * cache (a page that two sequences append to) leave either's bytes there.
+ */
+typedef struct {
+  int32_t nseq, T, Hq, Hkv, D, dtype;
+  int32_t page_size, num_pages, max_pages;
+  int32_t rot, interleaved;     /* rot: a multiple of 16, 0 .. D */
+  int64_t q_stride_t, q_stride_h, qo_stride_t, qo_stride_h;
+  int64_t k_stride_t, k_stride_h, v_stride_t, v_stride_h;     /* the new tokens' */
+  int64_t kc_stride_p, kc_stride_h, kc_stride_n, vc_stride_p, vc_stride_h, vc_stride_n;  /* the cache's: page, head, token */
+} entmax_append_params;
+
+int entmax_cache_append(const entmax_append_params* p, const void* Q, const void* K, const void* V, const int32_t* cu_seqlens,
+                        const int32_t* kv_len, const int32_t* page_table, const float* inv_freq, void* Qout, void* Kcache,
+                        void* Vcache, void* hip_stream);
+
 /* Scratch bytes the forward (is_bwd = 0) or backward (is_bwd != 0) needs for
  * these parameters; 0 if the parameters are invalid. Host-only, no GPU call. */
 size_t entmax_attn_workspace_bytes(const entmax_attn_params* p, int is_bwd);

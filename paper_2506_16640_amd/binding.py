@@ -353,3 +353,246 @@ def scale_proj_bwd(x, wb, wg, beta, gamma, dbeta, dgamma, gamma_scale=1.0, works
     if rc != 0:
         raise EntmaxAttnError(rc)
     return dx, dwb, dwg
+
+
+# ------------------------------------------------- serving: packed sequences, paged cache
+
+class SeqParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("nseq", "T", "Hq", "Hkv", "D", "dtype", "causal", "scale_layout", "logn_mode",
+                                               "bias_mode", "path", "page_size", "num_pages", "max_pages", "max_new", "max_keys")] +
+                [("alpha", ctypes.c_float), ("delta", ctypes.c_float)] +
+                [(n, ctypes.c_int64) for n in ("q_stride_t", "q_stride_h", "o_stride_t", "o_stride_h", "k_stride_p", "k_stride_h",
+                                               "k_stride_n", "v_stride_p", "v_stride_h", "v_stride_n")])
+
+
+class AppendParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("nseq", "T", "Hq", "Hkv", "D", "dtype", "page_size", "num_pages", "max_pages", "rot",
+                                               "interleaved")] +
+                [(n, ctypes.c_int64) for n in ("q_stride_t", "q_stride_h", "qo_stride_t", "qo_stride_h", "k_stride_t", "k_stride_h",
+                                               "v_stride_t", "v_stride_h", "kc_stride_p", "kc_stride_h", "kc_stride_n", "vc_stride_p",
+                                               "vc_stride_h", "vc_stride_n")])
+
+
+_lib.entmax_paged_attn_fwd.restype = ctypes.c_int
+_lib.entmax_paged_attn_fwd.argtypes = [ctypes.POINTER(SeqParams)] + [_vp] * 11 + [ctypes.c_size_t, _vp]
+_lib.entmax_packed_attn_fwd.restype = ctypes.c_int
+_lib.entmax_packed_attn_fwd.argtypes = [ctypes.POINTER(SeqParams)] + [_vp] * 9 + [ctypes.c_size_t, _vp]
+_lib.entmax_seq_workspace_bytes.restype = ctypes.c_size_t
+_lib.entmax_seq_workspace_bytes.argtypes = [ctypes.POINTER(SeqParams)]
+_lib.entmax_cache_append.restype = ctypes.c_int
+_lib.entmax_cache_append.argtypes = [ctypes.POINTER(AppendParams)] + [_vp] * 11
+
+_DTYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _rows_of(name, t, ref=None, heads=None):
+    """t is [T, H, D] with a contiguous last dimension, of ref's type and device."""
+    if t.dim() != 3 or (heads is not None and t.shape[1] != heads):
+        raise ValueError("%s must be [T,H,D]%s" % (name, "" if heads is None else " with %d heads" % heads))
+    if t.dtype not in _DTYPES:
+        raise TypeError("%s must be bfloat16 or float32" % name)
+    if t.numel() and t.stride(2) != 1:
+        raise ValueError("the last dimension of %s must be contiguous" % name)
+    if ref is not None:
+        if t.dtype != ref.dtype or t.device != ref.device:
+            raise TypeError("%s must have the dtype and device of the others" % name)
+        if t.shape[0] != ref.shape[0] or t.shape[2] != ref.shape[2]:
+            raise ValueError("%s must have as many rows and features as the others" % name)
+
+
+def _cache_of(name, t, ref):
+    if t.dim() != 4 or t.shape[3] != ref.shape[2]:
+        raise ValueError("%s must be [num_pages,Hkv,page_size,D]" % name)
+    if t.dtype != ref.dtype or t.device != ref.device:
+        raise TypeError("%s must have the dtype and device of the others" % name)
+    if t.numel() and t.stride(3) != 1:
+        raise ValueError("the last dimension of %s must be contiguous" % name)
+
+
+def _int_array(name, t, shape, ref):
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != len(shape) or t.device != ref.device or any(
+            w is not None and t.shape[k] != w for k, w in enumerate(shape)):
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s on the device of the others" %
+                         (name, "[%s]" % ", ".join("*" if w is None else str(w) for w in shape)))
+
+
+def _on_gpu(t):
+    if t.device.type != "cuda":
+        raise ValueError("the tensors must be on a GPU")
+
+
+def _stream_of(t):
+    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+
+
+def _row_strides(t):
+    """(token, head) strides; those of dimensions of size one or of empty tensors do not matter and are made valid ones."""
+    D = t.shape[2]
+    if t.numel() == 0:
+        return t.shape[1] * D, D
+    sh = t.stride(1) if t.shape[1] > 1 else D
+    return (t.stride(0) if t.shape[0] > 1 else max(t.shape[1] * D, (t.shape[1] - 1) * sh + D)), sh
+
+
+def _cache_strides(t):
+    P, H, n, D = t.shape
+    if t.numel() == 0:
+        return H * n * D, n * D, D
+    sn = t.stride(2) if n > 1 else D
+    sh = t.stride(1) if H > 1 else n * sn
+    return (t.stride(0) if P > 1 else H * n * D), sh, sn
+
+
+def _seq_params(q, Hkv, nseq, max_new, max_keys, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes, bias_mode, path, out):
+    _rows_of("q", q)
+    T, Hq, D = q.shape
+    if Hkv < 1 or Hq < 1 or Hq % Hkv:
+        raise ValueError("the query heads must be a multiple of the key/value heads")
+    if (beta is None) != (gamma is None):
+        raise ValueError("beta and gamma come together")
+    layout = 0 if beta is None else (1 if beta.dim() == 1 else 2)
+    for name, t, want in (("beta", beta, (Hq,) if layout == 1 else (Hq, T)), ("gamma", gamma, (Hq,) if layout == 1 else (Hq, T)),
+                          ("alibi_slopes", alibi_slopes, (Hq,))):
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != want or t.device != q.device):
+            raise ValueError("%s must be a contiguous float32 tensor of shape %s on the device of q" % (name, want))
+    if out is not None:
+        _rows_of("out", out, q, Hq)
+    p = SeqParams(nseq=nseq, T=T, Hq=Hq, Hkv=Hkv, D=D, dtype=_DTYPES[q.dtype], causal=int(bool(causal)), scale_layout=layout,
+                  logn_mode=int(logn_mode), bias_mode=int(bias_mode), path=int(path), max_new=int(max_new), max_keys=int(max_keys),
+                  alpha=float(alpha), delta=float(delta))
+    p.q_stride_t, p.q_stride_h = _row_strides(q)
+    p.o_stride_t, p.o_stride_h = (Hq * D, D) if out is None else _row_strides(out)
+    return p
+
+
+def _paged_params(q, k_cache, v_cache, page_table, max_new, max_keys, *args):
+    _cache_of("k_cache", k_cache, q)
+    _cache_of("v_cache", v_cache, q)
+    if v_cache.shape != k_cache.shape:
+        raise ValueError("v_cache must have the shape of k_cache")
+    _int_array("page_table", page_table, (None, None), q)
+    pages, Hkv, page, _ = k_cache.shape
+    most = page_table.shape[1] * page
+    p = _seq_params(q, Hkv, page_table.shape[0], q.shape[0] if max_new is None else max_new, most if max_keys is None else max_keys, *args)
+    p.page_size, p.num_pages, p.max_pages = page, pages, page_table.shape[1]
+    p.k_stride_p, p.k_stride_h, p.k_stride_n = _cache_strides(k_cache)
+    p.v_stride_p, p.v_stride_h, p.v_stride_n = _cache_strides(v_cache)
+    return p
+
+
+def _packed_params(q, k, v, nseq, max_len, *args):
+    _rows_of("q", q)
+    _rows_of("k", k, q)
+    _rows_of("v", v, q, k.shape[1])
+    most = q.shape[0] if max_len is None else max_len
+    p = _seq_params(q, k.shape[1], nseq, most, most, *args)
+    p.k_stride_n, p.k_stride_h = _row_strides(k)
+    p.v_stride_n, p.v_stride_h = _row_strides(v)
+    return p
+
+
+def _seq_workspace(p, device):
+    return torch.empty(max(int(_lib.entmax_seq_workspace_bytes(ctypes.byref(p))), 256), dtype=torch.uint8, device=device)
+
+
+def new_paged_workspace(q, k_cache, page_table, max_new=None, max_keys=None):
+    """Workspace for paged_attn_fwd calls of these shapes and bounds, whatever their other arguments."""
+    return _seq_workspace(_paged_params(q, k_cache, k_cache, page_table, max_new, max_keys, 1.5, None, None, 1.0, True, 0, None, 0, 0, None),
+                          q.device)
+
+
+def new_packed_workspace(q, k, cu_seqlens, max_len=None):
+    """Workspace for packed_attn_fwd calls of these shapes and bounds, whatever their other arguments."""
+    return _seq_workspace(_packed_params(q, k, k, cu_seqlens.shape[0] - 1, max_len, 1.5, None, None, 1.0, True, 0, None, 0, 0, None), q.device)
+
+
+def _seq_call(p, q, out, workspace, call):
+    _on_gpu(q)
+    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != q.device):
+        raise ValueError("workspace must be a contiguous uint8 tensor on the device of q")
+    with torch.cuda.device(q.device):
+        if out is None:
+            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)  # (rows that no sequence owns)
+        if workspace is None:
+            workspace = _seq_workspace(p, q.device)
+        rc = call(_ptr(out), _ptr(workspace), workspace.numel(), _stream_of(q))
+    if rc != 0:
+        raise EntmaxAttnError(rc)
+    return out
+
+
+def paged_attn_fwd(q, k_cache, v_cache, cu_seqlens, kv_len, page_table, max_new=None, max_keys=None, alpha=1.5, beta=None, gamma=None,
+                   delta=1.0, causal=True, logn_mode=0, alibi_slopes=None, bias_mode=0, path=0, out=None, workspace=None):
+    """Entmax attention of new tokens over a paged cache that holds their keys and values already (cache_append).
+    q [T,Hq,D]: the new tokens of all sequences, rows cu_seqlens[s] .. cu_seqlens[s+1]-1 those of sequence s; k_cache, v_cache
+    [num_pages,Hkv,page_size,D]; kv_len [nseq]: keys of each sequence, new ones included; page_table [nseq,max_pages]; all int32 on the GPU.
+    max_new, max_keys: bounds that no sequence passes (default: those of the shapes; close ones save workspace and launches).
+    beta, gamma: fp32 [Hq] or [Hq,T] or None; alibi_slopes: fp32 [Hq] or None.  Returns out [T,Hq,D]; rows that no sequence owns are left
+    as they are (zero in a tensor made here)."""
+    _rows_of("q", q)
+    p = _paged_params(q, k_cache, v_cache, page_table, max_new, max_keys, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes,
+                      bias_mode, path, out)
+    _int_array("cu_seqlens", cu_seqlens, (p.nseq + 1,), q)
+    _int_array("kv_len", kv_len, (p.nseq,), q)
+    return _seq_call(p, q, out, workspace, lambda o, ws, n, st: _lib.entmax_paged_attn_fwd(
+        ctypes.byref(p), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(cu_seqlens), _ptr(kv_len), _ptr(page_table), _ptr(beta), _ptr(gamma),
+        _ptr(alibi_slopes), o, ws, n, st))
+
+
+def packed_attn_fwd(q, k, v, cu_seqlens, max_len=None, alpha=1.5, beta=None, gamma=None, delta=1.0, causal=True, logn_mode=0,
+                    alibi_slopes=None, bias_mode=0, path=0, out=None, workspace=None):
+    """Entmax attention of whole prompts: q [T,Hq,D], k, v [T,Hkv,D], sequence s in rows cu_seqlens[s] .. cu_seqlens[s+1]-1.
+    max_len: no sequence is longer (default: T).  The other arguments and the result as in paged_attn_fwd."""
+    if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+        raise ValueError("cu_seqlens must be [nseq + 1]")
+    p = _packed_params(q, k, v, cu_seqlens.shape[0] - 1, max_len, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes, bias_mode, path,
+                       out)
+    _int_array("cu_seqlens", cu_seqlens, (p.nseq + 1,), q)
+    return _seq_call(p, q, out, workspace, lambda o, ws, n, st: _lib.entmax_packed_attn_fwd(
+        ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(beta), _ptr(gamma), _ptr(alibi_slopes), o, ws, n, st))
+
+
+def cache_append(k, v, k_cache, v_cache, cu_seqlens, kv_len, page_table, q=None, q_out=None, inv_freq=None, interleaved=False):
+    """Writes the new tokens' keys and values (k, v [T,Hkv,D]) to their places in the cache, keys rotated by their positions, and
+    returns the queries q [T,Hq,D] rotated likewise (q_out, which may be q; None without q).
+    inv_freq: fp32 [rot / 2], the angle per position of each pair of features; None: no rotation.  interleaved: pairs are neighbouring
+    features, else features i and i + rot / 2.  kv_len counts the new tokens.  Other arguments as in paged_attn_fwd."""
+    _rows_of("k", k)
+    _rows_of("v", v, k, k.shape[1])
+    _cache_of("k_cache", k_cache, k)
+    _cache_of("v_cache", v_cache, k)
+    if v_cache.shape != k_cache.shape or k_cache.shape[1] != k.shape[1]:
+        raise ValueError("k_cache and v_cache must be [num_pages,Hkv,page_size,D] with the heads of k")
+    _int_array("page_table", page_table, (None, None), k)
+    nseq = page_table.shape[0]
+    _int_array("cu_seqlens", cu_seqlens, (nseq + 1,), k)
+    _int_array("kv_len", kv_len, (nseq,), k)
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    if q is not None:
+        _rows_of("q", q, k)
+    if q_out is not None:
+        _rows_of("q_out", q_out, q, q.shape[1])
+    if inv_freq is not None and (inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or inv_freq.dim() != 1 or
+                                 inv_freq.device != k.device):
+        raise ValueError("inv_freq must be a contiguous float32 tensor [rot / 2] on the device of the others")
+    _on_gpu(k)
+    T, Hkv, D = k.shape
+    p = AppendParams(nseq=nseq, T=T, Hq=0 if q is None else q.shape[1], Hkv=Hkv, D=D, dtype=_DTYPES[k.dtype], page_size=k_cache.shape[2],
+                     num_pages=k_cache.shape[0], max_pages=page_table.shape[1], rot=0 if inv_freq is None else 2 * inv_freq.shape[0],
+                     interleaved=int(bool(interleaved)))
+    p.k_stride_t, p.k_stride_h = _row_strides(k)
+    p.v_stride_t, p.v_stride_h = _row_strides(v)
+    p.kc_stride_p, p.kc_stride_h, p.kc_stride_n = _cache_strides(k_cache)
+    p.vc_stride_p, p.vc_stride_h, p.vc_stride_n = _cache_strides(v_cache)
+    with torch.cuda.device(k.device):
+        if q is not None:
+            if q_out is None:
+                q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)  # (rows that no sequence owns)
+            p.q_stride_t, p.q_stride_h = _row_strides(q)
+            p.qo_stride_t, p.qo_stride_h = _row_strides(q_out)
+        rc = _lib.entmax_cache_append(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(kv_len), _ptr(page_table),
+                                      _ptr(inv_freq), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream_of(k))
+    if rc != 0:
+        raise EntmaxAttnError(rc)
+    return q_out

@@ -1,0 +1,98 @@
+// Host-side argument validation and workspace carving of the serving entry points (include/entmax_attn.h: packed
+// sequences, paged cache).  Plain C++, no HIP types.
+#pragma once
+#include "host_layout.h"
+
+namespace entmax {
+
+constexpr int kSeqMostKeys = 1 << 22;      // as for the other kernels
+constexpr long long kSeqMostBlocks = 1 << 23;  // workgroups of a launch (a launch has less than 2^32 threads)
+
+inline bool power_of_two(int x) { return x > 0 && (x & (x - 1)) == 0; }
+
+// a stride in elements: 16-byte steps, byte offsets that cannot wrap
+inline int check_stride(int64_t s, int64_t es, int64_t most) {
+  if (s < 0) return ENTMAX_ATTN_INVALID_ARG;
+  if (s > most) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  return (s * es) % 16 != 0 ? ENTMAX_ATTN_MISALIGNED : ENTMAX_ATTN_OK;
+}
+constexpr int64_t kMostStride = (int64_t)1 << 40;
+
+inline int check_heads(int32_t nseq, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype) {
+  if (nseq < 0 || T < 0 || Hq < 0 || Hkv <= 0) return ENTMAX_ATTN_INVALID_ARG;
+  if (Hq % Hkv != 0) return ENTMAX_ATTN_INVALID_ARG;
+  if (dtype != ENTMAX_ATTN_BF16 && dtype != ENTMAX_ATTN_FP32) return ENTMAX_ATTN_INVALID_ARG;
+  if (D != 64 && D != 128) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  if (Hq > 4096 || nseq > (1 << 20) || T > (1 << 26)) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  return ENTMAX_ATTN_OK;
+}
+inline int check_pages(int32_t page_size, int32_t num_pages, int32_t max_pages) {
+  if (num_pages < 0 || max_pages < 0) return ENTMAX_ATTN_INVALID_ARG;
+  if (!power_of_two(page_size) || page_size < 16 || page_size > 65536) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  return ENTMAX_ATTN_OK;
+}
+
+// groups of 128 folded rows (token, head of the group) over all sequences of a key/value head: sequence s starts at group
+// cu_seqlens[s] G / 128 + s, which leaves room for every sequence's ragged last group
+inline long long seq_blocks(int nseq, int T, int G) { return (long long)T * G / kBlockRows + nseq; }
+
+inline int check_seq_params(const entmax_seq_params* p) {
+  if (!p) return ENTMAX_ATTN_INVALID_ARG;
+  int rc = check_heads(p->nseq, p->T, p->Hq, p->Hkv, p->D, p->dtype);
+  if (rc != ENTMAX_ATTN_OK) return rc;
+  if (p->Hq == 0) return ENTMAX_ATTN_INVALID_ARG;
+  if ((p->causal | p->logn_mode | p->bias_mode | p->path) & ~1) return ENTMAX_ATTN_INVALID_ARG;
+  if (p->scale_layout < 0 || p->scale_layout > 2) return ENTMAX_ATTN_INVALID_ARG;
+  if (!(p->alpha > 1.0f) || !(p->alpha <= 2.0f) || !isfinite(p->delta)) return ENTMAX_ATTN_INVALID_ARG;
+  if (p->max_new < 0 || p->max_keys < 0) return ENTMAX_ATTN_INVALID_ARG;
+  const bool packed = p->page_size == 0 && p->num_pages == 0 && p->max_pages == 0;
+  if (packed) {
+    if (p->k_stride_p != 0 || p->v_stride_p != 0 || p->max_keys != p->max_new) return ENTMAX_ATTN_INVALID_ARG;
+  } else {
+    rc = check_pages(p->page_size, p->num_pages, p->max_pages);
+    if (rc != ENTMAX_ATTN_OK) return rc;
+    if (p->max_keys > (long long)p->max_pages * p->page_size) return ENTMAX_ATTN_INVALID_ARG;
+  }
+  if (p->max_keys > kSeqMostKeys) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  const int64_t es = p->dtype == ENTMAX_ATTN_BF16 ? 2 : 4;
+  const int64_t strides[10] = {p->q_stride_t, p->q_stride_h, p->o_stride_t, p->o_stride_h, p->k_stride_p,
+                               p->k_stride_h, p->k_stride_n, p->v_stride_p, p->v_stride_h, p->v_stride_n};
+  for (int k = 0; k < 10; ++k) {
+    rc = check_stride(strides[k], es, kMostStride);
+    if (rc != ENTMAX_ATTN_OK) return rc;
+  }
+  // (offsets of a few rows inside a tile are 32-bit numbers)
+  if (p->k_stride_n * es > (1 << 24) || p->v_stride_n * es > (1 << 24)) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  if (p->k_stride_n < p->D || p->v_stride_n < p->D) return ENTMAX_ATTN_INVALID_ARG;  // rows overlap
+  if (p->o_stride_t < p->D || (p->Hq > 1 && p->o_stride_h < p->D)) return ENTMAX_ATTN_INVALID_ARG;
+  if (seq_blocks(p->nseq, p->T, p->Hq / p->Hkv) * p->Hkv > kSeqMostBlocks) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  return ENTMAX_ATTN_OK;
+}
+
+inline int check_append_params(const entmax_append_params* p) {
+  if (!p) return ENTMAX_ATTN_INVALID_ARG;
+  int rc = check_heads(p->nseq, p->T, p->Hq, p->Hkv, p->D, p->dtype);
+  if (rc != ENTMAX_ATTN_OK) return rc;
+  rc = check_pages(p->page_size, p->num_pages, p->max_pages);
+  if (rc != ENTMAX_ATTN_OK) return rc;
+  if (p->rot < 0 || p->rot > p->D || (p->interleaved & ~1)) return ENTMAX_ATTN_INVALID_ARG;
+  if (p->rot % 16 != 0) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  if ((long long)p->max_pages * p->page_size > 0x7fffffffLL) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  const int64_t es = p->dtype == ENTMAX_ATTN_BF16 ? 2 : 4;
+  const int64_t strides[14] = {p->q_stride_t, p->q_stride_h, p->qo_stride_t, p->qo_stride_h, p->k_stride_t, p->k_stride_h, p->v_stride_t,
+                               p->v_stride_h, p->kc_stride_p, p->kc_stride_h, p->kc_stride_n, p->vc_stride_p, p->vc_stride_h, p->vc_stride_n};
+  for (int k = 0; k < 14; ++k) {
+    rc = check_stride(strides[k], es, kMostStride);
+    if (rc != ENTMAX_ATTN_OK) return rc;
+  }
+  if (p->kc_stride_n < p->D || p->vc_stride_n < p->D) return ENTMAX_ATTN_INVALID_ARG;
+  if (p->Hq > 0 && (p->qo_stride_t < p->D || (p->Hq > 1 && p->qo_stride_h < p->D))) return ENTMAX_ATTN_INVALID_ARG;
+  return ENTMAX_ATTN_OK;
+}
+
+inline size_t seq_workspace_bytes_of(const entmax_seq_params* p) {
+  if (check_seq_params(p) != ENTMAX_ATTN_OK) return 0;
+  return kAlign;
+}
+
+}  // namespace entmax

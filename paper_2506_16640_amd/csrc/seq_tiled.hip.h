@@ -1,0 +1,421 @@
+// Entmax attention of packed sequences over packed or paged keys, any density: one workgroup per 128 folded rows of a
+// key/value head (SeqRows), key tiles through LDS, scores recomputed by every sweep (S^T = K Q^T, a lane owns a row):
+//   1. a sample of the key tiles: bounds and a starting point for the threshold tau of
+//        f(tau) = sum_j [y_j - tau]_+^r - 1 = 0,   y = (alpha-1) s,  r = 1 / (alpha-1)
+//   2. sweeps over K that evaluate f and step (solve_step()); the first one notes which 32-key blocks can hold a positive term at all
+//   3. a sweep over K and V: O^T = V^T P^T on the matrix cores.  The accumulators of S^T are the second operand as they are; V^T comes out
+//      of row-major tiles through transposing LDS reads (ds_read_b64_tr_b16: sixteen lanes give four rows of sixteen
+//      elements, each lane gets a column), so that no transposed copy of V exists anywhere.
+#pragma once
+#include "fwd.hip.h"
+#include "seq.hip.h"
+
+namespace entmax {
+
+struct SeqArgs {
+  SeqGeom g;
+  const void* Q;
+  const void* K;
+  const void* V;
+  void* O;
+  int nblk;        // 128-row groups per key/value head (seq_blocks())
+  int mask_words;  // uint32 words that hold a bit per 32-key block
+};
+
+// The 128-row group of this workgroup: sequence, key/value head, first row; false: nothing to do.  The head runs fastest, so that a
+// head's groups meet on one XCD where the heads divide among the eight of them; groups run from the last to the first, a sequence's long rows first.
+__device__ __forceinline__ bool seq_block(const SeqGeom& g, int nblk, SeqView& v, int& hk, int& r0) {
+  hk = __builtin_amdgcn_readfirstlane(blockIdx.x % g.Hkv);
+  const int blk = nblk - 1 - __builtin_amdgcn_readfirstlane(blockIdx.x / g.Hkv);
+  // sequence s has the groups from cu[s] G / 128 + s on
+  const int G = g.G;
+  auto first = [G](int c, int s) { return (long long)c * G / kBlockRows + s; };
+  const int s = find_seq(g.cu, g.nseq, blk, first);
+  if (s >= g.nseq || !load_seq(g, s, v)) return false;
+  const long long local = blk - first(v.row0, s);
+  if (local < 0 || local * kBlockRows >= (long long)v.n * G) return false;
+  r0 = (int)local * kBlockRows;
+  return true;
+}
+
+template <typename T, int D>
+struct SeqTiledCfg {
+  static constexpr int KT = sizeof(T) == 2 ? 64 : 32;
+  static constexpr int kTileBytes = KT * D * (int)sizeof(T);
+  static constexpr int kOcc = sizeof(T) == 2 && D == 64 ? 3 : (sizeof(T) == 2 ? 2 : 1);
+  static size_t lds_bytes(int mask_words) { return 4 * (size_t)kTileBytes + (size_t)(kWaves + 1) * mask_words * 4; }
+};
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint2 read_transposed(const char* lds) {
+  const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)lds);
+  return __builtin_bit_cast(uint2, v);
+}
+
+// Fragments of V^T for the product that contracts over the 16 keys 16 c .. 16 c + 15 of a 32-key block, in the order of the accumulators:
+// element e of half hh is key 16 c + 8 (e / 4) + 4 hh + e % 4.
+template <typename T, int D, int KT>
+struct SeqValues {
+  static constexpr int NM = D / 32;
+  using VT = SeqTile<T, D, KT, sizeof(T) == 2>;
+  int voff[NM];
+  int li, hh;
+  __device__ __forceinline__ void init(int lane) {
+    li = lane & 31;
+    hh = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+      const int p = lane & 15, row = 4 * hh + (p >> 2);
+#pragma unroll
+      for (int mm = 0; mm < NM; ++mm)
+        voff[mm] = VT::off(row, 4 * mm + 2 * ((lane >> 4) & 1) + ((p & 3) >> 1)) + (p & 1) * 8;
+    }
+  }
+  __device__ __forceinline__ Frag<T> frag(const char* vt, int sb, int c, int mm) const {
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+      const char* at = vt + voff[mm] + (sb * 32 + 16 * c) * VT::kRowBytes;
+      const uint2 x = read_transposed(at), y = read_transposed(at + 8 * VT::kRowBytes);
+      f.v = u32x4_t{x.x, x.y, y.x, y.y};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = value(vt, sb * 32 + 16 * c + 8 * (e >> 2) + 4 * hh + (e & 3), 32 * mm + li);
+        if (e < 4) f.lo[e] = x; else f.hi[e - 4] = x;
+      }
+    }
+    return f;
+  }
+  static __device__ __forceinline__ float value(const char* vt, int row, int feature) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const char* at = vt + VT::off(row, feature / E) + (feature % E) * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2)
+      return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16);
+    else
+      return *reinterpret_cast<const float*>(at);
+  }
+  static __device__ __forceinline__ bool not_finite(const Frag<T>& f) {
+    bool bad = false;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) bad = bad || (f.v[k] & 0x7f80u) == 0x7f80u || (f.v[k] & 0x7f800000u) == 0x7f800000u;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        bad = bad || (__float_as_uint(f.lo[k]) & 0x7f800000u) == 0x7f800000u || (__float_as_uint(f.hi[k]) & 0x7f800000u) == 0x7f800000u;
+    }
+    return bad;
+  }
+  // oacc += V^T P^T of block sb.  special: some row does not see some key of the block (then 0 x infinity must not come in: where a value is not finite,
+  // the products with non-zero probabilities are formed one by one).
+  __device__ __forceinline__ void accumulate(const char* vt, int sb, const float (&p)[16], bool special, f32x16_t (&oacc)[NM]) const {
+    if (special) {
+      bool bad = false;
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int mm = 0; mm < NM; ++mm) bad = not_finite(frag(vt, sb, c, mm)) || bad;
+      if (__ballot(bad) != 0ull) {
+        one_by_one(vt, sb, p, oacc);
+        return;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      // the probabilities as the sum of two bf16 numbers: rounded to one, they would cost up to 2^-9 |v| of the output
+      Frag<T> ph, pl;
+      Elem<T>::pack_split(p + 8 * c, ph, pl);
+#pragma unroll
+      for (int mm = 0; mm < NM; ++mm) {
+        const Frag<T> v = frag(vt, sb, c, mm);
+        oacc[mm] = Elem<T>::mma(v, ph, oacc[mm]);
+        if constexpr (Elem<T>::kSplit) oacc[mm] = Elem<T>::mma(v, pl, oacc[mm]);
+      }
+    }
+  }
+  __device__ __forceinline__ void one_by_one(const char* vt, int sb, const float (&p)[16], f32x16_t (&oacc)[NM]) const {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float other = __shfl_xor(p[e], 32);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const float pk = half == hh ? p[e] : other;
+        if (pk > 0.f) {
+          const int row = sb * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+#pragma unroll
+          for (int mm = 0; mm < NM; ++mm)
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+              oacc[mm][x] = fmaf(pk, value(vt, row, 32 * mm + 8 * (x >> 2) + 4 * hh + (x & 3)), oacc[mm][x]);
+        }
+      }
+    }
+  }
+};
+
+// Four consecutive features of a lane's row, in the type of O
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, float x0, float x1, float x2, float x3) {
+  if constexpr (sizeof(T) == 2) {
+    typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+    const bf16x4_t b = {(__bf16)x0, (__bf16)x1, (__bf16)x2, (__bf16)x3};
+    *reinterpret_cast<uint2*>(dst) = __builtin_bit_cast(uint2, b);
+  } else {
+    *reinterpret_cast<f32x4_t*>(dst) = f32x4_t{x0, x1, x2, x3};
+  }
+}
+
+template <typename T, int D, int AM>
+__global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled_kernel(SeqArgs A) {
+  using Cfg = SeqTiledCfg<T, D>;
+  constexpr int KT = Cfg::KT, NSB = KT / 32, NC = D / 16, NM = D / 32, TB = Cfg::kTileBytes;
+  using KTile = SeqTile<T, D, KT, false>;
+  using Vals = SeqValues<T, D, KT>;
+  using VTile = typename Vals::VT;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const SeqGeom& g = A.g;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  SeqView v;
+  int hk, blk0;
+  if (!seq_block(g, A.nblk, v, hk, blk0)) return;  // (the same for the whole workgroup)
+  SeqKeys keys, vals;
+  keys.init(g, v, A.K, hk, false, sizeof(T));
+  vals.init(g, v, A.V, hk, true, sizeof(T));
+  SeqRows<T, D> q;
+  q.init(g, v, A.Q, hk, blk0 + wave * 32);
+  const int last_row = min(v.n * g.G, blk0 + kBlockRows) - 1;
+  const int block_lim = g.causal ? max(0, min(v.L - v.n + last_row / g.G + 1, v.L)) : v.L;
+  const int ntiles = __builtin_amdgcn_readfirstlane((block_lim + KT - 1) / KT);
+  const bool holes = seq_has_holes(keys, block_lim);
+  const float r = 1.0f / (g.alpha - 1.0f);
+  const int lane = q.lane;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+
+  WaveMask wm;
+  wm.words = reinterpret_cast<uint32_t*>(smem + 4 * TB);
+  wm.nwords = A.mask_words;
+  for (int w = threadIdx.x; w < (kWaves + 1) * A.mask_words; w += kThreads) wm.words[w] = 0u;
+
+  FragOff<T> koff[NC];
+#pragma unroll
+  for (int cc = 0; cc < NC; ++cc) koff[cc] = FragOff<T>::template make<typename KTile::Tile>(q.li, 2 * cc + q.hh);
+  auto scores = [&](const char* tl, int sb, int kt) {
+    f32x16_t acc = q.start(kt * KT + sb * 32);
+#pragma unroll
+    for (int cc = 0; cc < NC; ++cc) acc = Elem<T>::mma(koff[cc].load(tl, sb * 32 * KTile::kRowBytes), q.qf[cc], acc);
+    return acc;
+  };
+  auto visible = [&](int kt) -> uint32_t {  // blocks of the tile that some row of the wave sees
+    const int n = min(max((q.lim_max - kt * KT + 31) >> 5, 0), NSB);
+    return (1u << n) - 1u;
+  };
+  auto next = [&](int kt, auto needed) {
+    while (kt < ntiles && !needed(kt)) ++kt;
+    return kt;
+  };
+  // K tiles kt with needed(kt) (uniform), three of them under way while one is worked on: body(kt, tile)
+  auto sweep_k = [&](auto needed, auto body) {
+    typename KTile::Pages pg;
+    auto issue = [&](int t, int buf) { KTile::load(keys, pg, t * KT, v.L, lds0 + (uint32_t)buf * TB, wave, lane); };
+    int t0 = next(0, needed), t1 = ntiles, t2 = ntiles, t3 = ntiles;
+    __syncthreads();  // (the tile buffers are free)
+    if (t0 < ntiles) {
+      pg.ask(keys, t0 * KT, v.L, wave);
+      issue(t0, 0);
+      t1 = next(t0 + 1, needed);
+    }
+    if (t1 < ntiles) {
+      pg.ask(keys, t1 * KT, v.L, wave);
+      issue(t1, 1);
+      t2 = next(t1 + 1, needed);
+    }
+    if (t2 < ntiles) {
+      pg.ask(keys, t2 * KT, v.L, wave);
+      issue(t2, 2);
+      t3 = next(t2 + 1, needed);
+      if (t3 < ntiles) pg.ask(keys, t3 * KT, v.L, wave);
+      lds_loads_wait<2 * KTile::L>();
+    } else if (t1 < ntiles) {
+      lds_loads_wait<KTile::L>();
+    } else {
+      lds_loads_wait<0>();
+    }
+    __syncthreads();
+    int cur = 0;
+    while (t0 < ntiles) {
+      int t4 = ntiles;
+      if (t3 < ntiles) {
+        issue(t3, (cur + 3) & 3);  // that of the tile before, which every wave has left
+        t4 = next(t3 + 1, needed);
+        if (t4 < ntiles) pg.ask(keys, t4 * KT, v.L, wave);
+      }
+      body(t0, smem + cur * TB);
+      if (t3 < ntiles)
+        lds_loads_wait<2 * KTile::L>();
+      else if (t2 < ntiles)
+        lds_loads_wait<KTile::L>();
+      else
+        lds_loads_wait<0>();
+      __syncthreads();
+      cur = (cur + 1) & 3;
+      t0 = t1;
+      t1 = t2;
+      t2 = t3;
+      t3 = t4;
+    }
+  };
+  // fn(acc, sb, masked) on the scores of the blocks in act
+  auto each_block = [&](int kt, const char* tl, uint32_t act, auto fn) {
+    f32x16_t acc[NSB];
+#pragma unroll
+    for (int sb = 0; sb < NSB; ++sb)
+      if (act & (1u << sb)) acc[sb] = scores(tl, sb, kt);
+#pragma unroll
+    for (int sb = 0; sb < NSB; ++sb) {
+      if (!(act & (1u << sb))) continue;
+      const int j0 = kt * KT + sb * 32;
+      const bool masked = holes || j0 + 32 > q.lim_min;
+      if (masked) q.mask(acc[sb], j0, keys, holes);
+      fn(acc[sb], sb, masked);
+    }
+  };
+
+  // ------------------------------------------------------------ 1. a sample of the tiles
+  // (about eight tiles; all of them where there are no more, and where a tile may show a row no key at all)
+  const int every = holes ? 1 : max(1, ntiles >> 3);
+  float m = -kInf, ms1 = 0.f, ms2 = 0.f, msn = 0.f;
+  sweep_k([&](int kt) { return kt % every == 0; },
+          [&](int kt, const char* tl) {
+            each_block(kt, tl, visible(kt), [&](f32x16_t& acc, int, bool masked) {
+              if (!masked && AM != 0) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  ms1 += acc[e];
+                  ms2 = fmaf(acc[e], acc[e], ms2);
+                }
+                msn += 32.f;
+              }
+              m = fmaxf(m, max16(acc));
+            });
+          });
+  m = fmaxf(m, __shfl_xor(m, 32));
+  ms1 += __shfl_xor(ms1, 32);
+  ms2 += __shfl_xor(ms2, 32);
+  const bool live = q.lim > 0 && m > -kInf;
+  float my = live ? q.a * m : 0.f;
+  float lo = my - 1.0f;  // (the largest score is at least the sample's)
+  const float lo0 = lo;  // blocks without a term above it are zero for good
+  const float below = q.lim > 0 ? __builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)q.lim)) : 1.f;
+  float hi = every == 1 ? my - below : kInf;
+  float tau = lo;
+  if (live && msn >= 64.f) {
+    const float mean = ms1 / msn, var = ms2 / msn - mean * mean;
+    float t0;
+    if (var > 0.f && gauss_start<AM>(q.a * mean, q.a * sqrtf(var), (float)q.lim, t0)) tau = fminf(fmaxf(t0, lo), hi);
+  }
+
+  // ------------------------------------------------------------ 2. threshold
+  bool done = !live;
+  int iter = 0, more;
+  do {
+    const bool wave_on = __ballot(!done) != 0ull;
+    RowSums sums;
+    sums.clear();
+    const bool first = iter == 0;
+    sweep_k([&](int kt) { return first || wm.tile_bits<NSB>(kWaves, kt) != 0u; },
+            [&](int kt, const char* tl) {
+              if (!wave_on) return;
+              uint32_t act = visible(kt);
+              if (!first) act &= wm.tile_bits<NSB>(wave, kt);
+              each_block(kt, tl, act, [&](f32x16_t& acc, int sb, bool masked) {
+                const float lm = max16(acc);
+                if (first) {
+                  m = fmaxf(m, lm);
+                  const bool any = live && lm > -kInf && fmaf(lm, q.a, -lo0) > 0.f;
+                  if (__ballot(any) != 0ull && lane == 0) wm.set(wave, kt * NSB + sb);
+                }
+                const bool cand = lm > -kInf && fmaf(lm, q.a, -tau) > 0.f && !done;
+                if (__ballot(cand) == 0ull) return;
+                accumulate_block<AM>(sums, acc, q.a, tau, r, masked);
+              });
+            });
+    if (first) {
+      wm.merge(threadIdx.x);
+      m = fmaxf(m, __shfl_xor(m, 32));
+      my = live ? q.a * m : 0.f;
+      lo = fmaxf(lo, my - 1.0f);
+      hi = my - below;
+    }
+    sums.combine_halves();
+    if (!done) done = solve_step<AM>(sums, r, tau, lo, hi);
+    ++iter;
+    more = __syncthreads_or(done ? 0 : 1);
+  } while (more && iter < kMaxSolveIters);
+
+  // ------------------------------------------------------------ 3. O^T = V^T P^T
+  f32x16_t oacc[NM];
+#pragma unroll
+  for (int mm = 0; mm < NM; ++mm)
+    oacc[mm] = f32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  Vals vv;
+  vv.init(lane);
+  {
+    auto needed = [&](int kt) { return wm.tile_bits<NSB>(kWaves, kt) != 0u; };
+    typename KTile::Pages pk;
+    typename VTile::Pages pv;
+    auto ask = [&](int t) {
+      pk.ask(keys, t * KT, v.L, wave);
+      pv.ask(vals, t * KT, v.L, wave);
+    };
+    auto issue = [&](int t, int buf) {
+      KTile::load(keys, pk, t * KT, v.L, lds0 + (uint32_t)(2 * buf) * TB, wave, lane);
+      VTile::load(vals, pv, t * KT, v.L, lds0 + (uint32_t)(2 * buf + 1) * TB, wave, lane);
+    };
+    int t0 = next(0, needed), t1 = ntiles;
+    __syncthreads();
+    if (t0 < ntiles) {
+      ask(t0);
+      issue(t0, 0);
+      t1 = next(t0 + 1, needed);
+      if (t1 < ntiles) ask(t1);
+    }
+    lds_loads_wait<0>();
+    __syncthreads();
+    int cur = 0;
+    while (t0 < ntiles) {
+      int t2 = ntiles;
+      if (t1 < ntiles) {
+        issue(t1, cur ^ 1);
+        t2 = next(t1 + 1, needed);
+        if (t2 < ntiles) ask(t2);
+      }
+      const char* tl = smem + cur * 2 * TB;
+      const int kt = t0;
+      each_block(kt, tl, visible(kt) & wm.tile_bits<NSB>(wave, kt), [&](f32x16_t& acc, int sb, bool masked) {
+        const float lm = max16(acc);
+        const bool cand = live && lm > -kInf && fmaf(lm, q.a, -tau) > 0.f;
+        if (__ballot(cand) == 0ull) return;  // every probability of the block is zero
+        float p[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = masked && acc[e] == -kInf ? 0.f : fmaf(acc[e], q.a, -tau);
+          p[e] = live ? pow_r<AM>(fmaxf(x, 0.f), r) : 0.f;
+        }
+        vv.accumulate(tl + TB, sb, p, masked, oacc);
+      });
+      lds_loads_wait<0>();
+      __syncthreads();
+      cur ^= 1;
+      t0 = t1;
+      t1 = t2;
+    }
+  }
+  if (!q.valid) return;
+  T* o = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + q.t) * g.o_st + (long long)q.head * g.o_sh;
+#pragma unroll
+  for (int mm = 0; mm < NM; ++mm)
+#pragma unroll
+    for (int x = 0; x < 16; x += 4)
+      store4<T>(o + 32 * mm + 2 * x + 4 * q.hh, oacc[mm][x], oacc[mm][x + 1], oacc[mm][x + 2], oacc[mm][x + 3]);
+}
+
+}  // namespace entmax
