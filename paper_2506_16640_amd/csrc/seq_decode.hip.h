@@ -1,0 +1,571 @@
+// Serving attention of sequences with few new tokens (at most kSplitRows folded rows of a key/value head) against any number of keys: the keys, not
+// the rows, are split over the chip, and the bound is reading K once.
+//   seq_scores_kernel  raw scores d of the rows (y = (alpha-1) s = a d) for a piece of the keys, on the matrix cores straight from
+//                      memory, to the workspace -- only the 32-key blocks of a row that hold a score with y of at least (largest so far) - 1: the
+//                      others are zero at the lowest possible threshold.  What was written is noted beside each chunk's maximum (pack_cmax()).
+//   seq_solve_kernel   a workgroup per row: candidates, threshold, and, where they are few, the output from the values of the support
+//   seq_pv_kernel      rows with long supports: O^T = V^T P^T from the scores, keys split again; the last workgroup of a head adds the parts up
+// From the second kernel on y and the threshold are taken relative to the row's largest score (y = a (d - top), tau in [-1, 0)): large scores then cost no
+// bits of the probabilities.
+#pragma once
+#include "decode.hip.h"
+#include "seq.hip.h"
+#include "seq_layout.h"
+#include "seq_tiled.hip.h"
+
+namespace entmax {
+
+struct SeqDecodeArgs {
+  SeqGeom g;
+  const void* Q;
+  const void* K;
+  const void* V;
+  void* O;
+  float* scores;     // [nseq * Hkv][rows][nks]
+  uint32_t* cmax;    // [nseq * Hkv][rows][nchunks]
+  float* mult;       // [nseq * Hkv][rows] the rows' a
+  float2* found;     // [nseq * Hkv][rows] (threshold, or +inf: the row is finished; largest score)
+  int* arrived;      // [nseq * Hkv] workgroups of seq_pv_kernel that have left their part
+  float* part;       // [nseq * Hkv][pv_splits][rows][D]
+  int rows;          // rows of a head there is room for: min(max_new G, kSplitRows)
+  int nks, nchunks;
+  int chunks_per_wg, splits;    // seq_scores_kernel
+  int pv_keys, pv_splits;       // seq_pv_kernel: keys of a workgroup, workgroups of a head
+};
+
+// How far below the row's largest raw score a key may lie and still have a term at the lowest threshold (a little more, for the rounding)
+__device__ __forceinline__ float score_reach(float a) { return a > 0.f ? 1.00001f / a : kInf; }
+
+template <typename T, int D, int NQB>
+__global__ __launch_bounds__(kThreads) void seq_scores_kernel(SeqDecodeArgs A) {
+  constexpr int NC = D / 16;
+  constexpr int kBlocksPerChunk = kDecodeChunk / 32;
+  __shared__ int rowmax[NQB * 32];                             // ordered_bits() of a row's largest score so far
+  __shared__ float wmax[kDecodeMfmaChunks][kWaves][NQB * 32];  // per chunk: what each wave saw and wrote
+  __shared__ uint32_t wmask[kDecodeMfmaChunks][kWaves][NQB * 32];
+  const SeqGeom& g = A.g;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, hh = lane >> 5;
+  const int split = blockIdx.x % A.splits, s = blockIdx.x / A.splits, hk = blockIdx.y;
+  const int head = s * g.Hkv + hk;
+  if (split == 0 && tid == 0) A.arrived[head] = 0;
+  SeqView v;
+  if (!load_seq(g, s, v) || !split_seq(g, v)) return;
+  const int chunk0 = split * A.chunks_per_wg, jc0 = chunk0 * kDecodeChunk;
+  if (jc0 >= v.L) return;
+  const int nblk = min(A.chunks_per_wg * kBlocksPerChunk, (v.L - jc0 + 31) >> 5);  // 32-key blocks of this workgroup
+  SeqKeys keys;
+  keys.init(g, v, A.K, hk, false, sizeof(T));
+  auto page_of = [&](int blk) { return keys.page(min(jc0 + blk * 32 + li, v.L - 1)); };
+  Frag<T> kf[NC], kn[NC];
+  auto fetch = [&](Frag<T>* dst, int blk, int pg) {  // (rows past the end repeat the last one; their scores are masked)
+    const char* row = keys.row_in(pg, min(jc0 + blk * 32 + li, v.L - 1)) + 8 * hh * sizeof(T);
+#pragma unroll
+    for (int cc = 0; cc < NC; ++cc) dst[cc] = Elem<T>::load(row + 16 * cc * sizeof(T));
+  };
+  int pg = 0, pg_next = 0;  // pages of the blocks in kn and of those after them
+  if (wave < nblk) {
+    pg = page_of(wave);
+    if (wave + kWaves < nblk) pg_next = page_of(wave + kWaves);
+    fetch(kn, wave, pg);
+  }
+  const int R = v.n * g.G;
+  SeqRows<T, D> q[NQB];
+  float top[NQB], cm[NQB], reach[NQB];
+  uint32_t mask[NQB];
+#pragma unroll
+  for (int qb = 0; qb < NQB; ++qb) {
+    q[qb].init(g, v, A.Q, hk, qb * 32);
+    top[qb] = cm[qb] = -kInf;
+    mask[qb] = 0u;
+    reach[qb] = score_reach(q[qb].a);
+    if (split == 0 && wave == 0 && hh == 0 && q[qb].valid) A.mult[(long long)head * A.rows + qb * 32 + li] = q[qb].a;
+  }
+  if (tid < NQB * 32) rowmax[tid] = ordered_bits(-kInf);
+  for (int e = tid; e < kDecodeMfmaChunks * kWaves * NQB * 32; e += kThreads) {
+    (&wmax[0][0][0])[e] = -kInf;
+    (&wmask[0][0][0])[e] = 0u;
+  }
+  __syncthreads();
+  for (int blk = wave; blk < nblk; blk += kWaves) {
+#pragma unroll
+    for (int cc = 0; cc < NC; ++cc) kf[cc] = kn[cc];
+    const uint32_t holes = (uint32_t)__ballot(keys.is_hole(pg));  // of the block's 32 keys
+    if (blk + kWaves < nblk) {
+      pg = pg_next;
+      if (blk + 2 * kWaves < nblk) pg_next = page_of(blk + 2 * kWaves);
+      fetch(kn, blk + kWaves, pg);
+    }
+    const int j0 = jc0 + blk * 32;
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      if (qb * 32 >= R) break;
+      f32x16_t acc = q[qb].start(j0);
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc) acc = Elem<T>::mma(kf[cc], q[qb].qf[cc], acc);
+      if (j0 + 32 > q[qb].lim_min || holes != 0u) {
+        const int rel = q[qb].lim - j0;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int k = q[qb].key_of(e);
+          acc[e] = k < rel && ((holes >> k) & 1u) == 0u ? acc[e] : -kInf;
+        }
+      }
+      float m = max16(acc);
+      m = fmaxf(m, __shfl_xor(m, 32));
+      cm[qb] = fmaxf(cm[qb], m);
+      // (an older value only writes more)
+      top[qb] = fmaxf(top[qb], from_ordered_bits(__hip_atomic_load(&rowmax[qb * 32 + li], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)));
+      // (m = -inf for rows that see none of the block; the row's first lane decides for both)
+      const uint32_t rows = (uint32_t)__ballot(m > -kInf && m >= top[qb] - reach[qb] && q[qb].lim > 0);
+      if ((rows >> li) & 1u) {
+        if (m > top[qb]) {
+          top[qb] = m;
+          atomicMax(&rowmax[qb * 32 + li], ordered_bits(m));
+        }
+        mask[qb] |= 1u << (blk % kBlocksPerChunk);
+        float* dst = A.scores + ((long long)head * A.rows + qb * 32 + li) * A.nks + j0 + 4 * hh;  // (nks: a multiple of 32)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *reinterpret_cast<f32x4_t*>(dst + 8 * q4) = f32x4_t{acc[4 * q4], acc[4 * q4 + 1], acc[4 * q4 + 2], acc[4 * q4 + 3]};
+      }
+      if (blk % kBlocksPerChunk + kWaves >= kBlocksPerChunk || blk + kWaves >= nblk) {  // this wave's last block of the chunk
+        if (hh == 0) {
+          wmax[blk / kBlocksPerChunk][wave][qb * 32 + li] = cm[qb];
+          wmask[blk / kBlocksPerChunk][wave][qb * 32 + li] = mask[qb];
+        }
+        cm[qb] = -kInf;
+        mask[qb] = 0u;
+      }
+    }
+  }
+  __syncthreads();
+  for (int e = tid; e < A.chunks_per_wg * NQB * 32; e += kThreads) {
+    const int c = e / (NQB * 32), i = e % (NQB * 32);
+    if (i >= R || c * kBlocksPerChunk >= nblk) continue;
+    float mx = wmax[c][0][i];
+    uint32_t mk = wmask[c][0][i];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+      mx = fmaxf(mx, wmax[c][w][i]);
+      mk |= wmask[c][w][i];
+    }
+    A.cmax[((long long)head * A.rows + i) * A.nchunks + chunk0 + c] = pack_cmax(mx, mk);
+  }
+}
+
+// Sums over the workgroup (NT threads) of three values and the smallest of a fourth, the same in every thread.  Calls alternate between
+// the halves of buf (parity), so that one barrier per call is enough.
+template <int NT>
+__device__ __forceinline__ RowSums block_sums(RowSums s, float* buf, int parity) {
+  constexpr int kW = NT / 64;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    s.s0 += __shfl_xor(s.s0, off);
+    s.s1 += __shfl_xor(s.s1, off);
+    s.s2 += __shfl_xor(s.s2, off);
+    s.xmin = fminf(s.xmin, __shfl_xor(s.xmin, off));
+  }
+  f32x4_t* mine = reinterpret_cast<f32x4_t*>(buf) + parity * kW;
+  if ((threadIdx.x & 63) == 0) mine[threadIdx.x >> 6] = f32x4_t{s.s0, s.s1, s.s2, s.xmin};
+  __syncthreads();
+  RowSums t;
+  t.clear();
+#pragma unroll
+  for (int w = 0; w < kW; ++w) {
+    const f32x4_t o = mine[w];
+    t.s0 += o[0];
+    t.s1 += o[1];
+    t.s2 += o[2];
+    t.xmin = fminf(t.xmin, o[3]);
+  }
+  return t;
+}
+
+constexpr int kSolveThreads = 512;
+constexpr int kSolveList = 512;   // candidates kept in LDS, their output gathered here; rows with more are left to seq_pv_kernel
+
+template <typename T, int D, int AM>
+__global__ __launch_bounds__(kSolveThreads) void seq_solve_kernel(SeqDecodeArgs A) {
+  constexpr int NT = kSolveThreads, kW = NT / 64;
+  constexpr int E = 16 / (int)sizeof(T), LR = D / E;  // features of a lane, lanes of a value row
+  constexpr int kGroups = NT / LR;
+  __shared__ float2 list[kSolveList];          // (key index bits, raw score, then y)
+  __shared__ __attribute__((aligned(16))) float red[2 * kW * 4];
+  __shared__ float wmax[kW], wtop[kW];
+  __shared__ int count;
+  __shared__ float osum[kW * D];
+  const SeqGeom& g = A.g;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int row = blockIdx.x % A.rows, head = blockIdx.x / A.rows, hk = head % g.Hkv, s = head / g.Hkv;
+  SeqView v;
+  if (!load_seq(g, s, v) || !split_seq(g, v) || row >= v.n * g.G) return;
+  const int t = row / g.G, qh = hk * g.G + row % g.G;
+  const int lim = g.causal ? max(0, min(v.L - v.n + t + 1, v.L)) : v.L;
+  const long long at = (long long)head * A.rows + row;
+  T* o = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + t) * g.o_st + (long long)qh * g.o_sh;
+  float* d = A.scores + at * A.nks;
+  const float a = A.mult[at], reach = score_reach(a);
+  const uint32_t* cmax = A.cmax + at * A.nchunks;
+  const int nchunks = (v.L + kDecodeChunk - 1) / kDecodeChunk;
+  const float r = 1.0f / (g.alpha - 1.0f);
+  SeqKeys vals;
+  vals.init(g, v, A.V, hk, true, sizeof(T));
+  // lower bound of the largest score from the chunks' rounded maxima
+  uint32_t first_words = kCmaxNone;  // the words of chunks 0..63: every wave's own copy
+  if (lane < nchunks) first_words = cmax[lane];
+  float m = cmax_floor(first_words);
+  for (int c = 64 + tid; c < nchunks; c += NT) m = fmaxf(m, cmax_floor(cmax[c]));
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+  if (lane == 0) wmax[wave] = m;
+  if (tid == 0) count = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kW; ++w) m = fmaxf(m, wmax[w]);
+  if (lim == 0 || m == -kInf) {  // no visible key: an empty sum
+    if (tid < D) Elem<T>::store(o, tid, 0.f);
+    if (tid == 0) A.found[at] = make_float2(kInf, 0.f);
+    return;
+  }
+  const float floor_lo = m - reach;
+  // body(first key + 4 * lane, was it written) for the chunks whose word is `wanted`, twice 256 keys each
+  auto each_chunk = [&](auto wanted, auto body) {
+    int turn = 0;
+    for (int c0 = 0; c0 < nchunks; c0 += 64) {
+      const uint32_t word = c0 == 0 ? first_words : (c0 + lane < nchunks ? cmax[c0 + lane] : kCmaxNone);
+      unsigned long long hot = __ballot(c0 + lane < nchunks && wanted(word));
+      while (hot != 0ull) {
+        const int k = __builtin_ctzll(hot);
+        hot &= hot - 1ull;
+        if ((turn++ % kW) != wave) continue;
+        const uint32_t written = (uint32_t)__builtin_amdgcn_readlane((int)word, k);
+#pragma unroll
+        for (int u = 0; u < kDecodeChunk / 256; ++u) {
+          const int in_chunk = (u * 64 + lane) * 4;
+          body((c0 + k) * kDecodeChunk + in_chunk, ((written >> (in_chunk >> 5)) & 1u) != 0u);
+        }
+      }
+    }
+  };
+  float top = -kInf;  // the largest score itself
+  each_chunk([&](uint32_t word) { return (word & 0xffffu) != 0u && cmax_ceil(word) >= floor_lo; },
+             [&](int j, bool written) {
+               // (what was written is masked where the row does not see it, and whole blocks)
+               f32x4_t x = {-kInf, -kInf, -kInf, -kInf};
+               if (written) x = *reinterpret_cast<const f32x4_t*>(d + j);
+#pragma unroll
+               for (int k = 0; k < 4; ++k) {
+                 const bool in = x[k] >= floor_lo && x[k] > -kInf;
+                 top = fmaxf(top, x[k]);
+                 const unsigned long long all = __ballot(in);
+                 if (all == 0ull) continue;
+                 int pos = 0;
+                 if (lane == 0) pos = atomicAdd(&count, (int)__popcll(all));
+                 pos = __builtin_amdgcn_readfirstlane(pos) +
+                       (int)__builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u));
+                 if (in && pos < kSolveList) list[pos] = make_float2(__int_as_float(j + k), x[k]);
+               }
+             });
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+  if (lane == 0) wtop[wave] = top;
+  __syncthreads();
+  const int total = count;
+#pragma unroll
+  for (int w = 0; w < kW; ++w) top = fmaxf(top, wtop[w]);
+  // y = a (d - top) in [-1, 0]: the threshold lies between -1 and -n^(1-alpha)
+  float lo = -1.0f, hi = -__builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)lim)), tau = lo;
+  auto y_of = [&](float x) { return x > -kInf ? a * (x - top) : -kInf; };
+  // features of this lane of the value row of key j, times p
+  auto add_row = [&](int j, float p, float (&acc)[E]) {
+    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(vals.row(j) + (lane % LR) * 16);
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = fmaf(p, word_elem<T>(w, e), acc[e]);
+  };
+  float acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+
+  // The candidates come in the order in which the waves found them; the sums go in the order of the keys.
+  auto rank_of = [&](int key) {
+    int rank = 0;
+    for (int k = 0; k < total; ++k) rank += __float_as_int(list[k].x) < key ? 1 : 0;
+    return rank;
+  };
+  if (total <= 64) {  // one wave's, in registers
+    if (wave != 0) return;
+    float2 en = make_float2(0.f, 0.f);
+    if (lane < total) en = list[lane];
+    const int rank = rank_of(__float_as_int(en.x));
+    __builtin_amdgcn_wave_barrier();
+    if (lane < total) list[rank] = en;
+    __builtin_amdgcn_wave_barrier();
+    if (lane < total) en = list[lane];
+    const float y = lane < total ? y_of(en.y) : -kInf;
+    bool done = false;
+    for (int it = 0; !done && it < kMaxSolveIters; ++it) {
+      RowSums sums;
+      sums.clear();
+      accumulate<AM>(sums, y - tau, r);
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1) {
+        sums.s0 += __shfl_xor(sums.s0, off);
+        sums.s1 += __shfl_xor(sums.s1, off);
+        sums.s2 += __shfl_xor(sums.s2, off);
+        sums.xmin = fminf(sums.xmin, __shfl_xor(sums.xmin, off));
+      }
+      done = solve_step<AM>(sums, r, tau, lo, hi);
+    }
+    const float p = lane < total ? pow_r<AM>(fmaxf(y - tau, 0.f), r) : 0.f;
+    unsigned long long sup = __ballot(p > 0.f);
+    const int grp = lane / LR;
+    constexpr int WG = 64 / LR;  // value rows of the wave at a time
+    while (sup != 0ull) {
+      int mine = -1;
+#pragma unroll
+      for (int u = 0; u < WG; ++u) {
+        const int k = sup != 0ull ? __builtin_ctzll(sup) : -1;
+        sup &= sup - 1ull;  // (0 stays 0)
+        if (u == grp) mine = k;
+      }
+      const float pk = __shfl(p, max(mine, 0));
+      const int j = __shfl(__float_as_int(en.x), max(mine, 0));
+      if (mine >= 0) add_row(j, pk, acc);
+    }
+#pragma unroll
+    for (int off = LR; off < 64; off <<= 1)
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += __shfl_xor(acc[e], off);
+    if (lane < LR) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4) store4<T>(o + lane * E + e, acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+    }
+    if (lane == 0) A.found[at] = make_float2(kInf, 0.f);
+    return;
+  }
+  // tau from n values y_at(e)
+  auto solve = [&](auto y_at, int n) {
+    bool done = false;
+    for (int it = 0; !done && it < kMaxSolveIters; ++it) {
+      RowSums sums;
+      sums.clear();
+      for (int e = tid; e < n; e += NT) accumulate<AM>(sums, y_at(e) - tau, r);
+      sums = block_sums<NT>(sums, red, it & 1);
+      done = solve_step<AM>(sums, r, tau, lo, hi);
+    }
+  };
+  if (total <= kSolveList) {
+    static_assert(kSolveList <= NT, "a thread per candidate");
+    float2 en = make_float2(0.f, 0.f);
+    int rank = 0;
+    if (tid < total) {
+      en = list[tid];
+      rank = rank_of(__float_as_int(en.x));
+    }
+    __syncthreads();
+    if (tid < total) list[rank] = make_float2(en.x, y_of(en.y));
+    __syncthreads();
+    solve([&](int e) { return list[e].y; }, total);
+    for (int e = tid / LR; e < total; e += kGroups) {
+      const float x = list[e].y - tau;
+      if (x > 0.f) add_row(__float_as_int(list[e].x), pow_r<AM>(x, r), acc);
+    }
+    // lanes of equal features: within the wave, then over the waves in their order
+#pragma unroll
+    for (int off = LR; off < 64; off <<= 1)
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += __shfl_xor(acc[e], off);
+    if (lane < LR) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) osum[wave * D + lane * E + e] = acc[e];
+    }
+    __syncthreads();
+    if (tid < D) {
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) sum += osum[w * D + tid];
+      Elem<T>::store(o, tid, sum);
+    }
+    if (tid == 0) A.found[at] = make_float2(kInf, 0.f);
+    return;
+  }
+  // long supports: the row itself is read again and again, the blocks that were not written become -inf once and for all
+  each_chunk([&](uint32_t word) { return (word & 0xffffu) != 0xffffu; },
+             [&](int j, bool written) {
+               if (j < ((v.L + 31) & ~31) && !written) *reinterpret_cast<f32x4_t*>(d + j) = f32x4_t{-kInf, -kInf, -kInf, -kInf};
+             });
+  __syncthreads();
+  {
+    // starting point from the row's mean and deviation (gauss_start())
+    RowSums st;
+    st.clear();
+    for (int e = tid; e < lim; e += NT) {
+      const float x = y_of(d[e]);
+      if (x > -kInf) {
+        st.s0 += 1.f;
+        st.s1 += x;
+        st.s2 = fmaf(x, x, st.s2);
+      }
+    }
+    st = block_sums<NT>(st, red, 1);
+    const float mean = st.s1 / st.s0, var = st.s2 / st.s0 - mean * mean;
+    float t0;
+    if (st.s0 == (float)lim && var > 0.f && gauss_start<AM>(mean, sqrtf(var), st.s0, t0)) tau = fminf(fmaxf(t0, lo), hi);
+  }
+  solve([&](int e) { return y_of(d[e]); }, lim);
+  if (tid == 0) A.found[at] = make_float2(tau, top);
+}
+
+// Keys of a wave's tile and bytes of LDS for it: two tiles of V per wave
+template <typename T, int D>
+struct SeqPvCfg {
+  static constexpr int KT = 32;
+  static constexpr int kTileBytes = KT * D * (int)sizeof(T);
+};
+
+// O^T = V^T P^T for the rows that seq_solve_kernel left (tau finite).  Every wave goes through its own 32-key blocks of the workgroup's
+// piece of the keys; the waves' sums are added in their order, and the workgroup that comes last adds up the pieces in theirs.
+template <typename T, int D, int AM, int NQB>
+__global__ __launch_bounds__(kThreads) void seq_pv_kernel(SeqDecodeArgs A) {
+  constexpr int NM = D / 32, KT = 32;
+  using Vals = SeqValues<T, D, KT>;
+  __shared__ __attribute__((aligned(16))) char tiles[kWaves * SeqPvCfg<T, D>::kTileBytes];
+  __shared__ int last;
+  const SeqGeom& g = A.g;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, hh = lane >> 5;
+  const int split = blockIdx.x % A.pv_splits, s = blockIdx.x / A.pv_splits, hk = blockIdx.y;
+  const int head = s * g.Hkv + hk;
+  SeqView v;
+  if (!load_seq(g, s, v) || !split_seq(g, v)) return;
+  const int from = split * A.pv_keys;
+  if (from >= v.L) return;
+  const int R = v.n * g.G;
+  float tau[NQB], top[NQB], a[NQB];
+  bool left[NQB];
+  bool any = false;
+#pragma unroll
+  for (int qb = 0; qb < NQB; ++qb) {
+    const int row = qb * 32 + li;
+    const long long at = (long long)head * A.rows + row;
+    const float2 f = row < R ? A.found[at] : make_float2(kInf, 0.f);
+    a[qb] = row < R ? A.mult[at] : 0.f;
+    tau[qb] = f.x;
+    top[qb] = f.y;
+    left[qb] = tau[qb] < kInf;
+    any = any || left[qb];
+  }
+  if (__ballot(any) == 0ull) return;  // (the same for all waves)
+  const int to = min(v.L, from + A.pv_keys), nblk = (to - from + 31) >> 5;
+  const float r = 1.0f / (g.alpha - 1.0f);
+  SeqKeys vals;
+  vals.init(g, v, A.V, hk, true, sizeof(T));
+  // keys from this one on are not seen by every row; with holes, none is (SeqValues::accumulate())
+  int all_see = g.causal ? max(0, v.L - v.n + 1) : v.L;
+  {
+    int bad = 0;
+    for (int e = (from >> g.lps) + tid; e << g.lps < to; e += kThreads) bad |= vals.is_hole(vals.page(e << g.lps)) ? 1 : 0;
+    if (__syncthreads_or(bad)) all_see = 0;
+  }
+  char* tile = tiles + wave * SeqPvCfg<T, D>::kTileBytes;
+  Vals vv;
+  vv.init(lane);
+  f32x16_t oacc[NQB][NM];
+#pragma unroll
+  for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+    for (int mm = 0; mm < NM; ++mm)
+      oacc[qb][mm] = f32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  // the wave's tile: 64 lanes bring 1024 bytes at a time
+  using VT = typename Vals::VT;
+  constexpr int CPR = VT::kCpr, RW = VT::RW, L = KT / RW;
+  u32x4_t stage[L];
+  f32x4_t ys[NQB][4];
+  auto fetch = [&](int blk) {
+    const int j0 = from + blk * 32;
+#pragma unroll
+    for (int it = 0; it < L; ++it)
+      stage[it] = *reinterpret_cast<const u32x4_t*>(vals.row(min(j0 + it * RW + lane / CPR, v.L - 1)) + (lane % CPR) * 16);
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      if (qb * 32 >= R) break;
+      const float* y = A.scores + ((long long)head * A.rows + min(qb * 32 + li, R - 1)) * A.nks + j0 + 4 * hh;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) ys[qb][k] = *reinterpret_cast<const f32x4_t*>(y + 8 * k);
+    }
+  };
+  if (wave < nblk) fetch(wave);
+  for (int blk = wave; blk < nblk; blk += kWaves) {
+    __builtin_amdgcn_wave_barrier();  // (the tile is the wave's own: LDS operations of a wave are in order)
+#pragma unroll
+    for (int it = 0; it < L; ++it) {
+      const int row = it * RW + lane / CPR;
+      *reinterpret_cast<u32x4_t*>(tile + VT::off(row, lane % CPR)) = stage[it];
+    }
+    float p[NQB][16];
+    const int j0 = from + blk * 32;
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      if (qb * 32 >= R) break;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = fmaf(a[qb], ys[qb][e >> 2][e & 3] - top[qb], -tau[qb]);
+        p[qb][e] = left[qb] && ys[qb][e >> 2][e & 3] > -kInf ? pow_r<AM>(fmaxf(x, 0.f), r) : 0.f;
+      }
+    }
+    if (blk + kWaves < nblk) fetch(blk + kWaves);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb) {
+      if (qb * 32 >= R) break;
+      bool some = false;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) some = some || p[qb][e] > 0.f;
+      if (__ballot(some) != 0ull) vv.accumulate(tile, 0, p[qb], j0 + 32 > all_see, oacc[qb]);
+    }
+  }
+  // the waves' sums in LDS, 32 rows and one 32-feature block at a time: [wave][16][64]
+  float* red = reinterpret_cast<float*>(tiles);
+  static_assert(SeqPvCfg<T, D>::kTileBytes >= 16 * 64 * 4, "a wave's accumulators fit its tile");
+  float* part = A.part + ((long long)head * A.pv_splits + split) * A.rows * D;
+#pragma unroll
+  for (int qb = 0; qb < NQB; ++qb) {
+    if (qb * 32 >= R) break;
+#pragma unroll
+    for (int mm = 0; mm < NM; ++mm) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) red[(wave * 16 + e) * 64 + lane] = oacc[qb][mm][e];
+      __syncthreads();
+      // thread: row tid % 32 (of half tid / 32 % 2), accumulators 4 (tid / 64) .. + 3
+      f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += red[(w * 16 + 4 * wave + e) * 64 + lane];
+      const int row = qb * 32 + li;
+      if (row < R) *reinterpret_cast<f32x4_t*>(part + (long long)row * D + 32 * mm + 8 * wave + 4 * hh) = sum;
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  const int parts = (v.L + A.pv_keys - 1) / A.pv_keys;
+  if (tid == 0) last = atomicAdd(&A.arrived[head], 1) == parts - 1 ? 1 : 0;
+  __syncthreads();
+  if (last == 0) return;
+  __threadfence();
+  const float* all = A.part + (long long)head * A.pv_splits * A.rows * D;
+  for (int e = tid; e < R * (D / 4); e += kThreads) {
+    const int row = e / (D / 4), f = (e % (D / 4)) * 4;
+    if (!(A.found[(long long)head * A.rows + row].x < kInf)) continue;
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < parts; ++k) {
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(all + ((long long)k * A.rows + row) * D + f);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) sum[u] += x[u];
+    }
+    T* o = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + row / g.G) * g.o_st + (long long)(hk * g.G + row % g.G) * g.o_sh + f;
+    store4<T>(o, sum[0], sum[1], sum[2], sum[3]);
+  }
+}
+
+}  // namespace entmax

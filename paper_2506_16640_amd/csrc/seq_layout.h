@@ -66,6 +66,10 @@ inline int check_seq_params(const entmax_seq_params* p) {
   if (p->k_stride_n < p->D || p->v_stride_n < p->D) return ENTMAX_ATTN_INVALID_ARG;  // rows overlap
   if (p->o_stride_t < p->D || (p->Hq > 1 && p->o_stride_h < p->D)) return ENTMAX_ATTN_INVALID_ARG;
   if (seq_blocks(p->nseq, p->T, p->Hq / p->Hkv) * p->Hkv > kSeqMostBlocks) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  // (launches of the kernels that split the keys: workgroups of the value kernel, of one piece of the keys each; workgroups of rows)
+  if (!packed && ((long long)p->nseq * p->Hkv * (ceil_div(p->max_keys, kDecodeChunk) + 1) > kSeqMostBlocks ||
+                  (long long)p->nseq * p->Hkv * 64 > kSeqMostBlocks / 2))
+    return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
   return ENTMAX_ATTN_OK;
 }
 
@@ -90,9 +94,54 @@ inline int check_append_params(const entmax_append_params* p) {
   return ENTMAX_ATTN_OK;
 }
 
+// Paged sequences with at most this many folded rows (new tokens x heads of a group) go to the kernels that split the keys.
+constexpr int kSplitRows = 64;
+
+struct SeqLayout {
+  bool split;       // the call may hold such sequences
+  bool blocks;      // it may hold others
+  int rows;         // rows of a head in the score buffer
+  int nks, nchunks; // scores and chunks of a row
+  int chunks_per_wg, splits;  // of the score kernel
+  int pv_keys, pv_splits;     // of the value kernel
+  size_t off_cmax, off_mult, off_found, off_arrived, off_part, total;
+};
+
+inline SeqLayout make_seq_layout(const entmax_seq_params* p) {
+  SeqLayout L{};
+  const int G = p->Hq / p->Hkv;
+  const long long most_rows = (long long)p->max_new * G;
+  L.split = p->page_size != 0 && p->max_keys > 0 && G <= kSplitRows;
+  L.blocks = !L.split || most_rows > kSplitRows;
+  size_t o = 0;
+  if (L.split) {
+    const long long heads = (long long)p->nseq * p->Hkv;
+    L.rows = (int)(most_rows < kSplitRows ? most_rows : kSplitRows);
+    L.nks = ceil_div(p->max_keys, 32) * 32;
+    L.nchunks = ceil_div(p->max_keys, kDecodeChunk);
+    L.chunks_per_wg = decode_chunks_per_wg(heads, L.nchunks);
+    L.splits = ceil_div(L.nchunks, L.chunks_per_wg);
+    L.pv_keys = 1024;
+    L.pv_splits = ceil_div(p->max_keys, L.pv_keys);
+    const size_t rows = (size_t)heads * L.rows;
+    o += align_up(rows * L.nks * sizeof(float));
+    L.off_cmax = o;
+    o += align_up(rows * L.nchunks * sizeof(uint32_t));
+    L.off_mult = o;
+    o += align_up(rows * sizeof(float));
+    L.off_found = o;
+    o += align_up(rows * 2 * sizeof(float));
+    L.off_arrived = o;
+    o += align_up((size_t)heads * sizeof(int));
+    L.off_part = o;
+    o += align_up(rows * L.pv_splits * p->D * sizeof(float));
+  }
+  L.total = o < kAlign ? kAlign : o;
+  return L;
+}
+
 inline size_t seq_workspace_bytes_of(const entmax_seq_params* p) {
-  if (check_seq_params(p) != ENTMAX_ATTN_OK) return 0;
-  return kAlign;
+  return check_seq_params(p) == ENTMAX_ATTN_OK ? make_seq_layout(p).total : 0;
 }
 
 }  // namespace entmax

@@ -1,6 +1,7 @@
 // Launches of the serving attention for one (element type, head dimension); see seq_attn.hip.
 #pragma once
 #include "launch.hip.h"
+#include "seq_decode.hip.h"
 #include "seq_layout.h"
 #include "seq_tiled.hip.h"
 
@@ -62,11 +63,35 @@ bool launch_seq_tiled(const SeqArgs& a, hipStream_t st) {
   return launch_ok();
 }
 
+template <typename T, int D, int AM>
+bool launch_seq_split(const SeqDecodeArgs& a, hipStream_t st) {
+  const dim3 scores((unsigned)(a.g.nseq * a.splits), (unsigned)a.g.Hkv), pv((unsigned)(a.g.nseq * a.pv_splits), (unsigned)a.g.Hkv);
+  if (a.rows <= 32)
+    hipLaunchKernelGGL((seq_scores_kernel<T, D, 1>), scores, dim3(kThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((seq_scores_kernel<T, D, 2>), scores, dim3(kThreads), 0, st, a);
+  if (!launch_ok()) return false;
+  hipLaunchKernelGGL((seq_solve_kernel<T, D, AM>), dim3((unsigned)(a.g.nseq * a.g.Hkv * a.rows)), dim3(kSolveThreads), 0, st, a);
+  if (!launch_ok()) return false;
+  if (a.rows <= 32)
+    hipLaunchKernelGGL((seq_pv_kernel<T, D, AM, 1>), pv, dim3(kThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((seq_pv_kernel<T, D, AM, 2>), pv, dim3(kThreads), 0, st, a);
+  return launch_ok();
+}
+
+template <typename T, int D, int AM>
+bool launch_seq(const SeqArgs& a, const SeqDecodeArgs& d, const SeqLayout& L, hipStream_t st) {
+  if (L.blocks && !launch_seq_tiled<T, D, AM>(a, st)) return false;
+  return !a.split || launch_seq_split<T, D, AM>(d, st);
+}
+
 }  // namespace
 
 template <typename T, int D>
 int run_seq(const SeqCall& c) {
   const entmax_seq_params* p = c.p;
+  SeqLayout L = make_seq_layout(p);
   SeqArgs a;
   a.g = make_seq_geom(c);
   a.Q = c.Q;
@@ -75,12 +100,33 @@ int run_seq(const SeqCall& c) {
   a.O = c.O;
   a.nblk = (int)seq_blocks(p->nseq, p->T, a.g.G);
   a.mask_words = (p->max_keys + 1023) / 1024 + 1;
+  a.split = L.split && p->path == 0 ? 1 : 0;
+  if (!a.split) L.blocks = true;
+  SeqDecodeArgs d;
+  d.g = a.g;
+  d.Q = c.Q;
+  d.K = c.K;
+  d.V = c.V;
+  d.O = c.O;
+  d.scores = reinterpret_cast<float*>(c.ws);
+  d.cmax = reinterpret_cast<uint32_t*>(c.ws + L.off_cmax);
+  d.mult = reinterpret_cast<float*>(c.ws + L.off_mult);
+  d.found = reinterpret_cast<float2*>(c.ws + L.off_found);
+  d.arrived = reinterpret_cast<int*>(c.ws + L.off_arrived);
+  d.part = reinterpret_cast<float*>(c.ws + L.off_part);
+  d.rows = L.rows;
+  d.nks = L.nks;
+  d.nchunks = L.nchunks;
+  d.chunks_per_wg = L.chunks_per_wg;
+  d.splits = L.splits;
+  d.pv_keys = L.pv_keys;
+  d.pv_splits = L.pv_splits;
   bool ok = false;
   switch (alpha_mode(p->alpha)) {
-    case 1: ok = launch_seq_tiled<T, D, 1>(a, c.st); break;
-    case 2: ok = launch_seq_tiled<T, D, 2>(a, c.st); break;
-    case 3: ok = launch_seq_tiled<T, D, 3>(a, c.st); break;
-    default: ok = launch_seq_tiled<T, D, 0>(a, c.st); break;
+    case 1: ok = launch_seq<T, D, 1>(a, d, L, c.st); break;
+    case 2: ok = launch_seq<T, D, 2>(a, d, L, c.st); break;
+    case 3: ok = launch_seq<T, D, 3>(a, d, L, c.st); break;
+    default: ok = launch_seq<T, D, 0>(a, d, L, c.st); break;
   }
   return ok ? ENTMAX_ATTN_OK : ENTMAX_ATTN_LAUNCH_FAILED;
 }

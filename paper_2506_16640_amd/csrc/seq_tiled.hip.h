@@ -9,6 +9,7 @@
 #pragma once
 #include "fwd.hip.h"
 #include "seq.hip.h"
+#include "seq_layout.h"
 
 namespace entmax {
 
@@ -20,18 +21,23 @@ struct SeqArgs {
   void* O;
   int nblk;        // 128-row groups per key/value head (seq_blocks())
   int mask_words;  // uint32 words that hold a bit per 32-key block
+  int split;       // sequences with few rows are left to the kernels that split the keys
 };
+
+// Whether the kernels that split the keys take a sequence (else those for 128 rows at a time do)
+__device__ __forceinline__ bool split_seq(const SeqGeom& g, const SeqView& v) { return (long long)v.n * g.G <= kSplitRows; }
+
 
 // The 128-row group of this workgroup: sequence, key/value head, first row; false: nothing to do.  The head runs fastest, so that a
 // head's groups meet on one XCD where the heads divide among the eight of them; groups run from the last to the first, a sequence's long rows first.
-__device__ __forceinline__ bool seq_block(const SeqGeom& g, int nblk, SeqView& v, int& hk, int& r0) {
+__device__ __forceinline__ bool seq_block(const SeqGeom& g, int nblk, bool split, SeqView& v, int& hk, int& r0) {
   hk = __builtin_amdgcn_readfirstlane(blockIdx.x % g.Hkv);
   const int blk = nblk - 1 - __builtin_amdgcn_readfirstlane(blockIdx.x / g.Hkv);
   // sequence s has the groups from cu[s] G / 128 + s on
   const int G = g.G;
   auto first = [G](int c, int s) { return (long long)c * G / kBlockRows + s; };
   const int s = find_seq(g.cu, g.nseq, blk, first);
-  if (s >= g.nseq || !load_seq(g, s, v)) return false;
+  if (s >= g.nseq || !load_seq(g, s, v) || (split && split_seq(g, v))) return false;
   const long long local = blk - first(v.row0, s);
   if (local < 0 || local * kBlockRows >= (long long)v.n * G) return false;
   r0 = (int)local * kBlockRows;
@@ -176,7 +182,7 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   SeqView v;
   int hk, blk0;
-  if (!seq_block(g, A.nblk, v, hk, blk0)) return;  // (the same for the whole workgroup)
+  if (!seq_block(g, A.nblk, A.split != 0, v, hk, blk0)) return;  // (the same for the whole workgroup)
   SeqKeys keys, vals;
   keys.init(g, v, A.K, hk, false, sizeof(T));
   vals.init(g, v, A.V, hk, true, sizeof(T));
