@@ -75,14 +75,18 @@ struct SeqKeys {
     const long long sn_e = values ? g.v_sn : g.k_sn, sh_e = values ? g.v_sh : g.k_sh, sp_e = values ? g.v_sp : g.k_sp;
     sn = sn_e * esize;
     paged = g.table != nullptr;
-    pages = (Pages)(g.table + (paged ? (long long)v.s * g.max_pages : 0));
+    pages = (Pages)(paged ? g.table + (long long)v.s * g.max_pages : g.cu);
     sp = paged ? sp_e * esize : sn << g.lps;
     base = reinterpret_cast<const char*>(X) + hk * sh_e * esize + (paged ? 0 : (long long)v.row0 * sn);
     lps = g.lps;
     num_pages = g.num_pages;
   }
   // page of key j (0 <= j < L); a hole: not in 0 .. num_pages - 1
-  __device__ __forceinline__ int page(int j) const { return paged ? pages[j >> lps] : j >> lps; }
+  // (read in either case, packed from a place that is always there: no branch that the loads would wait for one by one)
+  __device__ __forceinline__ int page(int j) const {
+    const int x = j >> lps, y = pages[paged ? x : 0];
+    return paged ? y : x;
+  }
   __device__ __forceinline__ bool is_hole(int pg) const { return paged && (unsigned)pg >= (unsigned)num_pages; }
   // (a hole's keys are masked wherever they are used; they are read from page 0)
   __device__ __forceinline__ const char* row_in(int pg, int j) const {
@@ -141,34 +145,18 @@ struct SeqTile {
   }
 };
 
-// sign and size of a row's scale and distance bias, see bias_w() in common.hip.h
-template <typename T, int D>
-struct SeqRows {
-  static constexpr int NC = D / 16;
-  int lane, li, hh;
+// What belongs to a folded row.
+struct SeqRow {
   int t, head;          // token of the sequence, query head
   bool valid;
   int lim, pos;         // keys j < lim are visible; the row's position
-  int lim_min, lim_max; // over the wave's rows
   float a, c, w;        // as in QCtx: y_ij = a d_ij, d_ij = +-<q_i, k_j> + w max(pos - j, 0)
-  bool biased;          // some row of the wave has w != 0
-  Frag<T> qf[NC];
-
-  // rows r0 .. r0 + 31 of key/value head hk
-  __device__ __forceinline__ void init(const SeqGeom& g, const SeqView& v, const void* Q, int hk, int r0) {
-    lane = threadIdx.x & 63;
-    li = lane & 31;
-    hh = lane >> 5;
-    const int r = r0 + li;
+  __device__ __forceinline__ void init(const SeqGeom& g, const SeqView& v, int hk, int r, int D) {
     valid = r < v.n * g.G;
     t = valid ? r / g.G : 0;
     head = hk * g.G + (valid ? r - t * g.G : 0);
     pos = v.L - v.n + t;
     lim = !valid ? 0 : (g.causal ? max(0, min(pos + 1, v.L)) : v.L);
-    // (limits do not decrease from row to row)
-    lim_min = __builtin_amdgcn_readfirstlane(lim);
-    const int last = min(v.n * g.G - 1 - r0, 31);
-    lim_max = last < 0 ? 0 : __builtin_amdgcn_readlane(lim, last);
     float scale = g.delta;
     if (g.scale_layout != 0) {
       const long long idx = g.scale_layout == 1 ? head : (long long)head * g.T + v.row0 + t;
@@ -178,11 +166,45 @@ struct SeqRows {
     if (!valid) scale = 0.f;
     c = scale * (1.0f / sqrtf((float)D));
     a = (g.alpha - 1.0f) * fabsf(c);
-    w = 0.f;
+    w = 0.f;  // (see bias_w() in common.hip.h)
     if (g.slopes) {
       const float m = valid ? g.slopes[head] : 0.f;
       if (m != 0.f && a != 0.f) w = g.bias_mode == 0 ? (c < 0.f ? m : -m) * sqrtf((float)D) : -(g.alpha - 1.0f) * m / a;
     }
+  }
+  __device__ __forceinline__ SeqRow of_lane(int l) const {
+    SeqRow x;
+    x.t = __shfl(t, l);
+    x.head = __shfl(head, l);
+    x.valid = __shfl(valid ? 1 : 0, l) != 0;
+    x.lim = __shfl(lim, l);
+    x.pos = __shfl(pos, l);
+    x.a = __shfl(a, l);
+    x.c = __shfl(c, l);
+    x.w = __shfl(w, l);
+    return x;
+  }
+};
+
+// A wave's 32 rows, one to a lane pair, with the query fragments.
+template <typename T, int D>
+struct SeqRows : SeqRow {
+  static constexpr int NC = D / 16;
+  int lane, li, hh;
+  int lim_min, lim_max; // over the wave's rows
+  bool biased;          // some row of the wave has w != 0
+  Frag<T> qf[NC];
+
+  // rows r0 .. r0 + 31 of key/value head hk
+  __device__ __forceinline__ void init(const SeqGeom& g, const SeqView& v, const void* Q, int hk, int r0) {
+    lane = threadIdx.x & 63;
+    li = lane & 31;
+    hh = lane >> 5;
+    SeqRow::init(g, v, hk, r0 + li, D);
+    // (limits do not decrease from row to row)
+    lim_min = __builtin_amdgcn_readfirstlane(lim);
+    const int last = min(v.n * g.G - 1 - r0, 31);
+    lim_max = last < 0 ? 0 : __builtin_amdgcn_readlane(lim, last);
     biased = __ballot(w != 0.f) != 0ull;
     const T* q = reinterpret_cast<const T*>(Q) + (long long)(v.row0 + t) * g.q_st + (long long)head * g.q_sh;
 #pragma unroll

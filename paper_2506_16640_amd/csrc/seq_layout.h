@@ -65,7 +65,7 @@ inline int check_seq_params(const entmax_seq_params* p) {
   if (p->k_stride_n * es > (1 << 24) || p->v_stride_n * es > (1 << 24)) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
   if (p->k_stride_n < p->D || p->v_stride_n < p->D) return ENTMAX_ATTN_INVALID_ARG;  // rows overlap
   if (p->o_stride_t < p->D || (p->Hq > 1 && p->o_stride_h < p->D)) return ENTMAX_ATTN_INVALID_ARG;
-  if (seq_blocks(p->nseq, p->T, p->Hq / p->Hkv) * p->Hkv > kSeqMostBlocks) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  if (seq_blocks(p->nseq, p->T, p->Hq / p->Hkv) * p->Hkv * 4 > kSeqMostBlocks) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
   // (launches of the kernels that split the keys: workgroups of the value kernel, of one piece of the keys each; workgroups of rows)
   if (!packed && ((long long)p->nseq * p->Hkv * (ceil_div(p->max_keys, kDecodeChunk) + 1) > kSeqMostBlocks ||
                   (long long)p->nseq * p->Hkv * 64 > kSeqMostBlocks / 2))
@@ -97,13 +97,25 @@ inline int check_append_params(const entmax_append_params* p) {
 // Paged sequences with at most this many folded rows (new tokens x heads of a group) go to the kernels that split the keys.
 constexpr int kSplitRows = 64;
 
+constexpr int kSeqTopWords = 14;  // words that a lane of the sweep leaves
+// Workgroups that share the keys of a group of 128 rows in the sweep of the list kernels
+inline int seq_ksplit(long long groups, int max_keys) {
+  (void)groups;
+  (void)max_keys;
+  return 1;
+}
+
 struct SeqLayout {
   bool split;       // the call may hold such sequences
   bool blocks;      // it may hold others
+  size_t off_scores;
   int rows;         // rows of a head in the score buffer
   int nks, nchunks; // scores and chunks of a row
   int chunks_per_wg, splits;  // of the score kernel
   int pv_keys, pv_splits;     // of the value kernel
+  bool lists;       // groups of 128 rows go through the list kernels first
+  int ksplit;       // workgroups that share the keys of a group in their sweep
+  size_t off_blocks, off_votes, off_dense, off_tops;
   size_t off_cmax, off_mult, off_found, off_arrived, off_part, total;
 };
 
@@ -114,7 +126,21 @@ inline SeqLayout make_seq_layout(const entmax_seq_params* p) {
   L.split = p->page_size != 0 && p->max_keys > 0 && G <= kSplitRows;
   L.blocks = !L.split || most_rows > kSplitRows;
   size_t o = 0;
+  L.lists = p->dtype == ENTMAX_ATTN_BF16 && L.blocks;
+  if (L.lists) {
+    const long long groups = seq_blocks(p->nseq, p->T, G) * p->Hkv;
+    L.ksplit = seq_ksplit(groups, p->max_keys);
+    L.off_blocks = o;
+    o += align_up((size_t)groups * 2 * sizeof(int));
+    L.off_votes = o;
+    o += align_up((size_t)groups * L.ksplit * sizeof(int));
+    L.off_dense = o;
+    o += align_up((size_t)groups * sizeof(int));
+    L.off_tops = o;
+    o += align_up((size_t)groups * L.ksplit * kWaves * kSeqTopWords * 64 * sizeof(float));
+  }
   if (L.split) {
+    L.off_scores = o;
     const long long heads = (long long)p->nseq * p->Hkv;
     L.rows = (int)(most_rows < kSplitRows ? most_rows : kSplitRows);
     L.nks = ceil_div(p->max_keys, 32) * 32;

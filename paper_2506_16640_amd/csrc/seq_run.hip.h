@@ -3,6 +3,7 @@
 #include "launch.hip.h"
 #include "seq_decode.hip.h"
 #include "seq_layout.h"
+#include "seq_lists.hip.h"
 #include "seq_tiled.hip.h"
 
 namespace entmax {
@@ -80,8 +81,29 @@ bool launch_seq_split(const SeqDecodeArgs& a, hipStream_t st) {
   return launch_ok();
 }
 
+template <int D, int AM>
+bool launch_seq_lists(const SeqListArgs& a, hipStream_t st) {
+  const unsigned groups = (unsigned)(a.a.nblk * a.a.g.Hkv);
+  constexpr auto sweep = seq_sweep_kernel<D>;
+  if (!ensure_dynamic_lds<sweep>(SeqSweepCfg<D>::kLdsBytes)) return false;
+  hipLaunchKernelGGL(sweep, dim3(groups * (unsigned)a.ksplit), dim3(kThreads), SeqSweepCfg<D>::kLdsBytes, st, a);
+  if (!launch_ok()) return false;
+  if (a.ksplit == 1)
+    hipLaunchKernelGGL((seq_finish_kernel<D, AM, 1>), dim3(4 * groups), dim3(kThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((seq_finish_kernel<D, AM, 4>), dim3(4 * groups), dim3(kThreads), 0, st, a);
+  return launch_ok();
+}
+
 template <typename T, int D, int AM>
-bool launch_seq(const SeqArgs& a, const SeqDecodeArgs& d, const SeqLayout& L, hipStream_t st) {
+bool launch_seq(const SeqArgs& a_in, const SeqListArgs& l, const SeqDecodeArgs& d, const SeqLayout& L, hipStream_t st) {
+  SeqArgs a = a_in;
+  if constexpr (sizeof(T) == 2) {
+    if (l.ksplit > 0) {
+      if (!launch_seq_lists<D, AM>(l, st)) return false;
+      a.dense = l.dense;
+    }
+  }
   if (L.blocks && !launch_seq_tiled<T, D, AM>(a, st)) return false;
   return !a.split || launch_seq_split<T, D, AM>(d, st);
 }
@@ -102,13 +124,21 @@ int run_seq(const SeqCall& c) {
   a.mask_words = (p->max_keys + 1023) / 1024 + 1;
   a.split = L.split && p->path == 0 ? 1 : 0;
   if (!a.split) L.blocks = true;
+  a.dense = nullptr;
+  SeqListArgs l;
+  l.a = a;
+  l.blocks = reinterpret_cast<SeqBlock*>(c.ws + L.off_blocks);
+  l.votes = reinterpret_cast<int*>(c.ws + L.off_votes);
+  l.dense = reinterpret_cast<int*>(c.ws + L.off_dense);
+  l.tops = reinterpret_cast<float*>(c.ws + L.off_tops);
+  l.ksplit = L.lists && p->path == 0 ? L.ksplit : 0;
   SeqDecodeArgs d;
   d.g = a.g;
   d.Q = c.Q;
   d.K = c.K;
   d.V = c.V;
   d.O = c.O;
-  d.scores = reinterpret_cast<float*>(c.ws);
+  d.scores = reinterpret_cast<float*>(c.ws + L.off_scores);
   d.cmax = reinterpret_cast<uint32_t*>(c.ws + L.off_cmax);
   d.mult = reinterpret_cast<float*>(c.ws + L.off_mult);
   d.found = reinterpret_cast<float2*>(c.ws + L.off_found);
@@ -123,10 +153,10 @@ int run_seq(const SeqCall& c) {
   d.pv_splits = L.pv_splits;
   bool ok = false;
   switch (alpha_mode(p->alpha)) {
-    case 1: ok = launch_seq<T, D, 1>(a, d, L, c.st); break;
-    case 2: ok = launch_seq<T, D, 2>(a, d, L, c.st); break;
-    case 3: ok = launch_seq<T, D, 3>(a, d, L, c.st); break;
-    default: ok = launch_seq<T, D, 0>(a, d, L, c.st); break;
+    case 1: ok = launch_seq<T, D, 1>(a, l, d, L, c.st); break;
+    case 2: ok = launch_seq<T, D, 2>(a, l, d, L, c.st); break;
+    case 3: ok = launch_seq<T, D, 3>(a, l, d, L, c.st); break;
+    default: ok = launch_seq<T, D, 0>(a, l, d, L, c.st); break;
   }
   return ok ? ENTMAX_ATTN_OK : ENTMAX_ATTN_LAUNCH_FAILED;
 }

@@ -21,6 +21,7 @@ struct SeqArgs {
   void* O;
   int nblk;        // 128-row groups per key/value head (seq_blocks())
   int mask_words;  // uint32 words that hold a bit per 32-key block
+  const int* dense;  // NULL, or [Hkv * nblk]: only the groups that are marked
   int split;       // sequences with few rows are left to the kernels that split the keys
 };
 
@@ -28,15 +29,13 @@ struct SeqArgs {
 __device__ __forceinline__ bool split_seq(const SeqGeom& g, const SeqView& v) { return (long long)v.n * g.G <= kSplitRows; }
 
 
-// The 128-row group of this workgroup: sequence, key/value head, first row; false: nothing to do.  The head runs fastest, so that a
-// head's groups meet on one XCD where the heads divide among the eight of them; groups run from the last to the first, a sequence's long rows first.
-__device__ __forceinline__ bool seq_block(const SeqGeom& g, int nblk, bool split, SeqView& v, int& hk, int& r0) {
-  hk = __builtin_amdgcn_readfirstlane(blockIdx.x % g.Hkv);
-  const int blk = nblk - 1 - __builtin_amdgcn_readfirstlane(blockIdx.x / g.Hkv);
+// Group blk of 128 rows: its sequence and its first folded row; false: nothing to do.
+__device__ __forceinline__ bool seq_block(const SeqGeom& g, int blk, bool split, SeqView& v, int& r0) {
   // sequence s has the groups from cu[s] G / 128 + s on
   const int G = g.G;
   auto first = [G](int c, int s) { return (long long)c * G / kBlockRows + s; };
   const int s = find_seq(g.cu, g.nseq, blk, first);
+  r0 = 0;
   if (s >= g.nseq || !load_seq(g, s, v) || (split && split_seq(g, v))) return false;
   const long long local = blk - first(v.row0, s);
   if (local < 0 || local * kBlockRows >= (long long)v.n * G) return false;
@@ -180,9 +179,13 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const SeqGeom& g = A.g;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  // The head runs fastest, so that a head's groups meet on one XCD where the heads divide among the eight of them; the groups run from the
+  // last to the first, a sequence's long rows first.
+  const int hk = blockIdx.x % g.Hkv, blk = A.nblk - 1 - (int)blockIdx.x / g.Hkv;
+  if (A.dense && A.dense[hk * A.nblk + blk] == 0) return;
   SeqView v;
-  int hk, blk0;
-  if (!seq_block(g, A.nblk, A.split != 0, v, hk, blk0)) return;  // (the same for the whole workgroup)
+  int blk0;
+  if (!seq_block(g, blk, A.split != 0, v, blk0)) return;  // (the same for the whole workgroup)
   SeqKeys keys, vals;
   keys.init(g, v, A.K, hk, false, sizeof(T));
   vals.init(g, v, A.V, hk, true, sizeof(T));
