@@ -106,14 +106,15 @@ __device__ __forceinline__ bool seq_has_holes(const SeqKeys& k, int L) {
 // One tile of KT rows to LDS without registers in between (load_to_lds()).  16-byte chunks, swizzled by row: SWZ false: as LdsTile, for
 // ds_read_b128 of 32 rows at a time (keys) and for reads along a row; true: for transposed reads (values of 2 bytes), where four
 // consecutive rows' 32-byte pieces are read together and pairs of chunks must stay together.
-template <typename T, int D, int KT, bool TR>
+// NT: threads of the workgroup.
+template <typename T, int D, int KT, bool TR, int NT = kThreads>
 struct SeqTile {
   using Tile = LdsTile<T, KT, D>;
   static constexpr int kCpr = Tile::kCpr, kBytes = Tile::kBytes, kRowBytes = Tile::kRowBytes;
-  static constexpr int L = Tile::kChunks / kThreads;  // loads of a wave
-  static constexpr int RS = kThreads / kCpr;          // rows of the tile per load of the four waves
+  static constexpr int L = Tile::kChunks / NT;  // loads of a wave
+  static constexpr int RS = NT / kCpr;          // rows of the tile per load of all waves
   static constexpr int RW = 64 / kCpr;                // rows of a wave's load: within one page (page sizes are multiples of 16)
-  static_assert(16 % RW == 0 && Tile::kChunks % kThreads == 0, "a load's rows lie in one page");
+  static_assert(16 % RW == 0 && Tile::kChunks % NT == 0, "a load's rows lie in one page");
   static __device__ __forceinline__ int swz(int row) {
     if (!TR) return Tile::swz(row);
     return kCpr == 8 ? 2 * ((row >> 1) & 3) : 2 * (row & 7);
@@ -134,7 +135,7 @@ struct SeqTile {
     for (int it = 0; it < L; ++it) {
       const int row = it * RS + wave * RW;  // first row of this wave's load
       const uint32_t chunk = (uint32_t)(((lane % kCpr) ^ swz(row + rl)) << 4);
-      const uint32_t dst = lds + (uint32_t)((it * kThreads + wave * 64) * 16);
+      const uint32_t dst = lds + (uint32_t)((it * NT + wave * 64) * 16);
       if (j0 + KT <= n) {
         load_to_lds(k.row_in(p.pg[it], j0 + row), (uint32_t)rl * (uint32_t)k.sn + chunk, dst);
       } else {

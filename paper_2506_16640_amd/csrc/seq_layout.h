@@ -115,7 +115,7 @@ struct SeqLayout {
   int pv_keys, pv_splits;     // of the value kernel
   bool lists;       // groups of 128 rows go through the list kernels first
   int ksplit;       // workgroups that share the keys of a group in their sweep
-  size_t off_blocks, off_votes, off_dense, off_tops;
+  size_t off_blocks, off_votes, off_dense, off_bounds, off_tops;
   size_t off_cmax, off_mult, off_found, off_arrived, off_part, total;
 };
 
@@ -136,6 +136,8 @@ inline SeqLayout make_seq_layout(const entmax_seq_params* p) {
     o += align_up((size_t)groups * L.ksplit * sizeof(int));
     L.off_dense = o;
     o += align_up((size_t)groups * sizeof(int));
+    L.off_bounds = o;
+    o += align_up((size_t)groups * kBlockRows * 2 * sizeof(float));
     L.off_tops = o;
     o += align_up((size_t)groups * L.ksplit * kWaves * kSeqTopWords * 64 * sizeof(float));
   }

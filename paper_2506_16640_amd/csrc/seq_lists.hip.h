@@ -27,7 +27,8 @@ struct SeqListArgs {
   SeqBlock* blocks;  // [Hkv * nblk]
   float* tops;       // [Hkv * nblk][ksplit][4 waves][kTopWords][64]
   int* votes;        // [Hkv * nblk][ksplit] 1: the rows are dense
-  int* dense;        // [Hkv * nblk] 1: left to seq_tiled_kernel
+  int* dense;        // [Hkv * nblk] kFlagDense, kFlagWithBounds: left to seq_tiled_kernel (with the rows' bounds)
+  float2* bounds;    // [Hkv * nblk][128]
   int ksplit;        // workgroups that share the keys of a block
 };
 
@@ -242,7 +243,7 @@ __device__ __forceinline__ float min8(float x) { return dpp_min<0x4E>(dpp_min<0x
 constexpr int kFinishSlots = 16;    // groups of a row that an octet can hold (eight keys each)
 constexpr int kFinishSupport = 32;  // support entries of a row noted before their values are gathered
 constexpr int kScanList = 256;      // candidates of a row that is looked through key by key
-constexpr int kScanRows = 2;        // such rows of a wave (eight rows); with more the block is seq_tiled_kernel's
+constexpr int kScanRows = 1;        // such rows of a wave (eight rows); with more the block is seq_tiled_kernel's
 
 template <int D>
 struct OctetRow {  // of a key/value row or query: the lane's 16-byte words
@@ -269,6 +270,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
   constexpr int W = D / 64, NV = 3 * NS, kItems = 24 * NS;
   __shared__ int items_[kWaves][8][kItems];
   __shared__ float2 notes_[kWaves][kScanList];
+  __shared__ float scores_[kWaves][kFinishSlots * 64];
   static_assert(kScanList >= 8 * kFinishSupport, "the octets' support notes and a scanned row's candidates take turns");
   const SeqGeom& g = A.a.g;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, oct = lane >> 3, c = lane & 7;
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
   int vote = 0;
   for (int k = 0; k < A.ksplit; ++k) vote |= A.votes[(long long)id * A.ksplit + k];
   if (vote != 0) {
-    if (wv == 0 && threadIdx.x == 0) A.dense[id] = 1;
+    if (wv == 0 && threadIdx.x == 0) A.dense[id] = kFlagDense;
     return;
   }
   SeqView v;
@@ -335,6 +337,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
     lo = fmaxf(lo, t - 4e-6f * fmaxf(1.0f, fabsf(t)));
   }
   const float cut = raw_cut(a, live, lo);
+  if (c == 0) A.bounds[(long long)id * kBlockRows + wv * 32 + li] = make_float2(lo, live ? y1 : -kInf);
 
   // ---- the groups above the bound
   int* items = items_[wave][oct];
@@ -349,8 +352,12 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
   const bool lost = live && max8(last > -3.1e38f && gn.upper(last) > cut ? 1.f : 0.f) > 0.f;
   const bool hard = lost || n > kFinishSlots;
   const unsigned long long hard_octets = __ballot(hard && c == 0);
-  if ((int)__popcll(hard_octets) > kScanRows) {
-    if (lane == 0) A.dense[id] = 1;
+  int groups = c == 0 ? n : 0;  // of the wave's rows
+#pragma unroll
+  for (int off = 8; off < 64; off <<= 1) groups += __shfl_xor(groups, off);
+  // Rescoring goes by the groups, the sweeps of the tiled kernel by the keys
+  if ((int)__popcll(hard_octets) > kScanRows || __builtin_amdgcn_readfirstlane(groups) > SweepAgain<T>::most_groups(v.L) / 4) {
+    if (lane == 0) A.dense[id] = kFlagWithBounds;
     return;  // (no barriers in this kernel)
   }
   __builtin_amdgcn_wave_barrier();
@@ -411,30 +418,34 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
   auto left_end = [&](int lim) { return -__builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)max(lim, 1))); };
 
   float2* notes = notes_[wave] + oct * kFinishSupport;
-  // ---- scores, threshold, output; SLOTS: groups held (chosen per wave)
+  // ---- the groups' scores: slot k of this lane's row at ys[k * 64]
+  float* ys = scores_[wave] + lane;
+  float top = -kInf;
+  int most = n;  // over the wave's rows
+#pragma unroll
+  for (int off = 8; off < 64; off <<= 1) most = max(most, __shfl_xor(most, off));
+  most = __builtin_amdgcn_readfirstlane(most);
+  auto key_of = [&](int it) { return OctetScores<QCtx<T, D>, T, D, 8>::first_key(it >> 1, it & 1) + 8 * (c >> 2) + (c & 3); };
+  for (int k = 0; k < most; ++k) {
+    const int it = k < n ? items[k] : 0, j = key_of(it);
+    float d = eight(j - 8 * (c >> 2) - (c & 3), true, qw);
+    if (row.c < 0.f) d = -d;
+    d = fmaf(row.w, (float)max(row.pos - j, 0), d);
+    d = k < n && j < row.lim && d > -3.0e38f ? d : -kInf;
+    top = fmaxf(top, d);
+    ys[k * 64] = d;
+  }
+  top = max8(top);
+  const bool some = top > -kInf;
+  // ---- threshold, output; SLOTS: groups held in registers (chosen per wave)
   auto finish = [&](auto slots_) {
     constexpr int SLOTS = decltype(slots_)::value;
     float y[SLOTS];
-    int j0[SLOTS];
-    float top = -kInf;
 #pragma unroll
     for (int k = 0; k < SLOTS; ++k) {
-      y[k] = -kInf;
-      j0[k] = 0;
-      if (__ballot(k < n) == 0ull) continue;
-      const int it = k < n ? items[k] : 0;
-      j0[k] = OctetScores<QCtx<T, D>, T, D, 8>::first_key(it >> 1, it & 1);
-      float d = eight(j0[k], true, qw);
-      const int j = j0[k] + 8 * (c >> 2) + (c & 3);
-      if (row.c < 0.f) d = -d;
-      d = fmaf(row.w, (float)max(row.pos - j, 0), d);
-      y[k] = k < n && j < row.lim && d > -3.0e38f ? d : -kInf;
-      top = fmaxf(top, y[k]);
+      y[k] = k < most ? ys[k * 64] : -kInf;
+      y[k] = y[k] > -kInf ? a * (y[k] - top) : -kInf;
     }
-    top = max8(top);
-    const bool some = top > -kInf;
-#pragma unroll
-    for (int k = 0; k < SLOTS; ++k) y[k] = y[k] > -kInf ? a * (y[k] - top) : -kInf;
     float blo = -1.f, bhi = left_end(row.lim), tau = -1.f;
     bool done = !some;
     for (int it = 0; __ballot(!done) != 0ull && it < kMaxSolveIters; ++it) {
@@ -456,7 +467,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
       const unsigned long long all = __ballot(p > 0.f);
       if (all == 0ull) continue;
       const unsigned mask = (unsigned)(all >> (8 * oct)) & 0xffu;
-      if (p > 0.f) notes[cnt + (int)__popc(mask & ((1u << c) - 1u))] = make_float2(__int_as_float(j0[k] + 8 * (c >> 2) + (c & 3)), p);
+      if (p > 0.f) notes[cnt + (int)__popc(mask & ((1u << c) - 1u))] = make_float2(__int_as_float(key_of(items[k])), p);
       cnt += (int)__popc(mask);
       if (__ballot(cnt > kFinishSupport - 8) != 0ull) {  // no room for another eight
         __builtin_amdgcn_wave_barrier();
@@ -469,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
     gather(notes, 0, 1, cnt);
     if (row.valid && !hard) store(row);
   };
-  if (__ballot(n > 4) == 0ull)
+  if (most <= 4)
     finish(std::integral_constant<int, 4>());
   else
     finish(std::integral_constant<int, kFinishSlots>());
@@ -503,7 +514,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
       total += (int)__popcll(all);
     }
     if (total == 0 || total > kScanList) {  // (none: the bound came from sums in another order)
-      if (lane == 0) A.dense[id] = 1;
+      if (lane == 0) A.dense[id] = kFlagWithBounds;
       continue;
     }
     __builtin_amdgcn_wave_barrier();

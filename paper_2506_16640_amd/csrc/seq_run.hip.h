@@ -60,7 +60,7 @@ bool launch_seq_tiled(const SeqArgs& a, hipStream_t st) {
   const size_t smem = SeqTiledCfg<T, D>::lds_bytes(a.mask_words);
   constexpr auto kern = seq_tiled_kernel<T, D, AM>;
   if (!ensure_dynamic_lds<kern>(smem)) return false;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(a.nblk * a.g.Hkv)), dim3(kThreads), smem, st, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(a.nblk * a.g.Hkv)), dim3((SeqTiledCfg<T, D>::NT)), smem, st, a);
   return launch_ok();
 }
 
@@ -102,6 +102,7 @@ bool launch_seq(const SeqArgs& a_in, const SeqListArgs& l, const SeqDecodeArgs& 
     if (l.ksplit > 0) {
       if (!launch_seq_lists<D, AM>(l, st)) return false;
       a.dense = l.dense;
+      a.bounds = l.bounds;
     }
   }
   if (L.blocks && !launch_seq_tiled<T, D, AM>(a, st)) return false;
@@ -121,13 +122,18 @@ int run_seq(const SeqCall& c) {
   a.V = c.V;
   a.O = c.O;
   a.nblk = (int)seq_blocks(p->nseq, p->T, a.g.G);
-  a.mask_words = (p->max_keys + 1023) / 1024 + 1;
+  // a bit per 32-key block, per more of them where that takes more than 1024 words
+  a.mask_shift = 0;
+  while ((p->max_keys >> (10 + a.mask_shift)) >= 1024) ++a.mask_shift;
+  a.mask_words = (p->max_keys >> (10 + a.mask_shift)) + 1;
   a.split = L.split && p->path == 0 ? 1 : 0;
   if (!a.split) L.blocks = true;
   a.dense = nullptr;
+  a.bounds = nullptr;
   SeqListArgs l;
   l.a = a;
   l.blocks = reinterpret_cast<SeqBlock*>(c.ws + L.off_blocks);
+  l.bounds = reinterpret_cast<float2*>(c.ws + L.off_bounds);
   l.votes = reinterpret_cast<int*>(c.ws + L.off_votes);
   l.dense = reinterpret_cast<int*>(c.ws + L.off_dense);
   l.tops = reinterpret_cast<float*>(c.ws + L.off_tops);

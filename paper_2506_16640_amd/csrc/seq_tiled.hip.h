@@ -1,11 +1,14 @@
 // Entmax attention of packed sequences over packed or paged keys, any density: one workgroup per 128 folded rows of a
 // key/value head (SeqRows), key tiles through LDS, scores recomputed by every sweep (S^T = K Q^T, a lane owns a row):
-//   1. a sample of the key tiles: bounds and a starting point for the threshold tau of
+//   1. bounds and a starting point for the threshold tau of
 //        f(tau) = sum_j [y_j - tau]_+^r - 1 = 0,   y = (alpha-1) s,  r = 1 / (alpha-1)
+//      from the list kernels, or from a sample of the key tiles
 //   2. sweeps over K that evaluate f and step (solve_step()); the first one notes which 32-key blocks can hold a positive term at all
 //   3. a sweep over K and V: O^T = V^T P^T on the matrix cores.  The accumulators of S^T are the second operand as they are; V^T comes out
 //      of row-major tiles through transposing LDS reads (ds_read_b64_tr_b16: sixteen lanes give four rows of sixteen
 //      elements, each lane gets a column), so that no transposed copy of V exists anywhere.
+// A block's sweeps follow one another, and few blocks may be left to this kernel: so a block has 8 or 16 waves, and KS of them share the
+// keys of each tile for the same 32 rows (their sums are added in their order).
 #pragma once
 #include "fwd.hip.h"
 #include "seq.hip.h"
@@ -20,8 +23,9 @@ struct SeqArgs {
   const void* V;
   void* O;
   int nblk;        // 128-row groups per key/value head (seq_blocks())
-  int mask_words;  // uint32 words that hold a bit per 32-key block
-  const int* dense;  // NULL, or [Hkv * nblk]: only the groups that are marked
+  int mask_words, mask_shift;  // a bit for every 1 << mask_shift 32-key blocks in so many uint32 words
+  const int* dense;  // NULL, or [Hkv * nblk]: only the groups that are marked, kFlagDense or kFlagWithBounds
+  const float2* bounds;  // with dense: [Hkv * nblk][128] of groups with bounds: (lower bound of the threshold, (alpha-1) x largest score)
   int split;       // sequences with few rows are left to the kernels that split the keys
 };
 
@@ -45,10 +49,13 @@ __device__ __forceinline__ bool seq_block(const SeqGeom& g, int blk, bool split,
 
 template <typename T, int D>
 struct SeqTiledCfg {
-  static constexpr int KT = sizeof(T) == 2 ? 64 : 32;
+  static constexpr int NT = sizeof(T) == 2 && D == 64 ? 1024 : 512;  // (registers: 128 a thread, or 256)
+  static constexpr int KS = NT / kThreads;                           // waves that share the keys of 32 rows
+  static constexpr int BW = sizeof(T) == 4 && D == 128 ? 1 : 2;      // 32-key blocks of a wave per tile
+  static constexpr int KT = KS * BW * 32;
   static constexpr int kTileBytes = KT * D * (int)sizeof(T);
-  static constexpr int kOcc = sizeof(T) == 2 && D == 64 ? 3 : (sizeof(T) == 2 ? 2 : 1);
-  static size_t lds_bytes(int mask_words) { return 4 * (size_t)kTileBytes + (size_t)(kWaves + 1) * mask_words * 4; }
+  static_assert(kTileBytes == 32768, "four tiles and the masks fit a compute unit");
+  static size_t lds_bytes(int mask_words) { return 4 * (size_t)kTileBytes + (size_t)kWaves * mask_words * 4; }
 };
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -59,10 +66,10 @@ __device__ __forceinline__ uint2 read_transposed(const char* lds) {
 
 // Fragments of V^T for the product that contracts over the 16 keys 16 c .. 16 c + 15 of a 32-key block, in the order of the accumulators:
 // element e of half hh is key 16 c + 8 (e / 4) + 4 hh + e % 4.
-template <typename T, int D, int KT>
+template <typename T, int D, int KT, int NT = kThreads>
 struct SeqValues {
   static constexpr int NM = D / 32;
-  using VT = SeqTile<T, D, KT, sizeof(T) == 2>;
+  using VT = SeqTile<T, D, KT, sizeof(T) == 2, NT>;
   int voff[NM];
   int li, hh;
   __device__ __forceinline__ void init(int lane) {
@@ -170,19 +177,20 @@ __device__ __forceinline__ void store4(T* dst, float x0, float x1, float x2, flo
 }
 
 template <typename T, int D, int AM>
-__global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled_kernel(SeqArgs A) {
+__global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqArgs A) {
   using Cfg = SeqTiledCfg<T, D>;
-  constexpr int KT = Cfg::KT, NSB = KT / 32, NC = D / 16, NM = D / 32, TB = Cfg::kTileBytes;
-  using KTile = SeqTile<T, D, KT, false>;
-  using Vals = SeqValues<T, D, KT>;
+  constexpr int NT = Cfg::NT, KS = Cfg::KS, BW = Cfg::BW, KT = Cfg::KT, NSB = KT / 32, NC = D / 16, NM = D / 32, TB = Cfg::kTileBytes;
+  using KTile = SeqTile<T, D, KT, false, NT>;
+  using Vals = SeqValues<T, D, KT, NT>;
   using VTile = typename Vals::VT;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const SeqGeom& g = A.g;
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rg = wave & 3, ks = wave >> 2;
   // The head runs fastest, so that a head's groups meet on one XCD where the heads divide among the eight of them; the groups run from the
   // last to the first, a sequence's long rows first.
   const int hk = blockIdx.x % g.Hkv, blk = A.nblk - 1 - (int)blockIdx.x / g.Hkv;
-  if (A.dense && A.dense[hk * A.nblk + blk] == 0) return;
+  const int flag = A.dense ? A.dense[hk * A.nblk + blk] : kFlagDense;
+  if (flag == 0) return;
   SeqView v;
   int blk0;
   if (!seq_block(g, blk, A.split != 0, v, blk0)) return;  // (the same for the whole workgroup)
@@ -190,7 +198,7 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
   keys.init(g, v, A.K, hk, false, sizeof(T));
   vals.init(g, v, A.V, hk, true, sizeof(T));
   SeqRows<T, D> q;
-  q.init(g, v, A.Q, hk, blk0 + wave * 32);
+  q.init(g, v, A.Q, hk, blk0 + rg * 32);
   const int last_row = min(v.n * g.G, blk0 + kBlockRows) - 1;
   const int block_lim = g.causal ? max(0, min(v.L - v.n + last_row / g.G + 1, v.L)) : v.L;
   const int ntiles = __builtin_amdgcn_readfirstlane((block_lim + KT - 1) / KT);
@@ -199,24 +207,24 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
   const int lane = q.lane;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
 
-  WaveMask wm;
-  wm.words = reinterpret_cast<uint32_t*>(smem + 4 * TB);
-  wm.nwords = A.mask_words;
-  for (int w = threadIdx.x; w < (kWaves + 1) * A.mask_words; w += kThreads) wm.words[w] = 0u;
+  // which blocks can hold a positive term for some row of the row group: set in the first sweep over all keys
+  uint32_t* marks = reinterpret_cast<uint32_t*>(smem + 4 * TB);  // [4 row groups][mask_words]
+  for (int w = threadIdx.x; w < kWaves * A.mask_words; w += NT) marks[w] = 0u;
+  auto marked = [&](int group, int jb) {
+    const uint32_t word = __builtin_amdgcn_readfirstlane(marks[group * A.mask_words + (jb >> (A.mask_shift + 5))]);
+    return ((word >> ((jb >> A.mask_shift) & 31)) & 1u) != 0u;
+  };
+  auto tile_marked = [&](int kt) {
+    bool any = false;
+    for (int b = 0; b < NSB; ++b)
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) any = any || marked(k, kt * NSB + b);
+    return any;
+  };
 
   FragOff<T> koff[NC];
 #pragma unroll
   for (int cc = 0; cc < NC; ++cc) koff[cc] = FragOff<T>::template make<typename KTile::Tile>(q.li, 2 * cc + q.hh);
-  auto scores = [&](const char* tl, int sb, int kt) {
-    f32x16_t acc = q.start(kt * KT + sb * 32);
-#pragma unroll
-    for (int cc = 0; cc < NC; ++cc) acc = Elem<T>::mma(koff[cc].load(tl, sb * 32 * KTile::kRowBytes), q.qf[cc], acc);
-    return acc;
-  };
-  auto visible = [&](int kt) -> uint32_t {  // blocks of the tile that some row of the wave sees
-    const int n = min(max((q.lim_max - kt * KT + 31) >> 5, 0), NSB);
-    return (1u << n) - 1u;
-  };
   auto next = [&](int kt, auto needed) {
     while (kt < ntiles && !needed(kt)) ++kt;
     return kt;
@@ -272,55 +280,93 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
       t3 = t4;
     }
   };
-  // fn(acc, sb, masked) on the scores of the blocks in act
-  auto each_block = [&](int kt, const char* tl, uint32_t act, auto fn) {
-    f32x16_t acc[NSB];
+  // fn(acc, block of the tile, masked) on the scores of this wave's blocks of the tile that some row of it sees; with `only_marked` of those
+  // that are marked
+  auto each_block = [&](int kt, const char* tl, bool only_marked, auto fn) {
+    f32x16_t acc[BW];
+    bool act[BW];
 #pragma unroll
-    for (int sb = 0; sb < NSB; ++sb)
-      if (act & (1u << sb)) acc[sb] = scores(tl, sb, kt);
+    for (int b = 0; b < BW; ++b) {
+      const int sb = ks * BW + b, j0 = kt * KT + sb * 32;
+      act[b] = j0 < q.lim_max && (!only_marked || marked(rg, kt * NSB + sb));
+      if (!act[b]) continue;
+      acc[b] = q.start(j0);
 #pragma unroll
-    for (int sb = 0; sb < NSB; ++sb) {
-      if (!(act & (1u << sb))) continue;
-      const int j0 = kt * KT + sb * 32;
+      for (int cc = 0; cc < NC; ++cc) acc[b] = Elem<T>::mma(koff[cc].load(tl, sb * 32 * KTile::kRowBytes), q.qf[cc], acc[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < BW; ++b) {
+      if (!act[b]) continue;
+      const int sb = ks * BW + b, j0 = kt * KT + sb * 32;
       const bool masked = holes || j0 + 32 > q.lim_min;
-      if (masked) q.mask(acc[sb], j0, keys, holes);
-      fn(acc[sb], sb, masked);
+      if (masked) q.mask(acc[b], j0, keys, holes);
+      fn(acc[b], sb, masked);
     }
   };
+  // Exchange between the waves that share the row group's keys (in the tile buffers, which are free between sweeps).
+  f32x4_t* xch = reinterpret_cast<f32x4_t*>(smem);
+  auto post = [&](const f32x4_t& x) {
+    xch[wave * 64 + lane] = x;
+    __syncthreads();
+  };
 
-  // ------------------------------------------------------------ 1. a sample of the tiles
-  // (about eight tiles; all of them where there are no more, and where a tile may show a row no key at all)
-  const int every = holes ? 1 : max(1, ntiles >> 3);
-  float m = -kInf, ms1 = 0.f, ms2 = 0.f, msn = 0.f;
-  sweep_k([&](int kt) { return kt % every == 0; },
-          [&](int kt, const char* tl) {
-            each_block(kt, tl, visible(kt), [&](f32x16_t& acc, int, bool masked) {
-              if (!masked && AM != 0) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  ms1 += acc[e];
-                  ms2 = fmaf(acc[e], acc[e], ms2);
-                }
-                msn += 32.f;
-              }
-              m = fmaxf(m, max16(acc));
-            });
-          });
-  m = fmaxf(m, __shfl_xor(m, 32));
-  ms1 += __shfl_xor(ms1, 32);
-  ms2 += __shfl_xor(ms2, 32);
-  const bool live = q.lim > 0 && m > -kInf;
-  float my = live ? q.a * m : 0.f;
-  float lo = my - 1.0f;  // (the largest score is at least the sample's)
-  const float lo0 = lo;  // blocks without a term above it are zero for good
+  // ------------------------------------------------------------ 1. where to start
+  const bool given = flag == kFlagWithBounds;
+  float m = -kInf, my = 0.f, lo = -1.f, hi = 0.f, tau = -1.f;
   const float below = q.lim > 0 ? __builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)q.lim)) : 1.f;
-  float hi = every == 1 ? my - below : kInf;
-  float tau = lo;
-  if (live && msn >= 64.f) {
-    const float mean = ms1 / msn, var = ms2 / msn - mean * mean;
-    float t0;
-    if (var > 0.f && gauss_start<AM>(q.a * mean, q.a * sqrtf(var), (float)q.lim, t0)) tau = fminf(fmaxf(t0, lo), hi);
+  bool live, know_max = true;
+  if (given) {
+    const float2 bd = A.bounds[((long long)hk * A.nblk + blk) * kBlockRows + rg * 32 + q.li];
+    my = bd.y;
+    live = q.lim > 0 && my > -kInf;
+    if (!live) my = 0.f;
+    hi = my - below;
+    lo = live ? fminf(fmaxf(my - 1.0f, bd.x), hi) : my - 1.0f;
+    tau = lo;
+  } else {
+    // a sample of about four tiles (all of them where there are no more, and where a tile may show a row no key at all)
+    const int every = holes ? 1 : max(1, ntiles >> 2);
+    float ms1 = 0.f, ms2 = 0.f, msn = 0.f;
+    sweep_k([&](int kt) { return kt % every == 0; },
+            [&](int kt, const char* tl) {
+              each_block(kt, tl, false, [&](f32x16_t& acc, int, bool masked) {
+                if (!masked && AM != 0) {
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) {
+                    ms1 += acc[e];
+                    ms2 = fmaf(acc[e], acc[e], ms2);
+                  }
+                  msn += 32.f;
+                }
+                m = fmaxf(m, max16(acc));
+              });
+            });
+    m = fmaxf(m, __shfl_xor(m, 32));
+    ms1 += __shfl_xor(ms1, 32);
+    ms2 += __shfl_xor(ms2, 32);
+    post(f32x4_t{m, ms1, ms2, msn});
+    ms1 = ms2 = msn = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const f32x4_t x = xch[(4 * k + rg) * 64 + lane];
+      m = fmaxf(m, x[0]);
+      ms1 += x[1];
+      ms2 += x[2];
+      msn += x[3];
+    }
+    live = q.lim > 0 && m > -kInf;
+    know_max = every == 1;
+    my = live ? q.a * m : 0.f;
+    lo = my - 1.0f;  // (the largest score is at least the sample's)
+    hi = know_max ? my - below : kInf;
+    tau = lo;
+    if (live && msn >= 64.f) {
+      const float mean = ms1 / msn, var = ms2 / msn - mean * mean;
+      float t0;
+      if (var > 0.f && gauss_start<AM>(q.a * mean, q.a * sqrtf(var), (float)q.lim, t0)) tau = fminf(fmaxf(t0, lo), hi);
+    }
   }
+  const float lo0 = lo;  // blocks without a term above it are zero for good
 
   // ------------------------------------------------------------ 2. threshold
   bool done = !live;
@@ -330,31 +376,44 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
     RowSums sums;
     sums.clear();
     const bool first = iter == 0;
-    sweep_k([&](int kt) { return first || wm.tile_bits<NSB>(kWaves, kt) != 0u; },
+    sweep_k([&](int kt) { return first || tile_marked(kt); },
             [&](int kt, const char* tl) {
               if (!wave_on) return;
-              uint32_t act = visible(kt);
-              if (!first) act &= wm.tile_bits<NSB>(wave, kt);
-              each_block(kt, tl, act, [&](f32x16_t& acc, int sb, bool masked) {
+              each_block(kt, tl, !first, [&](f32x16_t& acc, int sb, bool masked) {
                 const float lm = max16(acc);
                 if (first) {
                   m = fmaxf(m, lm);
                   const bool any = live && lm > -kInf && fmaf(lm, q.a, -lo0) > 0.f;
-                  if (__ballot(any) != 0ull && lane == 0) wm.set(wave, kt * NSB + sb);
+                  const int jb = kt * NSB + sb;
+                  if (__ballot(any) != 0ull && lane == 0)
+                    atomicOr(&marks[rg * A.mask_words + (jb >> (A.mask_shift + 5))], 1u << ((jb >> A.mask_shift) & 31));
                 }
                 const bool cand = lm > -kInf && fmaf(lm, q.a, -tau) > 0.f && !done;
                 if (__ballot(cand) == 0ull) return;
                 accumulate_block<AM>(sums, acc, q.a, tau, r, masked);
               });
             });
-    if (first) {
-      wm.merge(threadIdx.x);
+    sums.combine_halves();
+    post(f32x4_t{sums.s0, sums.s1, sums.s2, sums.xmin});
+    sums.clear();
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const f32x4_t x = xch[(4 * k + rg) * 64 + lane];
+      sums.s0 += x[0];
+      sums.s1 += x[1];
+      sums.s2 += x[2];
+      sums.xmin = fminf(sums.xmin, x[3]);
+    }
+    if (first && !know_max) {
+      __syncthreads();
       m = fmaxf(m, __shfl_xor(m, 32));
+      post(f32x4_t{m, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int k = 0; k < KS; ++k) m = fmaxf(m, xch[(4 * k + rg) * 64 + lane][0]);
       my = live ? q.a * m : 0.f;
       lo = fmaxf(lo, my - 1.0f);
       hi = my - below;
     }
-    sums.combine_halves();
     if (!done) done = solve_step<AM>(sums, r, tau, lo, hi);
     ++iter;
     more = __syncthreads_or(done ? 0 : 1);
@@ -368,7 +427,6 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
   Vals vv;
   vv.init(lane);
   {
-    auto needed = [&](int kt) { return wm.tile_bits<NSB>(kWaves, kt) != 0u; };
     typename KTile::Pages pk;
     typename VTile::Pages pv;
     auto ask = [&](int t) {
@@ -379,12 +437,11 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
       KTile::load(keys, pk, t * KT, v.L, lds0 + (uint32_t)(2 * buf) * TB, wave, lane);
       VTile::load(vals, pv, t * KT, v.L, lds0 + (uint32_t)(2 * buf + 1) * TB, wave, lane);
     };
-    int t0 = next(0, needed), t1 = ntiles;
-    __syncthreads();
+    int t0 = next(0, tile_marked), t1 = ntiles;
     if (t0 < ntiles) {
       ask(t0);
       issue(t0, 0);
-      t1 = next(t0 + 1, needed);
+      t1 = next(t0 + 1, tile_marked);
       if (t1 < ntiles) ask(t1);
     }
     lds_loads_wait<0>();
@@ -394,12 +451,11 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
       int t2 = ntiles;
       if (t1 < ntiles) {
         issue(t1, cur ^ 1);
-        t2 = next(t1 + 1, needed);
+        t2 = next(t1 + 1, tile_marked);
         if (t2 < ntiles) ask(t2);
       }
       const char* tl = smem + cur * 2 * TB;
-      const int kt = t0;
-      each_block(kt, tl, visible(kt) & wm.tile_bits<NSB>(wave, kt), [&](f32x16_t& acc, int sb, bool masked) {
+      each_block(t0, tl, true, [&](f32x16_t& acc, int sb, bool masked) {
         const float lm = max16(acc);
         const bool cand = live && lm > -kInf && fmaf(lm, q.a, -tau) > 0.f;
         if (__ballot(cand) == 0ull) return;  // every probability of the block is zero
@@ -418,13 +474,29 @@ __global__ __launch_bounds__(kThreads, (SeqTiledCfg<T, D>::kOcc)) void seq_tiled
       t1 = t2;
     }
   }
-  if (!q.valid) return;
-  T* o = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + q.t) * g.o_st + (long long)q.head * g.o_sh;
+  // the sums of the waves that shared the keys, each of them adding up its part of the features
+  f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);  // [waves][NM * 4][64]
 #pragma unroll
   for (int mm = 0; mm < NM; ++mm)
 #pragma unroll
-    for (int x = 0; x < 16; x += 4)
-      store4<T>(o + 32 * mm + 2 * x + 4 * q.hh, oacc[mm][x], oacc[mm][x + 1], oacc[mm][x + 2], oacc[mm][x + 3]);
+    for (int x = 0; x < 4; ++x)
+      red[(wave * NM * 4 + mm * 4 + x) * 64 + lane] = f32x4_t{oacc[mm][4 * x], oacc[mm][4 * x + 1], oacc[mm][4 * x + 2], oacc[mm][4 * x + 3]};
+  __syncthreads();
+  if (!q.valid) return;
+  T* o = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + q.t) * g.o_st + (long long)q.head * g.o_sh;
+  constexpr int PER = NM * 4 / KS;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int f = ks * PER + u;  // features 32 (f / 4) + 8 (f % 4) + 4 hh on
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const f32x4_t x = red[((4 * k + rg) * NM * 4 + f) * 64 + lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    }
+    store4<T>(o + 8 * f + 4 * q.hh, sum[0], sum[1], sum[2], sum[3]);
+  }
 }
 
 }  // namespace entmax
