@@ -151,7 +151,9 @@ struct SeqRow {
   int t, head;          // token of the sequence, query head
   bool valid;
   int lim, pos;         // keys j < lim are visible; the row's position
-  float a, c, w;        // as in QCtx: y_ij = a d_ij, d_ij = +-<q_i, k_j> + w max(pos - j, 0)
+  // as in QCtx: y_ij = a d_ij, d_ij = +-<q_i, k_j> + w max(pos - j, 0).  A row of scale 0 (c = 0) has a = 1 and d_ij = 0, so that masked
+  // scores are never multiplied by zero.
+  float a, c, w;
   __device__ __forceinline__ void init(const SeqGeom& g, const SeqView& v, int hk, int r, int D) {
     valid = r < v.n * g.G;
     t = valid ? r / g.G : 0;
@@ -172,7 +174,13 @@ struct SeqRow {
       const float m = valid ? g.slopes[head] : 0.f;
       if (m != 0.f && a != 0.f) w = g.bias_mode == 0 ? (c < 0.f ? m : -m) * sqrtf((float)D) : -(g.alpha - 1.0f) * m / a;
     }
+    if (a == 0.f) {
+      a = 1.0f;
+      c = 0.f;
+    }
   }
+  // d_ij from the dot product, without the bias
+  __device__ __forceinline__ float signed_dot(float d) const { return c < 0.f ? -d : (c == 0.f ? 0.f : d); }
   __device__ __forceinline__ SeqRow of_lane(int l) const {
     SeqRow x;
     x.t = __shfl(t, l);
@@ -210,7 +218,7 @@ struct SeqRows : SeqRow {
     const T* q = reinterpret_cast<const T*>(Q) + (long long)(v.row0 + t) * g.q_st + (long long)head * g.q_sh;
 #pragma unroll
     for (int cc = 0; cc < NC; ++cc) {
-      Frag<T> f = valid ? Elem<T>::load(q + 16 * cc + 8 * hh) : Elem<T>::zero();
+      Frag<T> f = c != 0.f ? Elem<T>::load(q + 16 * cc + 8 * hh) : Elem<T>::zero();  // (0 beyond the last row, too)
       qf[cc] = c < 0.f ? Elem<T>::negate(f) : f;
     }
   }

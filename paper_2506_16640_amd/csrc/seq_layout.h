@@ -131,7 +131,7 @@ inline SeqLayout make_seq_layout(const entmax_seq_params* p) {
     const long long groups = seq_blocks(p->nseq, p->T, G) * p->Hkv;
     L.ksplit = seq_ksplit(groups, p->max_keys);
     L.off_blocks = o;
-    o += align_up((size_t)groups * 2 * sizeof(int));
+    o += align_up((size_t)groups * 5 * sizeof(int));
     L.off_votes = o;
     o += align_up((size_t)groups * L.ksplit * sizeof(int));
     L.off_dense = o;

@@ -17,11 +17,6 @@ namespace entmax {
 constexpr int kTopWords = kTopGroups + 2;  // of a lane: its groups, its largest score, how many of the groups were kept throughout
 static_assert(kTopWords == kSeqTopWords, "the workspace holds them");
 
-// what the sweep leaves of a block of 128 rows
-struct SeqBlock {
-  int s, r0;   // sequence (or -1: nothing to do), first folded row
-};
-
 struct SeqListArgs {
   SeqArgs a;
   SeqBlock* blocks;  // [Hkv * nblk]
@@ -57,7 +52,7 @@ __global__ __launch_bounds__(kThreads, 3) void seq_sweep_kernel(SeqListArgs A) {
   int r0;
   const bool mine = seq_block(g, blk, A.a.split != 0, v, r0);
   if (part == 0 && threadIdx.x == 0) {
-    A.blocks[id] = SeqBlock{mine ? v.s : -1, r0};
+    A.blocks[id] = SeqBlock{mine ? v.s : -1, v.row0, v.n, v.L, r0};
     A.dense[id] = 0;
   }
   if (!mine) return;
@@ -284,8 +279,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
     if (wv == 0 && threadIdx.x == 0) A.dense[id] = kFlagDense;
     return;
   }
-  SeqView v;
-  if (!load_seq(g, b.s, v)) return;
+  const SeqView v{b.s, b.row0, b.n, b.L};
   SeqKeys keys, vals;
   keys.init(g, v, A.a.K, hk, false, sizeof(T));
   vals.init(g, v, A.a.V, hk, true, sizeof(T));
@@ -338,6 +332,8 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
   }
   const float cut = raw_cut(a, live, lo);
   if (c == 0) A.bounds[(long long)id * kBlockRows + wv * 32 + li] = make_float2(lo, live ? y1 : -kInf);
+  if (__builtin_amdgcn_readfirstlane(__hip_atomic_load(&A.dense[id], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) != 0)
+    return;  // (others of the block's rows have given it up)
 
   // ---- the groups above the bound
   int* items = items_[wave][oct];
@@ -429,7 +425,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
   for (int k = 0; k < most; ++k) {
     const int it = k < n ? items[k] : 0, j = key_of(it);
     float d = eight(j - 8 * (c >> 2) - (c & 3), true, qw);
-    if (row.c < 0.f) d = -d;
+    d = row.signed_dot(d);
     d = fmaf(row.w, (float)max(row.pos - j, 0), d);
     d = k < n && j < row.lim && d > -3.0e38f ? d : -kInf;
     top = fmaxf(top, d);
@@ -502,7 +498,7 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
     for (int j8 = 0; j8 < hr.lim; j8 += 64) {
       const int first = j8 + 8 * oct, j = first + c;
       float d = eight(first, false, hq);
-      if (hr.c < 0.f) d = -d;
+      d = hr.signed_dot(d);
       d = fmaf(hr.w, (float)max(hr.pos - j, 0), d);
       const bool in = j < hr.lim && d > hcut && d > -3.0e38f;
       const unsigned long long all = __ballot(in);

@@ -57,7 +57,7 @@ inline SeqGeom make_seq_geom(const SeqCall& c) {
 
 template <typename T, int D, int AM>
 bool launch_seq_tiled(const SeqArgs& a, hipStream_t st) {
-  const size_t smem = SeqTiledCfg<T, D>::lds_bytes(a.mask_words);
+  const size_t smem = SeqTiledCfg<T, D>::lds_bytes(a.mark_words);
   constexpr auto kern = seq_tiled_kernel<T, D, AM>;
   if (!ensure_dynamic_lds<kern>(smem)) return false;
   hipLaunchKernelGGL(kern, dim3((unsigned)(a.nblk * a.g.Hkv)), dim3((SeqTiledCfg<T, D>::NT)), smem, st, a);
@@ -103,6 +103,7 @@ bool launch_seq(const SeqArgs& a_in, const SeqListArgs& l, const SeqDecodeArgs& 
       if (!launch_seq_lists<D, AM>(l, st)) return false;
       a.dense = l.dense;
       a.bounds = l.bounds;
+      a.blocks = l.blocks;
     }
   }
   if (L.blocks && !launch_seq_tiled<T, D, AM>(a, st)) return false;
@@ -122,14 +123,16 @@ int run_seq(const SeqCall& c) {
   a.V = c.V;
   a.O = c.O;
   a.nblk = (int)seq_blocks(p->nseq, p->T, a.g.G);
-  // a bit per 32-key block, per more of them where that takes more than 1024 words
-  a.mask_shift = 0;
-  while ((p->max_keys >> (10 + a.mask_shift)) >= 1024) ++a.mask_shift;
-  a.mask_words = (p->max_keys >> (10 + a.mask_shift)) + 1;
+  // a word per key tile, per more of them where that takes more than 16 KB
+  constexpr int KT = SeqTiledCfg<T, D>::KT;
+  a.mark_shift = 0;
+  while ((p->max_keys / KT >> a.mark_shift) >= 4095) ++a.mark_shift;
+  a.mark_words = (p->max_keys / KT >> a.mark_shift) + 1;
   a.split = L.split && p->path == 0 ? 1 : 0;
   if (!a.split) L.blocks = true;
   a.dense = nullptr;
   a.bounds = nullptr;
+  a.blocks = nullptr;
   SeqListArgs l;
   l.a = a;
   l.blocks = reinterpret_cast<SeqBlock*>(c.ws + L.off_blocks);

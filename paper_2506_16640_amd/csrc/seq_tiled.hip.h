@@ -16,6 +16,11 @@
 
 namespace entmax {
 
+// What the sweep of the list kernels leaves of a group of 128 rows, so that nobody has to look for its sequence again
+struct SeqBlock {
+  int s, row0, n, L, r0;  // the sequence (see SeqView; s = -1: nothing to do) and the group's first folded row
+};
+
 struct SeqArgs {
   SeqGeom g;
   const void* Q;
@@ -23,8 +28,9 @@ struct SeqArgs {
   const void* V;
   void* O;
   int nblk;        // 128-row groups per key/value head (seq_blocks())
-  int mask_words, mask_shift;  // a bit for every 1 << mask_shift 32-key blocks in so many uint32 words
+  int mark_shift, mark_words;  // seq_tiled_kernel: a word of marks for every 1 << mark_shift key tiles
   const int* dense;  // NULL, or [Hkv * nblk]: only the groups that are marked, kFlagDense or kFlagWithBounds
+  const SeqBlock* blocks;  // with dense: [Hkv * nblk]
   const float2* bounds;  // with dense: [Hkv * nblk][128] of groups with bounds: (lower bound of the threshold, (alpha-1) x largest score)
   int split;       // sequences with few rows are left to the kernels that split the keys
 };
@@ -49,13 +55,80 @@ __device__ __forceinline__ bool seq_block(const SeqGeom& g, int blk, bool split,
 
 template <typename T, int D>
 struct SeqTiledCfg {
-  static constexpr int NT = sizeof(T) == 2 && D == 64 ? 1024 : 512;  // (registers: 128 a thread, or 256)
+  static constexpr int NT = sizeof(T) == 2 ? (D == 64 ? 1024 : 512) : (D == 64 ? 512 : 256);  // (registers: 128, 256 or 512 a thread)
   static constexpr int KS = NT / kThreads;                           // waves that share the keys of 32 rows
-  static constexpr int BW = sizeof(T) == 4 && D == 128 ? 1 : 2;      // 32-key blocks of a wave per tile
+  static constexpr int BW = 2;                                       // 32-key blocks of a wave per tile
   static constexpr int KT = KS * BW * 32;
   static constexpr int kTileBytes = KT * D * (int)sizeof(T);
   static_assert(kTileBytes == 32768, "four tiles and the masks fit a compute unit");
-  static size_t lds_bytes(int mask_words) { return 4 * (size_t)kTileBytes + (size_t)kWaves * mask_words * 4; }
+  static size_t lds_bytes(int mark_words) { return 4 * (size_t)kTileBytes + (size_t)mark_words * 4; }
+};
+
+// Partial sums of the threshold function over a lane's keys at tau, x = [y - tau]_+ (at most 1, for tau is never below the largest y by
+// more: the clamp of the multiply-add is the lower and the upper limit in one):  g = sum x^(r-1), h = sum x^r, and with CURV
+// k = sum x^(r-2) (alpha 1.5: the count; alpha 2 and general alpha: not formed).
+struct SeqSums {
+  float g, h, k;
+};
+template <int AM, bool CURV>
+__device__ __forceinline__ void accumulate_keys(SeqSums& s, const f32x16_t& acc, float a, float tau, float r) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float x = __builtin_amdgcn_fmed3f(fmaf(acc[e], a, -tau), 0.f, 1.f);
+    if (AM == 1) {
+      s.g += x;
+      s.h = fmaf(x, x, s.h);
+      if (CURV) s.k += x > 0.f ? 1.f : 0.f;
+    } else if (AM == 2) {
+      s.h += x;
+      s.g += x > 0.f ? 1.f : 0.f;
+    } else if (AM == 3) {
+      const float x2 = x * x;
+      s.g = fmaf(x2, x, s.g);
+      s.h = fmaf(x2, x2, s.h);
+      if (CURV) s.k += x2;
+    } else if (x > 0.f) {
+      const float l = __builtin_amdgcn_logf(x);
+      s.h += __builtin_amdgcn_exp2f(r * l);
+      s.g += __builtin_amdgcn_exp2f((r - 1.f) * l);
+    }
+  }
+}
+
+// The search for a row's threshold from sums over all its keys, sweep by sweep.  f = h - 1, f' = -r g; the curvature comes from k
+// where it was formed, else from the change of g since the sweep before: the root of the quadratic model, inside the bracket.
+//   No sweep is spent on confirming the last step.  The model leaves out the third order: after a step t about t^3 w^2 is left, w the larger of g and
+// 2 B / A (both about one over the typical x), without a curvature t^2 w r / 2; a step that leaves less than 2^-20 by 64 times (16 times) that ends the
+// search.  (Rows of 40 to 4096 normal scores, alpha 1.25 to 1.7, from the list kernels' bounds: 1.5 sweeps, threshold within 2e-6; confirming would take one more.)
+// At alpha 2, where f is piecewise linear and its curvature jumps from key to key, the last step is confirmed.
+struct SeqSearch {
+  float tau, lo, hi, g_before, tau_before;
+  bool before;
+  __device__ __forceinline__ bool step(const SeqSums& s, float r, bool with_k, bool linear) {
+    const float f = s.h - 1.0f, A = r * s.g;
+    if (f >= 0.f) lo = fmaxf(lo, tau); else hi = fminf(hi, tau);
+    float B = 0.f;  // half of f''
+    bool curved = false;
+    if (with_k) {
+      B = 0.5f * r * (r - 1.0f) * s.k;
+      curved = true;
+    } else if (before && !linear && tau != tau_before) {
+      B = fmaxf(0.5f * r * (g_before - s.g) / (tau - tau_before), 0.f);
+      curved = true;
+    }
+    const float t = 2.0f * f / (A + __builtin_amdgcn_sqrtf(fmaxf(fmaf(A, A, -4.0f * B * f), 0.f)));
+    float to = tau + t;
+    const bool in = A > 0.f && to >= lo && to <= hi;
+    if (!in) to = hi < kInf ? 0.5f * (lo + hi) : lo;
+    const float at = fabsf(t), w = fmaxf(s.g, A > 0.f ? 2.0f * B / A : 0.f);
+    const float left = linear ? at : (curved ? 64.0f * at * (at * w) * (at * w) : 8.0f * at * (at * w) * r);
+    const bool fin = (in && left <= 0x1p-20f) || hi - lo <= 0x1p-22f;
+    before = true;
+    g_before = s.g;
+    tau_before = tau;
+    tau = to;
+    return fin;
+  }
 };
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -193,7 +266,13 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqA
   if (flag == 0) return;
   SeqView v;
   int blk0;
-  if (!seq_block(g, blk, A.split != 0, v, blk0)) return;  // (the same for the whole workgroup)
+  if (A.dense) {
+    const SeqBlock b = A.blocks[hk * A.nblk + blk];
+    v = SeqView{b.s, b.row0, b.n, b.L};
+    blk0 = b.r0;
+  } else if (!seq_block(g, blk, A.split != 0, v, blk0)) {  // (the same for the whole workgroup)
+    return;
+  }
   SeqKeys keys, vals;
   keys.init(g, v, A.K, hk, false, sizeof(T));
   vals.init(g, v, A.V, hk, true, sizeof(T));
@@ -207,20 +286,13 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqA
   const int lane = q.lane;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
 
-  // which blocks can hold a positive term for some row of the row group: set in the first sweep over all keys
-  uint32_t* marks = reinterpret_cast<uint32_t*>(smem + 4 * TB);  // [4 row groups][mask_words]
-  for (int w = threadIdx.x; w < kWaves * A.mask_words; w += NT) marks[w] = 0u;
-  auto marked = [&](int group, int jb) {
-    const uint32_t word = __builtin_amdgcn_readfirstlane(marks[group * A.mask_words + (jb >> (A.mask_shift + 5))]);
-    return ((word >> ((jb >> A.mask_shift) & 31)) & 1u) != 0u;
-  };
-  auto tile_marked = [&](int kt) {
-    bool any = false;
-    for (int b = 0; b < NSB; ++b)
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) any = any || marked(k, kt * NSB + b);
-    return any;
-  };
+  // which blocks can hold a positive term for some row of a row group, noted in the first sweep over all keys: bit
+  // 8 (row group) + (block of the tile) of the tile's word
+  static_assert(NSB <= 8, "eight bits a row group");
+  uint32_t* marks = reinterpret_cast<uint32_t*>(smem + 4 * TB);
+  for (int w = threadIdx.x; w < A.mark_words; w += NT) marks[w] = 0u;
+  auto marks_of = [&](int kt) { return (uint32_t)__builtin_amdgcn_readfirstlane(marks[kt >> A.mark_shift]); };
+  auto tile_marked = [&](int kt) { return marks_of(kt) != 0u; };
 
   FragOff<T> koff[NC];
 #pragma unroll
@@ -283,24 +355,18 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqA
   // fn(acc, block of the tile, masked) on the scores of this wave's blocks of the tile that some row of it sees; with `only_marked` of those
   // that are marked
   auto each_block = [&](int kt, const char* tl, bool only_marked, auto fn) {
-    f32x16_t acc[BW];
-    bool act[BW];
-#pragma unroll
+    const uint32_t bits = only_marked ? marks_of(kt) >> (8 * rg) : ~0u;
+#pragma unroll 1
     for (int b = 0; b < BW; ++b) {
       const int sb = ks * BW + b, j0 = kt * KT + sb * 32;
-      act[b] = j0 < q.lim_max && (!only_marked || marked(rg, kt * NSB + sb));
-      if (!act[b]) continue;
-      acc[b] = q.start(j0);
+      if (j0 >= q.lim_max || ((bits >> sb) & 1u) == 0u) continue;
+      f32x16_t acc = q.start(j0);
+      const char* at = tl + sb * 32 * KTile::kRowBytes;
 #pragma unroll
-      for (int cc = 0; cc < NC; ++cc) acc[b] = Elem<T>::mma(koff[cc].load(tl, sb * 32 * KTile::kRowBytes), q.qf[cc], acc[b]);
-    }
-#pragma unroll
-    for (int b = 0; b < BW; ++b) {
-      if (!act[b]) continue;
-      const int sb = ks * BW + b, j0 = kt * KT + sb * 32;
+      for (int cc = 0; cc < NC; ++cc) acc = Elem<T>::mma(koff[cc].load(at, 0), q.qf[cc], acc);
       const bool masked = holes || j0 + 32 > q.lim_min;
-      if (masked) q.mask(acc[b], j0, keys, holes);
-      fn(acc[b], sb, masked);
+      if (masked) q.mask(acc, j0, keys, holes);
+      fn(acc, sb, masked);
     }
   };
   // Exchange between the waves that share the row group's keys (in the tile buffers, which are free between sweeps).
@@ -369,55 +435,54 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqA
   const float lo0 = lo;  // blocks without a term above it are zero for good
 
   // ------------------------------------------------------------ 2. threshold
+  SeqSearch search{tau, lo, hi, 0.f, 0.f, false};
   bool done = !live;
   int iter = 0, more;
-  do {
+  auto sweep = [&](auto first_) {
+    constexpr bool FIRST = decltype(first_)::value;
     const bool wave_on = __ballot(!done) != 0ull;
-    RowSums sums;
-    sums.clear();
-    const bool first = iter == 0;
-    sweep_k([&](int kt) { return first || tile_marked(kt); },
+    SeqSums sums{0.f, 0.f, 0.f};
+    const float t_now = done ? kInf : search.tau;
+    sweep_k([&](int kt) { return FIRST || tile_marked(kt); },
             [&](int kt, const char* tl) {
               if (!wave_on) return;
-              each_block(kt, tl, !first, [&](f32x16_t& acc, int sb, bool masked) {
-                const float lm = max16(acc);
-                if (first) {
+              each_block(kt, tl, !FIRST, [&](f32x16_t& acc, int sb, bool masked) {
+                if (FIRST) {
+                  const float lm = max16(acc);
                   m = fmaxf(m, lm);
                   const bool any = live && lm > -kInf && fmaf(lm, q.a, -lo0) > 0.f;
-                  const int jb = kt * NSB + sb;
-                  if (__ballot(any) != 0ull && lane == 0)
-                    atomicOr(&marks[rg * A.mask_words + (jb >> (A.mask_shift + 5))], 1u << ((jb >> A.mask_shift) & 31));
+                  if (__ballot(any) == 0ull) return;
+                  if (lane == 0) atomicOr(&marks[kt >> A.mark_shift], 1u << (8 * rg + sb));
                 }
-                const bool cand = lm > -kInf && fmaf(lm, q.a, -tau) > 0.f && !done;
-                if (__ballot(cand) == 0ull) return;
-                accumulate_block<AM>(sums, acc, q.a, tau, r, masked);
+                accumulate_keys<AM, FIRST>(sums, acc, q.a, t_now, r);
               });
             });
-    sums.combine_halves();
-    post(f32x4_t{sums.s0, sums.s1, sums.s2, sums.xmin});
-    sums.clear();
+    sums.g += __shfl_xor(sums.g, 32);
+    sums.h += __shfl_xor(sums.h, 32);
+    sums.k += __shfl_xor(sums.k, 32);
+    if (FIRST) m = fmaxf(m, __shfl_xor(m, 32));
+    post(f32x4_t{sums.g, sums.h, sums.k, m});
+    sums = SeqSums{0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       const f32x4_t x = xch[(4 * k + rg) * 64 + lane];
-      sums.s0 += x[0];
-      sums.s1 += x[1];
-      sums.s2 += x[2];
-      sums.xmin = fminf(sums.xmin, x[3]);
+      sums.g += x[0];
+      sums.h += x[1];
+      sums.k += x[2];
+      if (FIRST) m = fmaxf(m, x[3]);
     }
-    if (first && !know_max) {
-      __syncthreads();
-      m = fmaxf(m, __shfl_xor(m, 32));
-      post(f32x4_t{m, 0.f, 0.f, 0.f});
-#pragma unroll
-      for (int k = 0; k < KS; ++k) m = fmaxf(m, xch[(4 * k + rg) * 64 + lane][0]);
+    if (FIRST && !know_max) {
       my = live ? q.a * m : 0.f;
-      lo = fmaxf(lo, my - 1.0f);
-      hi = my - below;
+      search.lo = fmaxf(search.lo, my - 1.0f);
+      search.hi = my - below;
     }
-    if (!done) done = solve_step<AM>(sums, r, tau, lo, hi);
+    if (!done) done = search.step(sums, r, FIRST && (AM == 1 || AM == 3), AM == 2);
     ++iter;
     more = __syncthreads_or(done ? 0 : 1);
-  } while (more && iter < kMaxSolveIters);
+  };
+  sweep(std::true_type());
+  while (more && iter < kMaxSolveIters) sweep(std::false_type());
+  tau = search.tau;
 
   // ------------------------------------------------------------ 3. O^T = V^T P^T
   f32x16_t oacc[NM];
@@ -426,6 +491,7 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqA
     oacc[mm] = f32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   Vals vv;
   vv.init(lane);
+  const float t_out = live ? tau : kInf;
   {
     typename KTile::Pages pk;
     typename VTile::Pages pv;
@@ -456,15 +522,13 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqA
       }
       const char* tl = smem + cur * 2 * TB;
       each_block(t0, tl, true, [&](f32x16_t& acc, int sb, bool masked) {
-        const float lm = max16(acc);
-        const bool cand = live && lm > -kInf && fmaf(lm, q.a, -tau) > 0.f;
-        if (__ballot(cand) == 0ull) return;  // every probability of the block is zero
-        float p[16];
+        float p[16], any = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float x = masked && acc[e] == -kInf ? 0.f : fmaf(acc[e], q.a, -tau);
-          p[e] = live ? pow_r<AM>(fmaxf(x, 0.f), r) : 0.f;
+          p[e] = pow_r<AM>(__builtin_amdgcn_fmed3f(fmaf(acc[e], q.a, -t_out), 0.f, 1.f), r);
+          any = fmaxf(any, p[e]);
         }
+        if (__ballot(any > 0.f) == 0ull) return;  // every probability of the block is zero
         vv.accumulate(tl + TB, sb, p, masked, oacc);
       });
       lds_loads_wait<0>();
