@@ -6,6 +6,7 @@ There is no fallback: if the library is missing, importing this module fails.
 """
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -356,6 +357,7 @@ def scale_proj_bwd(x, wb, wg, beta, gamma, dbeta, dgamma, gamma_scale=1.0, works
 
 
 # ------------------------------------------------- serving: packed sequences, paged cache
+# (A decode step is a few microseconds of GPU work: these functions look at every tensor once, and hand parameters over as packed bytes.)
 
 class SeqParams(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("nseq", "T", "Hq", "Hkv", "D", "dtype", "causal", "scale_layout", "logn_mode",
@@ -373,152 +375,183 @@ class AppendParams(ctypes.Structure):
                                                "vc_stride_h", "vc_stride_n")])
 
 
+_seq_bytes = struct.Struct("@16i2f10q")
+_append_bytes = struct.Struct("@11i4x14q")
+assert _seq_bytes.size == ctypes.sizeof(SeqParams) and _append_bytes.size == ctypes.sizeof(AppendParams)
+
 _lib.entmax_paged_attn_fwd.restype = ctypes.c_int
-_lib.entmax_paged_attn_fwd.argtypes = [ctypes.POINTER(SeqParams)] + [_vp] * 11 + [ctypes.c_size_t, _vp]
+_lib.entmax_paged_attn_fwd.argtypes = [_vp] * 12 + [ctypes.c_size_t, _vp]
 _lib.entmax_packed_attn_fwd.restype = ctypes.c_int
-_lib.entmax_packed_attn_fwd.argtypes = [ctypes.POINTER(SeqParams)] + [_vp] * 9 + [ctypes.c_size_t, _vp]
+_lib.entmax_packed_attn_fwd.argtypes = [_vp] * 10 + [ctypes.c_size_t, _vp]
 _lib.entmax_seq_workspace_bytes.restype = ctypes.c_size_t
-_lib.entmax_seq_workspace_bytes.argtypes = [ctypes.POINTER(SeqParams)]
+_lib.entmax_seq_workspace_bytes.argtypes = [_vp]
 _lib.entmax_cache_append.restype = ctypes.c_int
-_lib.entmax_cache_append.argtypes = [ctypes.POINTER(AppendParams)] + [_vp] * 11
+_lib.entmax_cache_append.argtypes = [_vp] * 12
 
 _DTYPES = {torch.bfloat16: 0, torch.float32: 1}
 
 
-def _rows_of(name, t, ref=None, heads=None):
-    """t is [T, H, D] with a contiguous last dimension, of ref's type and device."""
-    if t.dim() != 3 or (heads is not None and t.shape[1] != heads):
-        raise ValueError("%s must be [T,H,D]%s" % (name, "" if heads is None else " with %d heads" % heads))
+def _rows_of(name, t):
+    """Shape and (token, head) strides of a [T,H,D] tensor.  Strides of dimensions of size one or of empty tensors do not matter: valid ones."""
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError("%s must be [T,H,D]" % name)
+    T, H, D = shape
     if t.dtype not in _DTYPES:
         raise TypeError("%s must be bfloat16 or float32" % name)
-    if t.numel() and t.stride(2) != 1:
+    if T == 0 or H == 0 or D == 0:
+        return T, H, D, H * D, D
+    st, sh, sd = t.stride()
+    if sd != 1:
         raise ValueError("the last dimension of %s must be contiguous" % name)
-    if ref is not None:
-        if t.dtype != ref.dtype or t.device != ref.device:
-            raise TypeError("%s must have the dtype and device of the others" % name)
-        if t.shape[0] != ref.shape[0] or t.shape[2] != ref.shape[2]:
-            raise ValueError("%s must have as many rows and features as the others" % name)
+    if H == 1:
+        sh = D
+    if T == 1:
+        st = (H - 1) * sh + D
+    return T, H, D, st, sh
 
 
-def _cache_of(name, t, ref):
-    if t.dim() != 4 or t.shape[3] != ref.shape[2]:
-        raise ValueError("%s must be [num_pages,Hkv,page_size,D]" % name)
-    if t.dtype != ref.dtype or t.device != ref.device:
+def _like(name, t, ref, T, H, D, t_T, t_H, t_D):
+    if t.dtype != ref.dtype or t.get_device() != ref.get_device():
         raise TypeError("%s must have the dtype and device of the others" % name)
-    if t.numel() and t.stride(3) != 1:
+    if t_T != T or t_H != H or t_D != D:
+        raise ValueError("%s must be [%d,%d,%d]" % (name, T, H, D))
+
+
+def _cache_of(name, t, ref, D):
+    """Shape and (page, head, token) strides of a cache [num_pages,Hkv,page_size,D]."""
+    shape = t.shape
+    if len(shape) != 4 or shape[3] != D:
+        raise ValueError("%s must be [num_pages,Hkv,page_size,D]" % name)
+    if t.dtype != ref.dtype or t.get_device() != ref.get_device():
+        raise TypeError("%s must have the dtype and device of the others" % name)
+    P, H, n, _ = shape
+    if P == 0 or H == 0 or n == 0 or D == 0:
+        return shape, (H * n * D, n * D, D)
+    sp, sh, sn, sd = t.stride()
+    if sd != 1:
         raise ValueError("the last dimension of %s must be contiguous" % name)
+    if n == 1:
+        sn = D
+    if H == 1:
+        sh = n * sn
+    return shape, (H * n * D if P == 1 else sp, sh, sn)
 
 
-def _int_array(name, t, shape, ref):
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != len(shape) or t.device != ref.device or any(
-            w is not None and t.shape[k] != w for k, w in enumerate(shape)):
-        raise ValueError("%s must be a contiguous int32 tensor of shape %s on the device of the others" %
-                         (name, "[%s]" % ", ".join("*" if w is None else str(w) for w in shape)))
+def _int_array(name, t, ref, want):
+    """want: elements, None if any number will do."""
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != ref.get_device() or t.dim() != 1 or (want is not None and t.shape[0] != want):
+        raise ValueError("%s must be a contiguous int32 tensor%s on the device of the others" % (name, "" if want is None else " of %d elements" % want))
 
 
-def _on_gpu(t):
-    if t.device.type != "cuda":
-        raise ValueError("the tensors must be on a GPU")
+def _page_table(t, ref):
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != 2 or t.get_device() != ref.get_device():
+        raise ValueError("page_table must be a contiguous int32 tensor [nseq,max_pages] on the device of the others")
+    return t.shape
 
 
-def _stream_of(t):
-    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+def _floats(name, t, ref, want):
+    if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != want or t.get_device() != ref.get_device():
+        raise ValueError("%s must be a contiguous float32 tensor of shape %s on the device of the others" % (name, want))
 
 
-def _row_strides(t):
-    """(token, head) strides; those of dimensions of size one or of empty tensors do not matter and are made valid ones."""
-    D = t.shape[2]
-    if t.numel() == 0:
-        return t.shape[1] * D, D
-    sh = t.stride(1) if t.shape[1] > 1 else D
-    return (t.stride(0) if t.shape[0] > 1 else max(t.shape[1] * D, (t.shape[1] - 1) * sh + D)), sh
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
-def _cache_strides(t):
-    P, H, n, D = t.shape
-    if t.numel() == 0:
-        return H * n * D, n * D, D
-    sn = t.stride(2) if n > 1 else D
-    sh = t.stride(1) if H > 1 else n * sn
-    return (t.stride(0) if P > 1 else H * n * D), sh, sn
+class _DeviceOf:
+    """The GPU of a tensor as the current one, for calls from another one."""
+
+    def __init__(self, t):
+        if not t.is_cuda:
+            raise ValueError("the tensors must be on a GPU")
+        self.index = t.get_device()
+        self.guard = None if torch._C._cuda_getDevice() == self.index else torch.cuda.device(self.index)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch._C._cuda_getCurrentRawStream(self.index)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
 
 
-def _seq_params(q, Hkv, nseq, max_new, max_keys, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes, bias_mode, path, out):
-    _rows_of("q", q)
-    T, Hq, D = q.shape
+def _seq_params(q, rows, Hkv, nseq, pages, max_new, max_keys, k_strides, v_strides, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes,
+                bias_mode, path, out):
+    T, Hq, D, q_st, q_sh = rows
     if Hkv < 1 or Hq < 1 or Hq % Hkv:
         raise ValueError("the query heads must be a multiple of the key/value heads")
-    if (beta is None) != (gamma is None):
-        raise ValueError("beta and gamma come together")
-    layout = 0 if beta is None else (1 if beta.dim() == 1 else 2)
-    for name, t, want in (("beta", beta, (Hq,) if layout == 1 else (Hq, T)), ("gamma", gamma, (Hq,) if layout == 1 else (Hq, T)),
-                          ("alibi_slopes", alibi_slopes, (Hq,))):
-        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != want or t.device != q.device):
-            raise ValueError("%s must be a contiguous float32 tensor of shape %s on the device of q" % (name, want))
+    layout = 0
+    if beta is not None or gamma is not None:
+        if beta is None or gamma is None:
+            raise ValueError("beta and gamma come together")
+        layout = 1 if beta.dim() == 1 else 2
+        want = (Hq,) if layout == 1 else (Hq, T)
+        _floats("beta", beta, q, want)
+        _floats("gamma", gamma, q, want)
+    if alibi_slopes is not None:
+        _floats("alibi_slopes", alibi_slopes, q, (Hq,))
+    o_st, o_sh = Hq * D, D
     if out is not None:
-        _rows_of("out", out, q, Hq)
-    p = SeqParams(nseq=nseq, T=T, Hq=Hq, Hkv=Hkv, D=D, dtype=_DTYPES[q.dtype], causal=int(bool(causal)), scale_layout=layout,
-                  logn_mode=int(logn_mode), bias_mode=int(bias_mode), path=int(path), max_new=int(max_new), max_keys=int(max_keys),
-                  alpha=float(alpha), delta=float(delta))
-    p.q_stride_t, p.q_stride_h = _row_strides(q)
-    p.o_stride_t, p.o_stride_h = (Hq * D, D) if out is None else _row_strides(out)
-    return p
+        oT, oH, oD, o_st, o_sh = _rows_of("out", out)
+        _like("out", out, q, T, Hq, D, oT, oH, oD)
+    page_size, num_pages, max_pages = pages
+    return _seq_bytes.pack(nseq, T, Hq, Hkv, D, _DTYPES[q.dtype], 1 if causal else 0, layout, logn_mode, bias_mode, path, page_size, num_pages,
+                           max_pages, max_new, max_keys, alpha, delta, q_st, q_sh, o_st, o_sh, *k_strides, *v_strides)
 
 
 def _paged_params(q, k_cache, v_cache, page_table, max_new, max_keys, *args):
-    _cache_of("k_cache", k_cache, q)
-    _cache_of("v_cache", v_cache, q)
-    if v_cache.shape != k_cache.shape:
-        raise ValueError("v_cache must have the shape of k_cache")
-    _int_array("page_table", page_table, (None, None), q)
-    pages, Hkv, page, _ = k_cache.shape
-    most = page_table.shape[1] * page
-    p = _seq_params(q, Hkv, page_table.shape[0], q.shape[0] if max_new is None else max_new, most if max_keys is None else max_keys, *args)
-    p.page_size, p.num_pages, p.max_pages = page, pages, page_table.shape[1]
-    p.k_stride_p, p.k_stride_h, p.k_stride_n = _cache_strides(k_cache)
-    p.v_stride_p, p.v_stride_h, p.v_stride_n = _cache_strides(v_cache)
-    return p
+    rows = _rows_of("q", q)
+    shape, k_strides = _cache_of("k_cache", k_cache, q, rows[2])
+    v_strides = k_strides
+    if v_cache is not k_cache:
+        v_shape, v_strides = _cache_of("v_cache", v_cache, q, rows[2])
+        if v_shape != shape:
+            raise ValueError("v_cache must have the shape of k_cache")
+    nseq, max_pages = _page_table(page_table, q)
+    return nseq, _seq_params(q, rows, shape[1], nseq, (shape[2], shape[0], max_pages), rows[0] if max_new is None else max_new,
+                             max_pages * shape[2] if max_keys is None else max_keys, k_strides, v_strides, *args)
 
 
 def _packed_params(q, k, v, nseq, max_len, *args):
-    _rows_of("q", q)
-    _rows_of("k", k, q)
-    _rows_of("v", v, q, k.shape[1])
-    most = q.shape[0] if max_len is None else max_len
-    p = _seq_params(q, k.shape[1], nseq, most, most, *args)
-    p.k_stride_n, p.k_stride_h = _row_strides(k)
-    p.v_stride_n, p.v_stride_h = _row_strides(v)
-    return p
+    rows = _rows_of("q", q)
+    T, Hkv, D, k_st, k_sh = _rows_of("k", k)
+    _like("k", k, q, rows[0], Hkv, rows[2], T, Hkv, D)
+    v_st, v_sh = k_st, k_sh
+    if v is not k:
+        vT, vH, vD, v_st, v_sh = _rows_of("v", v)
+        _like("v", v, q, T, Hkv, D, vT, vH, vD)
+    most = T if max_len is None else max_len
+    return _seq_params(q, rows, Hkv, nseq, (0, 0, 0), most, most, (0, k_sh, k_st), (0, v_sh, v_st), *args)
 
 
-def _seq_workspace(p, device):
-    return torch.empty(max(int(_lib.entmax_seq_workspace_bytes(ctypes.byref(p))), 256), dtype=torch.uint8, device=device)
+def _seq_workspace(params, device):
+    return torch.empty(max(int(_lib.entmax_seq_workspace_bytes(params)), 256), dtype=torch.uint8, device=device)
+
+
+_DEFAULTS = (1.5, None, None, 1.0, True, 0, None, 0, 0, None)
 
 
 def new_paged_workspace(q, k_cache, page_table, max_new=None, max_keys=None):
     """Workspace for paged_attn_fwd calls of these shapes and bounds, whatever their other arguments."""
-    return _seq_workspace(_paged_params(q, k_cache, k_cache, page_table, max_new, max_keys, 1.5, None, None, 1.0, True, 0, None, 0, 0, None),
-                          q.device)
+    return _seq_workspace(_paged_params(q, k_cache, k_cache, page_table, max_new, max_keys, *_DEFAULTS)[1], q.device)
 
 
 def new_packed_workspace(q, k, cu_seqlens, max_len=None):
     """Workspace for packed_attn_fwd calls of these shapes and bounds, whatever their other arguments."""
-    return _seq_workspace(_packed_params(q, k, k, cu_seqlens.shape[0] - 1, max_len, 1.5, None, None, 1.0, True, 0, None, 0, 0, None), q.device)
+    return _seq_workspace(_packed_params(q, k, k, cu_seqlens.shape[0] - 1, max_len, *_DEFAULTS), q.device)
 
 
-def _seq_call(p, q, out, workspace, call):
-    _on_gpu(q)
-    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != q.device):
+def _outputs(q, params, out, workspace):
+    if out is None:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)  # (rows that no sequence owns)
+    if workspace is None:
+        workspace = _seq_workspace(params, q.device)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != q.get_device():
         raise ValueError("workspace must be a contiguous uint8 tensor on the device of q")
-    with torch.cuda.device(q.device):
-        if out is None:
-            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)  # (rows that no sequence owns)
-        if workspace is None:
-            workspace = _seq_workspace(p, q.device)
-        rc = call(_ptr(out), _ptr(workspace), workspace.numel(), _stream_of(q))
-    if rc != 0:
-        raise EntmaxAttnError(rc)
-    return out
+    return out, workspace
 
 
 def paged_attn_fwd(q, k_cache, v_cache, cu_seqlens, kv_len, page_table, max_new=None, max_keys=None, alpha=1.5, beta=None, gamma=None,
@@ -529,27 +562,36 @@ def paged_attn_fwd(q, k_cache, v_cache, cu_seqlens, kv_len, page_table, max_new=
     max_new, max_keys: bounds that no sequence passes (default: those of the shapes; close ones save workspace and launches).
     beta, gamma: fp32 [Hq] or [Hq,T] or None; alibi_slopes: fp32 [Hq] or None.  Returns out [T,Hq,D]; rows that no sequence owns are left
     as they are (zero in a tensor made here)."""
-    _rows_of("q", q)
-    p = _paged_params(q, k_cache, v_cache, page_table, max_new, max_keys, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes,
-                      bias_mode, path, out)
-    _int_array("cu_seqlens", cu_seqlens, (p.nseq + 1,), q)
-    _int_array("kv_len", kv_len, (p.nseq,), q)
-    return _seq_call(p, q, out, workspace, lambda o, ws, n, st: _lib.entmax_paged_attn_fwd(
-        ctypes.byref(p), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(cu_seqlens), _ptr(kv_len), _ptr(page_table), _ptr(beta), _ptr(gamma),
-        _ptr(alibi_slopes), o, ws, n, st))
+    nseq, p = _paged_params(q, k_cache, v_cache, page_table, max_new, max_keys, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes,
+                            bias_mode, path, out)
+    _int_array("cu_seqlens", cu_seqlens, q, nseq + 1)
+    _int_array("kv_len", kv_len, q, nseq)
+    with _DeviceOf(q) as stream:
+        out, workspace = _outputs(q, p, out, workspace)
+        rc = _lib.entmax_paged_attn_fwd(p, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cu_seqlens.data_ptr(), kv_len.data_ptr(),
+                                        page_table.data_ptr(), _at(beta), _at(gamma), _at(alibi_slopes), out.data_ptr(), workspace.data_ptr(),
+                                        workspace.numel(), stream)
+    if rc != 0:
+        raise EntmaxAttnError(rc)
+    return out
 
 
 def packed_attn_fwd(q, k, v, cu_seqlens, max_len=None, alpha=1.5, beta=None, gamma=None, delta=1.0, causal=True, logn_mode=0,
                     alibi_slopes=None, bias_mode=0, path=0, out=None, workspace=None):
     """Entmax attention of whole prompts: q [T,Hq,D], k, v [T,Hkv,D], sequence s in rows cu_seqlens[s] .. cu_seqlens[s+1]-1.
     max_len: no sequence is longer (default: T).  The other arguments and the result as in paged_attn_fwd."""
-    if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+    _int_array("cu_seqlens", cu_seqlens, q, None)
+    nseq = cu_seqlens.shape[0] - 1
+    if nseq < 0:
         raise ValueError("cu_seqlens must be [nseq + 1]")
-    p = _packed_params(q, k, v, cu_seqlens.shape[0] - 1, max_len, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes, bias_mode, path,
-                       out)
-    _int_array("cu_seqlens", cu_seqlens, (p.nseq + 1,), q)
-    return _seq_call(p, q, out, workspace, lambda o, ws, n, st: _lib.entmax_packed_attn_fwd(
-        ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(beta), _ptr(gamma), _ptr(alibi_slopes), o, ws, n, st))
+    p = _packed_params(q, k, v, nseq, max_len, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes, bias_mode, path, out)
+    with _DeviceOf(q) as stream:
+        out, workspace = _outputs(q, p, out, workspace)
+        rc = _lib.entmax_packed_attn_fwd(p, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(), _at(beta), _at(gamma),
+                                         _at(alibi_slopes), out.data_ptr(), workspace.data_ptr(), workspace.numel(), stream)
+    if rc != 0:
+        raise EntmaxAttnError(rc)
+    return out
 
 
 def cache_append(k, v, k_cache, v_cache, cu_seqlens, kv_len, page_table, q=None, q_out=None, inv_freq=None, interleaved=False):
@@ -557,42 +599,37 @@ def cache_append(k, v, k_cache, v_cache, cu_seqlens, kv_len, page_table, q=None,
     returns the queries q [T,Hq,D] rotated likewise (q_out, which may be q; None without q).
     inv_freq: fp32 [rot / 2], the angle per position of each pair of features; None: no rotation.  interleaved: pairs are neighbouring
     features, else features i and i + rot / 2.  kv_len counts the new tokens.  Other arguments as in paged_attn_fwd."""
-    _rows_of("k", k)
-    _rows_of("v", v, k, k.shape[1])
-    _cache_of("k_cache", k_cache, k)
-    _cache_of("v_cache", v_cache, k)
-    if v_cache.shape != k_cache.shape or k_cache.shape[1] != k.shape[1]:
+    T, Hkv, D, k_st, k_sh = _rows_of("k", k)
+    vT, vH, vD, v_st, v_sh = _rows_of("v", v)
+    _like("v", v, k, T, Hkv, D, vT, vH, vD)
+    shape, kc_strides = _cache_of("k_cache", k_cache, k, D)
+    v_shape, vc_strides = _cache_of("v_cache", v_cache, k, D)
+    if v_shape != shape or shape[1] != Hkv:
         raise ValueError("k_cache and v_cache must be [num_pages,Hkv,page_size,D] with the heads of k")
-    _int_array("page_table", page_table, (None, None), k)
-    nseq = page_table.shape[0]
-    _int_array("cu_seqlens", cu_seqlens, (nseq + 1,), k)
-    _int_array("kv_len", kv_len, (nseq,), k)
-    if q is None and q_out is not None:
-        raise ValueError("q_out without q")
+    nseq, max_pages = _page_table(page_table, k)
+    _int_array("cu_seqlens", cu_seqlens, k, nseq + 1)
+    _int_array("kv_len", kv_len, k, nseq)
+    Hq, q_st, q_sh, qo_st, qo_sh, rot = 0, 0, 0, 0, 0, 0
     if q is not None:
-        _rows_of("q", q, k)
-    if q_out is not None:
-        _rows_of("q_out", q_out, q, q.shape[1])
-    if inv_freq is not None and (inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or inv_freq.dim() != 1 or
-                                 inv_freq.device != k.device):
-        raise ValueError("inv_freq must be a contiguous float32 tensor [rot / 2] on the device of the others")
-    _on_gpu(k)
-    T, Hkv, D = k.shape
-    p = AppendParams(nseq=nseq, T=T, Hq=0 if q is None else q.shape[1], Hkv=Hkv, D=D, dtype=_DTYPES[k.dtype], page_size=k_cache.shape[2],
-                     num_pages=k_cache.shape[0], max_pages=page_table.shape[1], rot=0 if inv_freq is None else 2 * inv_freq.shape[0],
-                     interleaved=int(bool(interleaved)))
-    p.k_stride_t, p.k_stride_h = _row_strides(k)
-    p.v_stride_t, p.v_stride_h = _row_strides(v)
-    p.kc_stride_p, p.kc_stride_h, p.kc_stride_n = _cache_strides(k_cache)
-    p.vc_stride_p, p.vc_stride_h, p.vc_stride_n = _cache_strides(v_cache)
-    with torch.cuda.device(k.device):
-        if q is not None:
-            if q_out is None:
-                q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)  # (rows that no sequence owns)
-            p.q_stride_t, p.q_stride_h = _row_strides(q)
-            p.qo_stride_t, p.qo_stride_h = _row_strides(q_out)
-        rc = _lib.entmax_cache_append(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), _ptr(kv_len), _ptr(page_table),
-                                      _ptr(inv_freq), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream_of(k))
+        qT, Hq, qD, q_st, q_sh = _rows_of("q", q)
+        _like("q", q, k, T, Hq, D, qT, Hq, qD)
+        qo_st, qo_sh = Hq * D, D
+        if q_out is not None:
+            oT, oH, oD, qo_st, qo_sh = _rows_of("q_out", q_out)
+            _like("q_out", q_out, q, T, Hq, D, oT, oH, oD)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if inv_freq is not None:
+        if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or inv_freq.dim() != 1 or inv_freq.get_device() != k.get_device():
+            raise ValueError("inv_freq must be a contiguous float32 tensor [rot / 2] on the device of the others")
+        rot = 2 * inv_freq.shape[0]
+    p = _append_bytes.pack(nseq, T, Hq, Hkv, D, _DTYPES[k.dtype], shape[2], shape[0], max_pages, rot, 1 if interleaved else 0, q_st, q_sh, qo_st,
+                           qo_sh, k_st, k_sh, v_st, v_sh, *kc_strides, *vc_strides)
+    with _DeviceOf(k) as stream:
+        if q is not None and q_out is None:
+            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)  # (rows that no sequence owns)
+        rc = _lib.entmax_cache_append(p, _at(q), k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                                      _at(inv_freq), _at(q_out), k_cache.data_ptr(), v_cache.data_ptr(), stream)
     if rc != 0:
         raise EntmaxAttnError(rc)
     return q_out

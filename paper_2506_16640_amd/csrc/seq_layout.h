@@ -98,11 +98,13 @@ inline int check_append_params(const entmax_append_params* p) {
 constexpr int kSplitRows = 64;
 
 constexpr int kSeqTopWords = 14;  // words that a lane of the sweep leaves
-// Workgroups that share the keys of a group of 128 rows in the sweep of the list kernels
+// Workgroups that share the keys of a group of 128 rows in the sweep of the list kernels: as many as bring the launch to three for
+// every CU, while a share is not shorter than 1024 keys (and the finish kernel can hold what they leave).
+constexpr int kSeqMostSplit = 4;
 inline int seq_ksplit(long long groups, int max_keys) {
-  (void)groups;
-  (void)max_keys;
-  return 1;
+  int n = 1;
+  while (n < kSeqMostSplit && groups * n < 768 && max_keys >= 1024 * (n + 1)) ++n;
+  return n;
 }
 
 struct SeqLayout {
