@@ -232,6 +232,23 @@ struct SeqRows : SeqRow {
     }
     return acc;
   }
+  // S^T of 32 keys whose fragments frag(cc) gives, on top of acc.  fp32: four sums of a quarter of the features each, for the rounding
+  // (sums of 64 products one after the other cost twice the error of the output).
+  template <class F>
+  __device__ __forceinline__ f32x16_t dots(f32x16_t acc, F frag) const {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc) acc = Elem<T>::mma(frag(cc), qf[cc], acc);
+    } else {
+      const f32x16_t zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      f32x16_t part[4] = {zero, zero, zero, zero};
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc) part[cc & 3] = Elem<T>::mma(frag(cc), qf[cc], part[cc & 3]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[e] += (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
+    }
+    return acc;
+  }
   // keys of the block at j0 that the row does not see; with holes, those on pages that are none as well
   __device__ __forceinline__ void mask(f32x16_t& acc, int j0, const SeqKeys& k, bool holes) const {
     const int rel = lim - j0;

@@ -1,8 +1,9 @@
 // Serving attention of sequences with few new tokens (at most kSplitRows folded rows of a key/value head) against any number of keys: the keys, not
 // the rows, are split over the chip, and the bound is reading K once.
 //   seq_scores_kernel  raw scores d of the rows (y = (alpha-1) s = a d) for a piece of the keys, on the matrix cores straight from
-//                      memory, to the workspace -- only the 32-key blocks of a row that hold a score with y of at least (largest so far) - 1: the
-//                      others are zero at the lowest possible threshold.  What was written is noted beside each chunk's maximum (pack_cmax()).
+//                      memory, to the workspace, with the largest of every row and block of 32 keys.  A row's scores of a block are
+//                      written only if y of the largest is at least that of the largest so far less one: the others have no term at the
+//                      lowest possible threshold.  (So whoever knows a row's largest score knows from a block's whether it was written.)
 //   seq_solve_kernel   a workgroup per row: candidates, threshold, and, where they are few, the output from the values of the support
 //   seq_pv_kernel      rows with long supports: O^T = V^T P^T from the scores, keys split again; the last workgroup of a head adds the parts up
 // From the second kernel on y and the threshold are taken relative to the row's largest score (y = a (d - top), tau in [-1, 0)): large scores then cost no
@@ -21,28 +22,25 @@ struct SeqDecodeArgs {
   const void* K;
   const void* V;
   void* O;
-  float* scores;     // [nseq * Hkv][rows][nks]
-  uint32_t* cmax;    // [nseq * Hkv][rows][nchunks]
+  float* scores;     // [nseq * Hkv][rows][32 nblk]
+  float* bmax;       // [nseq * Hkv][rows][nblk] largest score of each 32-key block that starts before the sequence's end
   float* mult;       // [nseq * Hkv][rows] the rows' a
   float2* found;     // [nseq * Hkv][rows] (threshold, or +inf: the row is finished; largest score)
   int* arrived;      // [nseq * Hkv] workgroups of seq_pv_kernel that have left their part
   float* part;       // [nseq * Hkv][pv_splits][rows][D]
   int rows;          // rows of a head there is room for: min(max_new G, kSplitRows)
-  int nks, nchunks;
-  int chunks_per_wg, splits;    // seq_scores_kernel
-  int pv_keys, pv_splits;       // seq_pv_kernel: keys of a workgroup, workgroups of a head
+  int nblk;          // 32-key blocks of max_keys
+  int run, splits;           // seq_scores_kernel: consecutive blocks of a wave, workgroups of a head
+  int pv_keys, pv_splits;    // seq_pv_kernel: keys of a workgroup, workgroups of a head
 };
 
 // How far below the row's largest raw score a key may lie and still have a term at the lowest threshold (a little more, for the rounding)
-__device__ __forceinline__ float score_reach(float a) { return a > 0.f ? 1.00001f / a : kInf; }
+__device__ __forceinline__ float score_reach(float a) { return 1.00001f / a; }
 
 template <typename T, int D, int NQB>
 __global__ __launch_bounds__(kThreads) void seq_scores_kernel(SeqDecodeArgs A) {
   constexpr int NC = D / 16;
-  constexpr int kBlocksPerChunk = kDecodeChunk / 32;
-  __shared__ int rowmax[NQB * 32];                             // ordered_bits() of a row's largest score so far
-  __shared__ float wmax[kDecodeMfmaChunks][kWaves][NQB * 32];  // per chunk: what each wave saw and wrote
-  __shared__ uint32_t wmask[kDecodeMfmaChunks][kWaves][NQB * 32];
+  __shared__ int rowmax[NQB * 32];  // ordered_bits() of a row's largest score so far
   const SeqGeom& g = A.g;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, hh = lane >> 5;
   const int split = blockIdx.x % A.splits, s = blockIdx.x / A.splits, hk = blockIdx.y;
@@ -50,58 +48,49 @@ __global__ __launch_bounds__(kThreads) void seq_scores_kernel(SeqDecodeArgs A) {
   if (split == 0 && tid == 0) A.arrived[head] = 0;
   SeqView v;
   if (!load_seq(g, s, v) || !split_seq(g, v)) return;
-  const int chunk0 = split * A.chunks_per_wg, jc0 = chunk0 * kDecodeChunk;
-  if (jc0 >= v.L) return;
-  const int nblk = min(A.chunks_per_wg * kBlocksPerChunk, (v.L - jc0 + 31) >> 5);  // 32-key blocks of this workgroup
+  if (split * kWaves * A.run * 32 >= v.L) return;
+  const int blk0 = (split * kWaves + wave) * A.run, end = min(blk0 + A.run, (v.L + 31) >> 5);  // this wave's blocks (there may be none)
   SeqKeys keys;
   keys.init(g, v, A.K, hk, false, sizeof(T));
-  auto page_of = [&](int blk) { return keys.page(min(jc0 + blk * 32 + li, v.L - 1)); };
+  auto page_of = [&](int blk) { return keys.page(min(blk * 32 + li, v.L - 1)); };
   Frag<T> kf[NC], kn[NC];
   auto fetch = [&](Frag<T>* dst, int blk, int pg) {  // (rows past the end repeat the last one; their scores are masked)
-    const char* row = keys.row_in(pg, min(jc0 + blk * 32 + li, v.L - 1)) + 8 * hh * sizeof(T);
+    const char* row = keys.row_in(pg, min(blk * 32 + li, v.L - 1)) + 8 * hh * sizeof(T);
 #pragma unroll
     for (int cc = 0; cc < NC; ++cc) dst[cc] = Elem<T>::load(row + 16 * cc * sizeof(T));
   };
-  int pg = 0, pg_next = 0;  // pages of the blocks in kn and of those after them
-  if (wave < nblk) {
-    pg = page_of(wave);
-    if (wave + kWaves < nblk) pg_next = page_of(wave + kWaves);
-    fetch(kn, wave, pg);
+  int pg = 0, pg_next = 0;  // pages of the block in kn and of the one after it
+  if (blk0 < end) {
+    pg = page_of(blk0);
+    pg_next = page_of(min(blk0 + 1, end - 1));
+    fetch(kn, blk0, pg);
   }
   const int R = v.n * g.G;
   SeqRows<T, D> q[NQB];
-  float top[NQB], cm[NQB], reach[NQB];
-  uint32_t mask[NQB];
+  float top[NQB], reach[NQB];
 #pragma unroll
   for (int qb = 0; qb < NQB; ++qb) {
     q[qb].init(g, v, A.Q, hk, qb * 32);
-    top[qb] = cm[qb] = -kInf;
-    mask[qb] = 0u;
+    top[qb] = -kInf;
     reach[qb] = score_reach(q[qb].a);
     if (split == 0 && wave == 0 && hh == 0 && q[qb].valid) A.mult[(long long)head * A.rows + qb * 32 + li] = q[qb].a;
   }
   if (tid < NQB * 32) rowmax[tid] = ordered_bits(-kInf);
-  for (int e = tid; e < kDecodeMfmaChunks * kWaves * NQB * 32; e += kThreads) {
-    (&wmax[0][0][0])[e] = -kInf;
-    (&wmask[0][0][0])[e] = 0u;
-  }
   __syncthreads();
-  for (int blk = wave; blk < nblk; blk += kWaves) {
+  for (int blk = blk0; blk < end; ++blk) {
 #pragma unroll
     for (int cc = 0; cc < NC; ++cc) kf[cc] = kn[cc];
     const uint32_t holes = (uint32_t)__ballot(keys.is_hole(pg));  // of the block's 32 keys
-    if (blk + kWaves < nblk) {
+    if (blk + 1 < end) {
       pg = pg_next;
-      if (blk + 2 * kWaves < nblk) pg_next = page_of(blk + 2 * kWaves);
-      fetch(kn, blk + kWaves, pg);
+      pg_next = page_of(min(blk + 2, end - 1));
+      fetch(kn, blk + 1, pg);
     }
-    const int j0 = jc0 + blk * 32;
+    const int j0 = blk * 32;
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
       if (qb * 32 >= R) break;
-      f32x16_t acc = q[qb].start(j0);
-#pragma unroll
-      for (int cc = 0; cc < NC; ++cc) acc = Elem<T>::mma(kf[cc], q[qb].qf[cc], acc);
+      f32x16_t acc = q[qb].dots(q[qb].start(j0), [&](int cc) { return kf[cc]; });
       if (j0 + 32 > q[qb].lim_min || holes != 0u) {
         const int rel = q[qb].lim - j0;
 #pragma unroll
@@ -112,7 +101,8 @@ __global__ __launch_bounds__(kThreads) void seq_scores_kernel(SeqDecodeArgs A) {
       }
       float m = max16(acc);
       m = fmaxf(m, __shfl_xor(m, 32));
-      cm[qb] = fmaxf(cm[qb], m);
+      const long long row = (long long)head * A.rows + qb * 32 + li;
+      if (hh == 0 && q[qb].valid) A.bmax[row * A.nblk + blk] = m;
       // (an older value only writes more)
       top[qb] = fmaxf(top[qb], from_ordered_bits(__hip_atomic_load(&rowmax[qb * 32 + li], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)));
       // (m = -inf for rows that see none of the block; the row's first lane decides for both)
@@ -122,34 +112,12 @@ __global__ __launch_bounds__(kThreads) void seq_scores_kernel(SeqDecodeArgs A) {
           top[qb] = m;
           atomicMax(&rowmax[qb * 32 + li], ordered_bits(m));
         }
-        mask[qb] |= 1u << (blk % kBlocksPerChunk);
-        float* dst = A.scores + ((long long)head * A.rows + qb * 32 + li) * A.nks + j0 + 4 * hh;  // (nks: a multiple of 32)
+        float* dst = A.scores + (row * A.nblk + blk) * 32 + 4 * hh;
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4)
           *reinterpret_cast<f32x4_t*>(dst + 8 * q4) = f32x4_t{acc[4 * q4], acc[4 * q4 + 1], acc[4 * q4 + 2], acc[4 * q4 + 3]};
       }
-      if (blk % kBlocksPerChunk + kWaves >= kBlocksPerChunk || blk + kWaves >= nblk) {  // this wave's last block of the chunk
-        if (hh == 0) {
-          wmax[blk / kBlocksPerChunk][wave][qb * 32 + li] = cm[qb];
-          wmask[blk / kBlocksPerChunk][wave][qb * 32 + li] = mask[qb];
-        }
-        cm[qb] = -kInf;
-        mask[qb] = 0u;
-      }
     }
-  }
-  __syncthreads();
-  for (int e = tid; e < A.chunks_per_wg * NQB * 32; e += kThreads) {
-    const int c = e / (NQB * 32), i = e % (NQB * 32);
-    if (i >= R || c * kBlocksPerChunk >= nblk) continue;
-    float mx = wmax[c][0][i];
-    uint32_t mk = wmask[c][0][i];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
-      mx = fmaxf(mx, wmax[c][w][i]);
-      mk |= wmask[c][w][i];
-    }
-    A.cmax[((long long)head * A.rows + i) * A.nchunks + chunk0 + c] = pack_cmax(mx, mk);
   }
 }
 
@@ -183,6 +151,7 @@ __device__ __forceinline__ RowSums block_sums(RowSums s, float* buf, int parity)
 
 constexpr int kSolveThreads = 512;
 constexpr int kSolveList = 512;   // candidates kept in LDS, their output gathered here; rows with more are left to seq_pv_kernel
+constexpr int kSolveHeld = 16;    // scores of a long row that a thread holds in registers
 
 template <typename T, int D, int AM>
 __global__ __launch_bounds__(kSolveThreads) void seq_solve_kernel(SeqDecodeArgs A) {
@@ -191,7 +160,7 @@ __global__ __launch_bounds__(kSolveThreads) void seq_solve_kernel(SeqDecodeArgs 
   constexpr int kGroups = NT / LR;
   __shared__ float2 list[kSolveList];          // (key index bits, raw score, then y)
   __shared__ __attribute__((aligned(16))) float red[2 * kW * 4];
-  __shared__ float wmax[kW], wtop[kW];
+  __shared__ float wtop[kW];
   __shared__ int count;
   __shared__ float osum[kW * D];
   const SeqGeom& g = A.g;
@@ -203,79 +172,68 @@ __global__ __launch_bounds__(kSolveThreads) void seq_solve_kernel(SeqDecodeArgs 
   const int lim = g.causal ? max(0, min(v.L - v.n + t + 1, v.L)) : v.L;
   const long long at = (long long)head * A.rows + row;
   T* o = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + t) * g.o_st + (long long)qh * g.o_sh;
-  float* d = A.scores + at * A.nks;
+  const float* d = A.scores + at * A.nblk * 32;
+  const float* bmax = A.bmax + at * A.nblk;
+  const int nblk = (v.L + 31) >> 5;
   const float a = A.mult[at], reach = score_reach(a);
-  const uint32_t* cmax = A.cmax + at * A.nchunks;
-  const int nchunks = (v.L + kDecodeChunk - 1) / kDecodeChunk;
   const float r = 1.0f / (g.alpha - 1.0f);
   SeqKeys vals;
   vals.init(g, v, A.V, hk, true, sizeof(T));
-  // lower bound of the largest score from the chunks' rounded maxima
-  uint32_t first_words = kCmaxNone;  // the words of chunks 0..63: every wave's own copy
-  if (lane < nchunks) first_words = cmax[lane];
-  float m = cmax_floor(first_words);
-  for (int c = 64 + tid; c < nchunks; c += NT) m = fmaxf(m, cmax_floor(cmax[c]));
+  // the largest score from the blocks' (the first NT of them are held)
+  const float first = tid < nblk ? bmax[tid] : -kInf;
+  float top = first;
+  for (int b = tid + NT; b < nblk; b += NT) top = fmaxf(top, bmax[b]);
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-  if (lane == 0) wmax[wave] = m;
+  for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+  if (lane == 0) wtop[wave] = top;
   if (tid == 0) count = 0;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kW; ++w) m = fmaxf(m, wmax[w]);
-  if (lim == 0 || m == -kInf) {  // no visible key: an empty sum
+  for (int w = 0; w < kW; ++w) top = fmaxf(top, wtop[w]);
+  if (lim == 0 || top == -kInf) {  // no visible key: an empty sum
     if (tid < D) Elem<T>::store(o, tid, 0.f);
     if (tid == 0) A.found[at] = make_float2(kInf, 0.f);
     return;
   }
-  const float floor_lo = m - reach;
-  // body(first key + 4 * lane, was it written) for the chunks whose word is `wanted`, twice 256 keys each
-  auto each_chunk = [&](auto wanted, auto body) {
-    int turn = 0;
-    for (int c0 = 0; c0 < nchunks; c0 += 64) {
-      const uint32_t word = c0 == 0 ? first_words : (c0 + lane < nchunks ? cmax[c0 + lane] : kCmaxNone);
-      unsigned long long hot = __ballot(c0 + lane < nchunks && wanted(word));
-      while (hot != 0ull) {
-        const int k = __builtin_ctzll(hot);
-        hot &= hot - 1ull;
-        if ((turn++ % kW) != wave) continue;
-        const uint32_t written = (uint32_t)__builtin_amdgcn_readlane((int)word, k);
+  const float floor_lo = top - reach;  // (at most top, which is always a candidate)
+  auto hot = [&](float m) { return m >= floor_lo && m > -kInf; };
+  // the candidates: two blocks of a wave at a time, half a wave each, and two such pairs under way; a row with more than the list holds is
+  // counted no further
+  for (int b0 = 0; b0 < nblk; b0 += NT) {
+    const int b = b0 + tid;
+    const float m = b0 == 0 ? first : (b < nblk ? bmax[b] : -kInf);
+    unsigned long long todo = __ballot(b < nblk && hot(m));
+    while (todo != 0ull) {
+      if (__hip_atomic_load(&count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > kSolveList) break;
+      int mine[2];
+      float x[2];
 #pragma unroll
-        for (int u = 0; u < kDecodeChunk / 256; ++u) {
-          const int in_chunk = (u * 64 + lane) * 4;
-          body((c0 + k) * kDecodeChunk + in_chunk, ((written >> (in_chunk >> 5)) & 1u) != 0u);
-        }
+      for (int u = 0; u < 2; ++u) {
+        const int k0 = todo != 0ull ? __builtin_ctzll(todo) : -1;
+        todo &= todo - 1ull;  // (0 stays 0)
+        const int k1 = todo != 0ull ? __builtin_ctzll(todo) : -1;
+        todo &= todo - 1ull;
+        mine[u] = lane < 32 ? k0 : k1;
+        x[u] = mine[u] >= 0 ? d[(b0 + wave * 64 + mine[u]) * 32 + (lane & 31)] : -kInf;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bool in = hot(x[u]);
+        const unsigned long long all = __ballot(in);
+        if (all == 0ull) continue;
+        int pos = 0;
+        if (lane == 0) pos = atomicAdd(&count, (int)__popcll(all));
+        pos = __builtin_amdgcn_readfirstlane(pos) +
+              (int)__builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u));
+        if (in && pos < kSolveList) list[pos] = make_float2(__int_as_float((b0 + wave * 64 + mine[u]) * 32 + (lane & 31)), x[u]);
       }
     }
-  };
-  float top = -kInf;  // the largest score itself
-  each_chunk([&](uint32_t word) { return (word & 0xffffu) != 0u && cmax_ceil(word) >= floor_lo; },
-             [&](int j, bool written) {
-               // (what was written is masked where the row does not see it, and whole blocks)
-               f32x4_t x = {-kInf, -kInf, -kInf, -kInf};
-               if (written) x = *reinterpret_cast<const f32x4_t*>(d + j);
-#pragma unroll
-               for (int k = 0; k < 4; ++k) {
-                 const bool in = x[k] >= floor_lo && x[k] > -kInf;
-                 top = fmaxf(top, x[k]);
-                 const unsigned long long all = __ballot(in);
-                 if (all == 0ull) continue;
-                 int pos = 0;
-                 if (lane == 0) pos = atomicAdd(&count, (int)__popcll(all));
-                 pos = __builtin_amdgcn_readfirstlane(pos) +
-                       (int)__builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u));
-                 if (in && pos < kSolveList) list[pos] = make_float2(__int_as_float(j + k), x[k]);
-               }
-             });
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-  if (lane == 0) wtop[wave] = top;
+  }
   __syncthreads();
   const int total = count;
-#pragma unroll
-  for (int w = 0; w < kW; ++w) top = fmaxf(top, wtop[w]);
   // y = a (d - top) in [-1, 0]: the threshold lies between -1 and -n^(1-alpha)
   float lo = -1.0f, hi = -__builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)lim)), tau = lo;
-  auto y_of = [&](float x) { return x > -kInf ? a * (x - top) : -kInf; };
+  auto y_of = [&](float x) { return a * (x - top); };
   // features of this lane of the value row of key j, times p
   auto add_row = [&](int j, float p, float (&acc)[E]) {
     const u32x4_t w = *reinterpret_cast<const u32x4_t*>(vals.row(j) + (lane % LR) * 16);
@@ -389,30 +347,47 @@ __global__ __launch_bounds__(kSolveThreads) void seq_solve_kernel(SeqDecodeArgs 
     if (tid == 0) A.found[at] = make_float2(kInf, 0.f);
     return;
   }
-  // long supports: the row itself is read again and again, the blocks that were not written become -inf once and for all
-  each_chunk([&](uint32_t word) { return (word & 0xffffu) != 0xffffu; },
-             [&](int j, bool written) {
-               if (j < ((v.L + 31) & ~31) && !written) *reinterpret_cast<f32x4_t*>(d + j) = f32x4_t{-kInf, -kInf, -kInf, -kInf};
-             });
-  __syncthreads();
+  // Long supports.  Key e of the row counts if its block was written; -inf (y far below -1) else.  The first kSolveHeld NT of them are read once.
+  const int n = nblk * 32;
+  auto y_at = [&](int e) { return e < n && hot(bmax[e >> 5]) ? y_of(d[e]) : -kInf; };
+  float held[kSolveHeld];
+#pragma unroll
+  for (int k = 0; k < kSolveHeld; ++k) held[k] = y_at(tid + k * NT);
+  auto each = [&](auto fn) {
+#pragma unroll
+    for (int k = 0; k < kSolveHeld; ++k) fn(held[k]);
+    for (int e = tid + kSolveHeld * NT; e < n; e += 4 * NT) {
+      float y[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) y[u] = y_at(e + u * NT);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) fn(y[u]);
+    }
+  };
   {
-    // starting point from the row's mean and deviation (gauss_start())
+    // starting point from the mean and deviation of a row all of whose blocks were written (gauss_start())
     RowSums st;
     st.clear();
-    for (int e = tid; e < lim; e += NT) {
-      const float x = y_of(d[e]);
-      if (x > -kInf) {
+    each([&](float y) {
+      if (y > -kInf) {
         st.s0 += 1.f;
-        st.s1 += x;
-        st.s2 = fmaf(x, x, st.s2);
+        st.s1 += y;
+        st.s2 = fmaf(y, y, st.s2);
       }
-    }
+    });
     st = block_sums<NT>(st, red, 1);
     const float mean = st.s1 / st.s0, var = st.s2 / st.s0 - mean * mean;
     float t0;
     if (st.s0 == (float)lim && var > 0.f && gauss_start<AM>(mean, sqrtf(var), st.s0, t0)) tau = fminf(fmaxf(t0, lo), hi);
   }
-  solve([&](int e) { return y_of(d[e]); }, lim);
+  bool done = false;
+  for (int it = 0; !done && it < kMaxSolveIters; ++it) {
+    RowSums sums;
+    sums.clear();
+    each([&](float y) { accumulate<AM>(sums, y - tau, r); });
+    sums = block_sums<NT>(sums, red, it & 1);
+    done = solve_step<AM>(sums, r, tau, lo, hi);
+  }
   if (tid == 0) A.found[at] = make_float2(tau, top);
 }
 
@@ -448,7 +423,7 @@ __global__ __launch_bounds__(kThreads) void seq_pv_kernel(SeqDecodeArgs A) {
     const int row = qb * 32 + li;
     const long long at = (long long)head * A.rows + row;
     const float2 f = row < R ? A.found[at] : make_float2(kInf, 0.f);
-    a[qb] = row < R ? A.mult[at] : 0.f;
+    a[qb] = row < R ? A.mult[at] : 1.f;
     tau[qb] = f.x;
     top[qb] = f.y;
     left[qb] = tau[qb] < kInf;
@@ -480,20 +455,36 @@ __global__ __launch_bounds__(kThreads) void seq_pv_kernel(SeqDecodeArgs A) {
   constexpr int CPR = VT::kCpr, RW = VT::RW, L = KT / RW;
   u32x4_t stage[L];
   f32x4_t ys[NQB][4];
+  int pages[L];       // of the block after the one that is fetched next
+  float best[NQB];    // its largest score of this lane's row
+  auto ask = [&](int blk) {
+    const int j0 = from + min(blk, nblk - 1) * 32;
+#pragma unroll
+    for (int it = 0; it < L; ++it) pages[it] = vals.page(min(j0 + it * RW + lane / CPR, v.L - 1));
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb)
+      best[qb] = left[qb] ? A.bmax[((long long)head * A.rows + qb * 32 + li) * A.nblk + (j0 >> 5)] : -kInf;
+  };
   auto fetch = [&](int blk) {
     const int j0 = from + blk * 32;
 #pragma unroll
     for (int it = 0; it < L; ++it)
-      stage[it] = *reinterpret_cast<const u32x4_t*>(vals.row(min(j0 + it * RW + lane / CPR, v.L - 1)) + (lane % CPR) * 16);
+      stage[it] = *reinterpret_cast<const u32x4_t*>(vals.row_in(pages[it], min(j0 + it * RW + lane / CPR, v.L - 1)) + (lane % CPR) * 16);
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
       if (qb * 32 >= R) break;
-      const float* y = A.scores + ((long long)head * A.rows + min(qb * 32 + li, R - 1)) * A.nks + j0 + 4 * hh;
+      // (what was not written has no term)
+      const bool there = best[qb] > -kInf && best[qb] >= top[qb] - score_reach(a[qb]);
+      const float* y = A.scores + (((long long)head * A.rows + qb * 32 + li) * A.nblk + (j0 >> 5)) * 32 + 4 * hh;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) ys[qb][k] = *reinterpret_cast<const f32x4_t*>(y + 8 * k);
+      for (int k = 0; k < 4; ++k) ys[qb][k] = there ? *reinterpret_cast<const f32x4_t*>(y + 8 * k) : f32x4_t{-kInf, -kInf, -kInf, -kInf};
     }
   };
-  if (wave < nblk) fetch(wave);
+  if (wave < nblk) {
+    ask(wave);
+    fetch(wave);
+    ask(wave + kWaves);
+  }
   for (int blk = wave; blk < nblk; blk += kWaves) {
     __builtin_amdgcn_wave_barrier();  // (the tile is the wave's own: LDS operations of a wave are in order)
 #pragma unroll
@@ -509,10 +500,13 @@ __global__ __launch_bounds__(kThreads) void seq_pv_kernel(SeqDecodeArgs A) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float x = fmaf(a[qb], ys[qb][e >> 2][e & 3] - top[qb], -tau[qb]);
-        p[qb][e] = left[qb] && ys[qb][e >> 2][e & 3] > -kInf ? pow_r<AM>(fmaxf(x, 0.f), r) : 0.f;
+        p[qb][e] = left[qb] ? pow_r<AM>(fmaxf(x, 0.f), r) : 0.f;
       }
     }
-    if (blk + kWaves < nblk) fetch(blk + kWaves);
+    if (blk + kWaves < nblk) {
+      fetch(blk + kWaves);
+      ask(blk + 2 * kWaves);
+    }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
@@ -558,6 +552,7 @@ __global__ __launch_bounds__(kThreads) void seq_pv_kernel(SeqDecodeArgs A) {
     const int row = e / (D / 4), f = (e % (D / 4)) * 4;
     if (!(A.found[(long long)head * A.rows + row].x < kInf)) continue;
     f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int k = 0; k < parts; ++k) {
       const f32x4_t x = *reinterpret_cast<const f32x4_t*>(all + ((long long)k * A.rows + row) * D + f);
 #pragma unroll

@@ -67,7 +67,7 @@ inline int check_seq_params(const entmax_seq_params* p) {
   if (p->o_stride_t < p->D || (p->Hq > 1 && p->o_stride_h < p->D)) return ENTMAX_ATTN_INVALID_ARG;
   if (seq_blocks(p->nseq, p->T, p->Hq / p->Hkv) * p->Hkv * 4 > kSeqMostBlocks) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
   // (launches of the kernels that split the keys: workgroups of the value kernel, of one piece of the keys each; workgroups of rows)
-  if (!packed && ((long long)p->nseq * p->Hkv * (ceil_div(p->max_keys, kDecodeChunk) + 1) > kSeqMostBlocks ||
+  if (!packed && ((long long)p->nseq * p->Hkv * (ceil_div(p->max_keys, kWaves * 32) + 1) > kSeqMostBlocks ||
                   (long long)p->nseq * p->Hkv * 64 > kSeqMostBlocks / 2))
     return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
   return ENTMAX_ATTN_OK;
@@ -107,18 +107,26 @@ inline int seq_ksplit(long long groups, int max_keys) {
   return n;
 }
 
+// Blocks of a wave of the score kernel: up to eight, while the launch has at least 2048 workgroups of the longest sequence's size (most
+// are shorter); with many rows more, so that they know a large score sooner and write fewer of the others.
+inline int seq_run(long long heads, int nblk, int rows) {
+  int n = rows > 16 ? 4 : 1;
+  while (n < 8 && heads * ceil_div(nblk, kWaves * 2 * n) >= 2048) n *= 2;
+  return n;
+}
+
 struct SeqLayout {
   bool split;       // the call may hold such sequences
   bool blocks;      // it may hold others
   size_t off_scores;
   int rows;         // rows of a head in the score buffer
-  int nks, nchunks; // scores and chunks of a row
-  int chunks_per_wg, splits;  // of the score kernel
+  int nblk;         // 32-key blocks of a row
+  int run, splits;  // of the score kernel: blocks of a wave, workgroups of a head
   int pv_keys, pv_splits;     // of the value kernel
   bool lists;       // groups of 128 rows go through the list kernels first
   int ksplit;       // workgroups that share the keys of a group in their sweep
   size_t off_blocks, off_votes, off_dense, off_bounds, off_tops;
-  size_t off_cmax, off_mult, off_found, off_arrived, off_part, total;
+  size_t off_bmax, off_mult, off_found, off_arrived, off_part, total;
 };
 
 inline SeqLayout make_seq_layout(const entmax_seq_params* p) {
@@ -147,16 +155,15 @@ inline SeqLayout make_seq_layout(const entmax_seq_params* p) {
     L.off_scores = o;
     const long long heads = (long long)p->nseq * p->Hkv;
     L.rows = (int)(most_rows < kSplitRows ? most_rows : kSplitRows);
-    L.nks = ceil_div(p->max_keys, 32) * 32;
-    L.nchunks = ceil_div(p->max_keys, kDecodeChunk);
-    L.chunks_per_wg = decode_chunks_per_wg(heads, L.nchunks);
-    L.splits = ceil_div(L.nchunks, L.chunks_per_wg);
-    L.pv_keys = 1024;
+    L.nblk = ceil_div(p->max_keys, 32);
+    L.run = seq_run(heads, L.nblk, L.rows);
+    L.splits = ceil_div(L.nblk, kWaves * L.run);
+    L.pv_keys = 512;
     L.pv_splits = ceil_div(p->max_keys, L.pv_keys);
     const size_t rows = (size_t)heads * L.rows;
-    o += align_up(rows * L.nks * sizeof(float));
-    L.off_cmax = o;
-    o += align_up(rows * L.nchunks * sizeof(uint32_t));
+    o += align_up(rows * L.nblk * 32 * sizeof(float));
+    L.off_bmax = o;
+    o += align_up(rows * L.nblk * sizeof(float));
     L.off_mult = o;
     o += align_up(rows * sizeof(float));
     L.off_found = o;

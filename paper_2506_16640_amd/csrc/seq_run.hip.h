@@ -148,15 +148,14 @@ int run_seq(const SeqCall& c) {
   d.V = c.V;
   d.O = c.O;
   d.scores = reinterpret_cast<float*>(c.ws + L.off_scores);
-  d.cmax = reinterpret_cast<uint32_t*>(c.ws + L.off_cmax);
+  d.bmax = reinterpret_cast<float*>(c.ws + L.off_bmax);
   d.mult = reinterpret_cast<float*>(c.ws + L.off_mult);
   d.found = reinterpret_cast<float2*>(c.ws + L.off_found);
   d.arrived = reinterpret_cast<int*>(c.ws + L.off_arrived);
   d.part = reinterpret_cast<float*>(c.ws + L.off_part);
   d.rows = L.rows;
-  d.nks = L.nks;
-  d.nchunks = L.nchunks;
-  d.chunks_per_wg = L.chunks_per_wg;
+  d.nblk = L.nblk;
+  d.run = L.run;
   d.splits = L.splits;
   d.pv_keys = L.pv_keys;
   d.pv_splits = L.pv_splits;

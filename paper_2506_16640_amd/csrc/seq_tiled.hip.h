@@ -360,10 +360,8 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqA
     for (int b = 0; b < BW; ++b) {
       const int sb = ks * BW + b, j0 = kt * KT + sb * 32;
       if (j0 >= q.lim_max || ((bits >> sb) & 1u) == 0u) continue;
-      f32x16_t acc = q.start(j0);
       const char* at = tl + sb * 32 * KTile::kRowBytes;
-#pragma unroll
-      for (int cc = 0; cc < NC; ++cc) acc = Elem<T>::mma(koff[cc].load(at, 0), q.qf[cc], acc);
+      f32x16_t acc = q.dots(q.start(j0), [&](int cc) { return koff[cc].load(at, 0); });
       const bool masked = holes || j0 + 32 > q.lim_min;
       if (masked) q.mask(acc, j0, keys, holes);
       fn(acc, sb, masked);
