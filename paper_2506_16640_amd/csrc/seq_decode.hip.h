@@ -149,26 +149,30 @@ __device__ __forceinline__ RowSums block_sums(RowSums s, float* buf, int parity)
   return t;
 }
 
-constexpr int kSolveThreads = 512;
-constexpr int kSolveList = 512;   // candidates kept in LDS, their output gathered here; rows with more are left to seq_pv_kernel
+constexpr int kSolveList = 256;   // candidates kept in LDS, their output gathered here; rows with more are left to seq_pv_kernel
 constexpr int kSolveHeld = 16;    // scores of a long row that a thread holds in registers
 
-template <typename T, int D, int AM>
-__global__ __launch_bounds__(kSolveThreads) void seq_solve_kernel(SeqDecodeArgs A) {
-  constexpr int NT = kSolveThreads, kW = NT / 64;
+template <typename T, int D, int NT>
+struct SolveLds {
+  static constexpr int kW = NT / 64;
+  float2 list[kSolveList];  // (key index bits, raw score, then y)
+  __attribute__((aligned(16))) float red[2 * kW * 4];
+  float wtop[kW];
+  int count;
+  float osum[kW * D];
+};
+
+template <typename T, int D, int AM, int NT>
+__device__ __forceinline__ void solve_row(const SeqDecodeArgs& A, SolveLds<T, D, NT>& lds, const SeqView& v, int head, int row) {
+  constexpr int kW = NT / 64;
   constexpr int E = 16 / (int)sizeof(T), LR = D / E;  // features of a lane, lanes of a value row
   constexpr int kGroups = NT / LR;
-  __shared__ float2 list[kSolveList];          // (key index bits, raw score, then y)
-  __shared__ __attribute__((aligned(16))) float red[2 * kW * 4];
-  __shared__ float wtop[kW];
-  __shared__ int count;
-  __shared__ float osum[kW * D];
+  float2* list = lds.list;
+  float *red = lds.red, *wtop = lds.wtop, *osum = lds.osum;
+  int& count = lds.count;
   const SeqGeom& g = A.g;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int row = blockIdx.x % A.rows, head = blockIdx.x / A.rows, hk = head % g.Hkv, s = head / g.Hkv;
-  SeqView v;
-  if (!load_seq(g, s, v) || !split_seq(g, v) || row >= v.n * g.G) return;
-  const int t = row / g.G, qh = hk * g.G + row % g.G;
+  const int hk = head % g.Hkv, t = row / g.G, qh = hk * g.G + row % g.G;
   const int lim = g.causal ? max(0, min(v.L - v.n + t + 1, v.L)) : v.L;
   const long long at = (long long)head * A.rows + row;
   T* o = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + t) * g.o_st + (long long)qh * g.o_sh;
@@ -391,12 +395,45 @@ __global__ __launch_bounds__(kSolveThreads) void seq_solve_kernel(SeqDecodeArgs 
   if (tid == 0) A.found[at] = make_float2(tau, top);
 }
 
+// NT: threads of a workgroup.  It takes the rows blockIdx.x % stride, + stride, .. of a head (one, but where few sequences of many have many rows).
+template <typename T, int D, int AM, int NT>
+__global__ __launch_bounds__(NT) void seq_solve_kernel(SeqDecodeArgs A, int stride) {
+  __shared__ SolveLds<T, D, NT> lds;
+  const int head = blockIdx.x / stride, s = head / A.g.Hkv;
+  SeqView v;
+  if (!load_seq(A.g, s, v) || !split_seq(A.g, v)) return;
+  for (int row = blockIdx.x % stride; row < v.n * A.g.G; row += stride) {
+    solve_row<T, D, AM, NT>(A, lds, v, head, row);
+    __syncthreads();
+  }
+}
+
 // Keys of a wave's tile and bytes of LDS for it: two tiles of V per wave
 template <typename T, int D>
 struct SeqPvCfg {
   static constexpr int KT = 32;
   static constexpr int kTileBytes = KT * D * (int)sizeof(T);
 };
+
+// four floats to and from memory at agent scope
+__device__ __forceinline__ void put_part(float* at, const f32x4_t& x) {
+  unsigned long long* p = reinterpret_cast<unsigned long long*>(at);
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    __hip_atomic_store(p + k, (unsigned long long)__float_as_uint(x[2 * k]) | (unsigned long long)__float_as_uint(x[2 * k + 1]) << 32, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x4_t get_part(const float* at) {
+  const unsigned long long* p = reinterpret_cast<const unsigned long long*>(at);
+  f32x4_t x;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const unsigned long long v = __hip_atomic_load(p + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    x[2 * k] = __uint_as_float((uint32_t)v);
+    x[2 * k + 1] = __uint_as_float((uint32_t)(v >> 32));
+  }
+  return x;
+}
 
 // O^T = V^T P^T for the rows that seq_solve_kernel left (tau finite).  Every wave goes through its own 32-key blocks of the workgroup's
 // piece of the keys; the waves' sums are added in their order, and the workgroup that comes last adds up the pieces in theirs.
@@ -537,16 +574,18 @@ __global__ __launch_bounds__(kThreads) void seq_pv_kernel(SeqDecodeArgs A) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += red[(w * 16 + 4 * wave + e) * 64 + lane];
       const int row = qb * 32 + li;
-      if (row < R) *reinterpret_cast<f32x4_t*>(part + (long long)row * D + 32 * mm + 8 * wave + 4 * hh) = sum;
+      if (row < R) put_part(part + (long long)row * D + 32 * mm + 8 * wave + 4 * hh, sum);
     }
   }
-  __threadfence();
+  // The parts pass through memory that all XCDs see: written and read by operations of agent scope, each workgroup's finished (the wait of
+  // every wave, then the barrier) before it counts itself.  A fence of agent scope would write back the whole L2, for every workgroup
+  // (decode_dense, 768 of them: 118 us).
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   const int parts = (v.L + A.pv_keys - 1) / A.pv_keys;
-  if (tid == 0) last = atomicAdd(&A.arrived[head], 1) == parts - 1 ? 1 : 0;
+  if (tid == 0) last = __hip_atomic_fetch_add(&A.arrived[head], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1 ? 1 : 0;
   __syncthreads();
   if (last == 0) return;
-  __threadfence();
   const float* all = A.part + (long long)head * A.pv_splits * A.rows * D;
   for (int e = tid; e < R * (D / 4); e += kThreads) {
     const int row = e / (D / 4), f = (e % (D / 4)) * 4;
@@ -554,7 +593,7 @@ __global__ __launch_bounds__(kThreads) void seq_pv_kernel(SeqDecodeArgs A) {
     f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int k = 0; k < parts; ++k) {
-      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(all + ((long long)k * A.rows + row) * D + f);
+      const f32x4_t x = get_part(all + ((long long)k * A.rows + row) * D + f);
 #pragma unroll
       for (int u = 0; u < 4; ++u) sum[u] += x[u];
     }

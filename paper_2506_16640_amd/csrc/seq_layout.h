@@ -107,11 +107,12 @@ inline int seq_ksplit(long long groups, int max_keys) {
   return n;
 }
 
-// Blocks of a wave of the score kernel: up to eight, while the launch has at least 2048 workgroups of the longest sequence's size (most
-// are shorter); with many rows more, so that they know a large score sooner and write fewer of the others.
+// Consecutive blocks of a wave of the score kernel: as many as leave 1024 workgroups of sequences of max_keys (fewer keep memory waiting: 4 x 4 heads
+// of 32768 keys 20 us with 2048 workgroups, 17 with 1024), at most four (sequences may be much shorter: 64 x 2 heads of 200 to 8192 keys 45 us with eight,
+// 24 with four).  Many rows always take four, so that they know a large score sooner and write fewer of the others.
 inline int seq_run(long long heads, int nblk, int rows) {
   int n = rows > 16 ? 4 : 1;
-  while (n < 8 && heads * ceil_div(nblk, kWaves * 2 * n) >= 2048) n *= 2;
+  while (n < 4 && heads * ceil_div(nblk, kWaves * 2 * n) >= 1024) n *= 2;
   return n;
 }
 

@@ -72,7 +72,14 @@ bool launch_seq_split(const SeqDecodeArgs& a, hipStream_t st) {
   else
     hipLaunchKernelGGL((seq_scores_kernel<T, D, 2>), scores, dim3(kThreads), 0, st, a);
   if (!launch_ok()) return false;
-  hipLaunchKernelGGL((seq_solve_kernel<T, D, AM>), dim3((unsigned)(a.g.nseq * a.g.Hkv * a.rows)), dim3(kSolveThreads), 0, st, a);
+  // A workgroup per row, of 512 threads while three of them for every CU are as many as there are rows, else of 256; with more than 4096 rows (most of them
+  // of no sequence, if some have many new tokens) a workgroup takes several in turn.
+  const long long heads = (long long)a.g.nseq * a.g.Hkv;
+  const int stride = (int)(heads * a.rows <= 4096 ? a.rows : (4096 / heads > 1 ? 4096 / heads : 1));
+  if (heads * a.rows <= 768)
+    hipLaunchKernelGGL((seq_solve_kernel<T, D, AM, 512>), dim3((unsigned)(heads * stride)), dim3(512), 0, st, a, stride);
+  else
+    hipLaunchKernelGGL((seq_solve_kernel<T, D, AM, 256>), dim3((unsigned)(heads * stride)), dim3(256), 0, st, a, stride);
   if (!launch_ok()) return false;
   if (a.rows <= 32)
     hipLaunchKernelGGL((seq_pv_kernel<T, D, AM, 1>), pv, dim3(kThreads), 0, st, a);
