@@ -150,6 +150,7 @@ __device__ __forceinline__ RowSums block_sums(RowSums s, float* buf, int parity)
 }
 
 constexpr int kSolveList = 256;   // candidates kept in LDS, their output gathered here; rows with more are left to seq_pv_kernel
+constexpr int kSolveManyBlocks = 24;
 constexpr int kSolveHeld = 16;    // scores of a long row that a thread holds in registers
 
 template <typename T, int D, int NT>
@@ -158,6 +159,7 @@ struct SolveLds {
   float2 list[kSolveList];  // (key index bits, raw score, then y)
   __attribute__((aligned(16))) float red[2 * kW * 4];
   float wtop[kW];
+  int whot[kW];
   int count;
   float osum[kW * D];
 };
@@ -199,8 +201,43 @@ __device__ __forceinline__ void solve_row(const SeqDecodeArgs& A, SolveLds<T, D,
     if (tid == 0) A.found[at] = make_float2(kInf, 0.f);
     return;
   }
-  const float floor_lo = top - reach;  // (at most top, which is always a candidate)
+  float floor_lo = top - reach;  // (at most top, which is always a candidate)
   auto hot = [&](float m) { return m >= floor_lo && m > -kInf; };
+  // y = a (d - top) in [-1, 0]: the threshold lies between -1 and -n^(1-alpha)
+  auto y_of = [&](float x) { return a * (x - top); };
+  float lo = -1.0f, hi = -__builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)lim));
+  {
+    // Where many blocks come within reach: Newton steps from the left on the blocks' largest scores (scores of different keys: dropping the others
+    // can only lower the threshold) give a higher floor, and far fewer candidates.
+    const unsigned long long mine = __ballot(hot(first));
+    if (lane == 0) lds.whot[wave] = (int)__popcll(mine);
+    __syncthreads();
+    int blocks = 0;
+#pragma unroll
+    for (int w = 0; w < kW; ++w) blocks += lds.whot[w];
+    if (blocks > kSolveManyBlocks) {
+      float t = -1.0f;
+      for (int it = 0; it < 4; ++it) {
+        RowSums sums;
+        sums.clear();
+        auto term = [&](float m) {
+          const float x = hot(m) ? fmaxf(y_of(m) - t, 0.f) : 0.f;
+          const float gx = x > 0.f ? pow_rm1<AM>(x, r) : 0.f;
+          sums.s0 += gx;
+          sums.s1 = fmaf(gx, x, sums.s1);
+        };
+        term(first);
+        for (int b = tid + NT; b < nblk; b += NT) term(bmax[b]);
+        sums = block_sums<NT>(sums, red, it & 1);
+        if (!(sums.s1 > 1.0f)) break;  // (the same in every thread)
+        t += (sums.s1 - 1.0f) / (r * sums.s0);
+      }
+      lo = fminf(fmaxf(lo, t - 4e-6f), hi);
+      floor_lo = fmaf(lo, reach, top);
+      __syncthreads();  // (red is used again)
+    }
+  }
+  float tau = lo;
   // the candidates: two blocks of a wave at a time, half a wave each, and two such pairs under way; a row with more than the list holds is
   // counted no further
   for (int b0 = 0; b0 < nblk; b0 += NT) {
@@ -235,9 +272,6 @@ __device__ __forceinline__ void solve_row(const SeqDecodeArgs& A, SolveLds<T, D,
   }
   __syncthreads();
   const int total = count;
-  // y = a (d - top) in [-1, 0]: the threshold lies between -1 and -n^(1-alpha)
-  float lo = -1.0f, hi = -__builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)lim)), tau = lo;
-  auto y_of = [&](float x) { return a * (x - top); };
   // features of this lane of the value row of key j, times p
   auto add_row = [&](int j, float p, float (&acc)[E]) {
     const u32x4_t w = *reinterpret_cast<const u32x4_t*>(vals.row(j) + (lane % LR) * 16);
@@ -353,7 +387,10 @@ __device__ __forceinline__ void solve_row(const SeqDecodeArgs& A, SolveLds<T, D,
   }
   // Long supports.  Key e of the row counts if its block was written; -inf (y far below -1) else.  The first kSolveHeld NT of them are read once.
   const int n = nblk * 32;
-  auto y_at = [&](int e) { return e < n && hot(bmax[e >> 5]) ? y_of(d[e]) : -kInf; };
+  auto y_at = [&](int e) {
+    const float m = bmax[min(e, n - 1) >> 5], x = d[min(e, n - 1)];  // (two loads, not one after the other)
+    return e < n && hot(m) ? y_of(x) : -kInf;
+  };
   float held[kSolveHeld];
 #pragma unroll
   for (int k = 0; k < kSolveHeld; ++k) held[k] = y_at(tid + k * NT);
@@ -368,22 +405,6 @@ __device__ __forceinline__ void solve_row(const SeqDecodeArgs& A, SolveLds<T, D,
       for (int u = 0; u < 4; ++u) fn(y[u]);
     }
   };
-  {
-    // starting point from the mean and deviation of a row all of whose blocks were written (gauss_start())
-    RowSums st;
-    st.clear();
-    each([&](float y) {
-      if (y > -kInf) {
-        st.s0 += 1.f;
-        st.s1 += y;
-        st.s2 = fmaf(y, y, st.s2);
-      }
-    });
-    st = block_sums<NT>(st, red, 1);
-    const float mean = st.s1 / st.s0, var = st.s2 / st.s0 - mean * mean;
-    float t0;
-    if (st.s0 == (float)lim && var > 0.f && gauss_start<AM>(mean, sqrtf(var), st.s0, t0)) tau = fminf(fmaxf(t0, lo), hi);
-  }
   bool done = false;
   for (int it = 0; !done && it < kMaxSolveIters; ++it) {
     RowSums sums;

@@ -238,6 +238,7 @@ __device__ __forceinline__ float min8(float x) { return dpp_min<0x4E>(dpp_min<0x
 constexpr int kFinishSlots = 16;    // groups of a row that an octet can hold (eight keys each)
 constexpr int kFinishSupport = 32;  // support entries of a row noted before their values are gathered
 constexpr int kScanList = 256;      // candidates of a row that is looked through key by key
+constexpr int kScanKeys = 2048;     // ... of at most so many keys (64 at a time, 0.7 us each)
 constexpr int kScanRows = 1;        // such rows of a wave (eight rows); with more the block is seq_tiled_kernel's
 
 template <int D>
@@ -260,7 +261,7 @@ struct OctetRow {  // of a key/value row or query: the lane's 16-byte words
 
 // NS: parts of the sweep (ksplit <= NS)
 template <int D, int AM, int NS>
-__global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
+__global__ __launch_bounds__(kThreads, 4) void seq_finish_kernel(SeqListArgs A) {
   using T = bf16_t;
   constexpr int W = D / 64, NV = 3 * NS, kItems = 24 * NS;
   __shared__ int items_[kWaves][8][kItems];
@@ -347,12 +348,13 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
   }
   const bool lost = live && max8(last > -3.1e38f && gn.upper(last) > cut ? 1.f : 0.f) > 0.f;
   const bool hard = lost || n > kFinishSlots;
+  const bool too_long = hard && row.lim > kScanKeys;
   const unsigned long long hard_octets = __ballot(hard && c == 0);
   int groups = c == 0 ? n : 0;  // of the wave's rows
 #pragma unroll
   for (int off = 8; off < 64; off <<= 1) groups += __shfl_xor(groups, off);
   // Rescoring goes by the groups, the sweeps of the tiled kernel by the keys
-  if ((int)__popcll(hard_octets) > kScanRows || __builtin_amdgcn_readfirstlane(groups) > SweepAgain<T>::most_groups(v.L) / 4) {
+  if ((int)__popcll(hard_octets) > kScanRows || __ballot(too_long) != 0ull || __builtin_amdgcn_readfirstlane(groups) > SweepAgain<T>::most_groups(v.L) / 4) {
     if (lane == 0) A.dense[id] = kFlagWithBounds;
     return;  // (no barriers in this kernel)
   }
@@ -365,8 +367,11 @@ __global__ __launch_bounds__(kThreads) void seq_finish_kernel(SeqListArgs A) {
     // (all eight within one page; keys behind the last one repeat it)
     const int jp = min(first, v.L - 1);
     const int pg = keys.page(jp);
+    const char* at = keys.row_in(pg, jp);
+    const uint32_t sn = (uint32_t)keys.sn;
+    const int most = v.L - 1 - jp;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) kw[k].load(keys.row_in(pg, min(first + (strided ? 8 * (k >> 2) + (k & 3) : k), v.L - 1)), c);
+    for (int k = 0; k < 8; ++k) kw[k].load(at + (uint32_t)min(strided ? 8 * (k >> 2) + (k & 3) : k, most) * sn, c);
     float s[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) s[k] = kw[k].dot(qw_);
