@@ -116,6 +116,8 @@ inline int seq_run(long long heads, int nblk, int rows) {
   return n;
 }
 
+constexpr long long kSeqWideBelow = 512;
+
 struct SeqLayout {
   bool split;       // the call may hold such sequences
   bool blocks;      // it may hold others

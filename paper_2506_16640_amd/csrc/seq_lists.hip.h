@@ -130,8 +130,9 @@ __global__ __launch_bounds__(kThreads, 3) void seq_sweep_kernel(SeqListArgs A) {
       m1 = fmaxf(m1, top.take(acc, gn, j0 >> 5));
     }
   };
-  // Dense rows show on the first tile: for three quarters of a wave's rows half of the keys of the first block come within the
-  // threshold's reach of the block's largest score.  If all waves find so the block is seq_tiled_kernel's.
+  // Dense rows show on the first tile: for three quarters of a wave's rows nearly all keys of the first block come within the
+  // threshold's reach of the block's largest score.  If all waves find so the block is seq_tiled_kernel's, which then starts from a sample.  (Rows of
+  // fewer candidates get better bounds from this sweep than the sample gives, and save it more than the sweep takes.)
   if (first < whole_end) {
     const f32x16_t acc = scores(smem, 0, first);
     const float lm = max16(acc);
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(kThreads, 3) void seq_sweep_kernel(SeqListArgs A) {
     int near = 0;
 #pragma unroll
     for (int e = 0; e < 16; ++e) near += (acc[e] + reach > lm) ? 1 : 0;
-    const bool dense = 4 * (int)__popcll(__ballot(near >= 8)) >= 3 * (int)__popcll(__ballot(q.lim > 0));
+    const bool dense = 4 * (int)__popcll(__ballot(near >= 15)) >= 3 * (int)__popcll(__ballot(q.lim > 0));
     if (dense && lane == 0) votes[wave] = 1;
     __syncthreads();
   }

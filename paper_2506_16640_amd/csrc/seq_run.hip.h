@@ -55,12 +55,18 @@ inline SeqGeom make_seq_geom(const SeqCall& c) {
   return g;
 }
 
-template <typename T, int D, int AM>
-bool launch_seq_tiled(const SeqArgs& a, hipStream_t st) {
-  const size_t smem = SeqTiledCfg<T, D>::lds_bytes(a.mark_words);
-  constexpr auto kern = seq_tiled_kernel<T, D, AM>;
+template <typename T, int D, int AM, bool WIDE>
+bool launch_seq_tiled(const SeqArgs& a_in, hipStream_t st) {
+  using Cfg = SeqTiledCfg<T, D, WIDE>;
+  SeqArgs a = a_in;
+  // a word of marks per key tile, per more of them where that takes more than 16 KB
+  a.mark_shift = 0;
+  while ((a.g.max_keys / Cfg::KT >> a.mark_shift) >= 4095) ++a.mark_shift;
+  a.mark_words = (a.g.max_keys / Cfg::KT >> a.mark_shift) + 1;
+  const size_t smem = Cfg::lds_bytes(a.mark_words);
+  constexpr auto kern = seq_tiled_kernel<T, D, AM, WIDE>;
   if (!ensure_dynamic_lds<kern>(smem)) return false;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(a.nblk * a.g.Hkv)), dim3((SeqTiledCfg<T, D>::NT)), smem, st, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(a.nblk * a.g.Hkv)), dim3(Cfg::NT), smem, st, a);
   return launch_ok();
 }
 
@@ -113,7 +119,11 @@ bool launch_seq(const SeqArgs& a_in, const SeqListArgs& l, const SeqDecodeArgs& 
       a.blocks = l.blocks;
     }
   }
-  if (L.blocks && !launch_seq_tiled<T, D, AM>(a, st)) return false;
+  if (L.blocks) {
+    // many groups: small workgroups, whose starts and waits overlap; few: all waves of a compute unit on each
+    const bool wide = (long long)a.nblk * a.g.Hkv < kSeqWideBelow;
+    if (!(wide ? launch_seq_tiled<T, D, AM, true>(a, st) : launch_seq_tiled<T, D, AM, false>(a, st))) return false;
+  }
   return !a.split || launch_seq_split<T, D, AM>(d, st);
 }
 
@@ -130,11 +140,6 @@ int run_seq(const SeqCall& c) {
   a.V = c.V;
   a.O = c.O;
   a.nblk = (int)seq_blocks(p->nseq, p->T, a.g.G);
-  // a word per key tile, per more of them where that takes more than 16 KB
-  constexpr int KT = SeqTiledCfg<T, D>::KT;
-  a.mark_shift = 0;
-  while ((p->max_keys / KT >> a.mark_shift) >= 4095) ++a.mark_shift;
-  a.mark_words = (p->max_keys / KT >> a.mark_shift) + 1;
   a.split = L.split && p->path == 0 ? 1 : 0;
   if (!a.split) L.blocks = true;
   a.dense = nullptr;

@@ -53,14 +53,16 @@ __device__ __forceinline__ bool seq_block(const SeqGeom& g, int blk, bool split,
   return true;
 }
 
-template <typename T, int D>
+// WIDE: KS waves share the keys of 32 rows, one workgroup fills a compute unit; else a workgroup of four waves, two or more to a unit.
+template <typename T, int D, bool WIDE>
 struct SeqTiledCfg {
-  static constexpr int NT = sizeof(T) == 2 ? (D == 64 ? 1024 : 512) : (D == 64 ? 512 : 256);  // (registers: 128, 256 or 512 a thread)
-  static constexpr int KS = NT / kThreads;                           // waves that share the keys of 32 rows
-  static constexpr int BW = 2;                                       // 32-key blocks of a wave per tile
+  static constexpr int KS = !WIDE || (sizeof(T) == 4 && D == 128) ? 1 : (sizeof(T) == 2 && D == 64 ? 4 : 2);
+  static constexpr int NT = KS * kThreads;
+  static constexpr int kWavesPerSimd = sizeof(T) == 2 && D == 64 ? (WIDE ? 4 : 3) : (sizeof(T) == 4 && D == 128 ? 1 : 2);
+  static constexpr int BW = sizeof(T) == 4 && D == 128 ? 1 : 2;      // 32-key blocks of a wave per tile
   static constexpr int KT = KS * BW * 32;
   static constexpr int kTileBytes = KT * D * (int)sizeof(T);
-  static_assert(kTileBytes == 32768, "four tiles and the masks fit a compute unit");
+  static_assert(kTileBytes <= 32768, "four tiles and the marks fit a compute unit");
   static size_t lds_bytes(int mark_words) { return 4 * (size_t)kTileBytes + (size_t)mark_words * 4; }
 };
 
@@ -249,9 +251,9 @@ __device__ __forceinline__ void store4(T* dst, float x0, float x1, float x2, flo
   }
 }
 
-template <typename T, int D, int AM>
-__global__ __launch_bounds__((SeqTiledCfg<T, D>::NT)) void seq_tiled_kernel(SeqArgs A) {
-  using Cfg = SeqTiledCfg<T, D>;
+template <typename T, int D, int AM, bool WIDE>
+__global__ __launch_bounds__((SeqTiledCfg<T, D, WIDE>::NT), (SeqTiledCfg<T, D, WIDE>::kWavesPerSimd)) void seq_tiled_kernel(SeqArgs A) {
+  using Cfg = SeqTiledCfg<T, D, WIDE>;
   constexpr int NT = Cfg::NT, KS = Cfg::KS, BW = Cfg::BW, KT = Cfg::KT, NSB = KT / 32, NC = D / 16, NM = D / 32, TB = Cfg::kTileBytes;
   using KTile = SeqTile<T, D, KT, false, NT>;
   using Vals = SeqValues<T, D, KT, NT>;
