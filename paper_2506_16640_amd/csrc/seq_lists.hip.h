@@ -236,10 +236,10 @@ __device__ __forceinline__ float dpp_min(float x) {
 __device__ __forceinline__ float max8(float x) { return dpp_max<0x4E>(dpp_max<0xB1>(dpp_max<0x141>(x))); }
 __device__ __forceinline__ float min8(float x) { return dpp_min<0x4E>(dpp_min<0xB1>(dpp_min<0x141>(x))); }
 
-constexpr int kFinishSlots = 16;    // groups of a row that an octet can hold (eight keys each)
+constexpr int kFinishSlots = 24;    // groups of a row that an octet can hold (eight keys each)
 constexpr int kFinishSupport = 32;  // support entries of a row noted before their values are gathered
 constexpr int kScanList = 256;      // candidates of a row that is looked through key by key
-constexpr int kScanKeys = 2048;     // ... of at most so many keys (64 at a time, 0.7 us each)
+constexpr int kScanKeys = 32768;    // ... of at most so many keys
 constexpr int kScanRows = 1;        // such rows of a wave (eight rows); with more the block is seq_tiled_kernel's
 
 template <int D>
@@ -262,7 +262,7 @@ struct OctetRow {  // of a key/value row or query: the lane's 16-byte words
 
 // NS: parts of the sweep (ksplit <= NS)
 template <int D, int AM, int NS>
-__global__ __launch_bounds__(kThreads, 4) void seq_finish_kernel(SeqListArgs A) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(SeqListArgs A) {
   using T = bf16_t;
   constexpr int W = D / 64, NV = 3 * NS, kItems = 24 * NS;
   __shared__ int items_[kWaves][8][kItems];
@@ -431,9 +431,9 @@ __global__ __launch_bounds__(kThreads, 4) void seq_finish_kernel(SeqListArgs A) 
   for (int k = 0; k < most; ++k) {
     const int it = k < n ? items[k] : 0, j = key_of(it);
     float d = eight(j - 8 * (c >> 2) - (c & 3), true, qw);
-    d = row.signed_dot(d);
-    d = fmaf(row.w, (float)max(row.pos - j, 0), d);
-    d = k < n && j < row.lim && d > -3.0e38f ? d : -kInf;
+    const bool there = k < n && j < row.lim && d > -3.0e38f;  // (-inf: a hole)
+    d = fmaf(row.w, (float)max(row.pos - j, 0), row.signed_dot(d));
+    d = there ? d : -kInf;
     top = fmaxf(top, d);
     ys[k * 64] = d;
   }
@@ -484,6 +484,8 @@ __global__ __launch_bounds__(kThreads, 4) void seq_finish_kernel(SeqListArgs A) 
   };
   if (most <= 4)
     finish(std::integral_constant<int, 4>());
+  else if (most <= 12)
+    finish(std::integral_constant<int, 12>());
   else
     finish(std::integral_constant<int, kFinishSlots>());
 
@@ -500,20 +502,25 @@ __global__ __launch_bounds__(kThreads, 4) void seq_finish_kernel(SeqListArgs A) 
     float2* list = notes_[wave];
     int total = 0;
     float top = -kInf;
+    constexpr int U = W == 1 ? 4 : 2;  // octets' loads under way
 #pragma unroll 1
-    for (int j8 = 0; j8 < hr.lim; j8 += 64) {
-      const int first = j8 + 8 * oct, j = first + c;
-      float d = eight(first, false, hq);
-      d = hr.signed_dot(d);
-      d = fmaf(hr.w, (float)max(hr.pos - j, 0), d);
-      const bool in = j < hr.lim && d > hcut && d > -3.0e38f;
-      const unsigned long long all = __ballot(in);
-      const int at = total + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u));
-      if (in) {
-        if (at < kScanList) list[at] = make_float2(__int_as_float(j), d);
-        top = fmaxf(top, d);
+    for (int j8 = 0; j8 < hr.lim; j8 += 64 * U) {
+      float d[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) d[u] = eight(j8 + 64 * u + 8 * oct, false, hq);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int j = j8 + 64 * u + 8 * oct + c;
+        const float x = fmaf(hr.w, (float)max(hr.pos - j, 0), hr.signed_dot(d[u]));
+        const bool in = j < hr.lim && d[u] > -3.0e38f && x > hcut;
+        const unsigned long long all = __ballot(in);
+        const int at = total + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u));
+        if (in) {
+          if (at < kScanList) list[at] = make_float2(__int_as_float(j), x);
+          top = fmaxf(top, x);
+        }
+        total += (int)__popcll(all);
       }
-      total += (int)__popcll(all);
     }
     if (total == 0 || total > kScanList) {  // (none: the bound came from sums in another order)
       if (lane == 0) A.dense[id] = kFlagWithBounds;
