@@ -154,6 +154,9 @@ struct SeqRow {
   // as in QCtx: y_ij = a d_ij, d_ij = +-<q_i, k_j> + w max(pos - j, 0).  A row of scale 0 (c = 0) has a = 1 and d_ij = 0, so that masked
   // scores are never multiplied by zero.
   float a, c, w;
+  // FAST: (ln n)^gamma from the hardware's logarithm and exponential, a few 1e-7 off: it multiplies the distances of scores from the row's largest, at
+  // most 1 where they count (kernels with bf16 results)
+  template <bool FAST>
   __device__ __forceinline__ void init(const SeqGeom& g, const SeqView& v, int hk, int r, int D) {
     valid = r < v.n * g.G;
     t = valid ? r / g.G : 0;
@@ -164,7 +167,11 @@ struct SeqRow {
     if (g.scale_layout != 0) {
       const long long idx = g.scale_layout == 1 ? head : (long long)head * g.T + v.row0 + t;
       const int n = g.logn_mode == 0 ? v.L : lim;
-      if (n > 1) scale += g.beta[idx] * powf(logf((float)n), g.gamma[idx]);
+      const float be = g.beta[idx], ga = g.gamma[idx];
+      if (n > 1) {
+        const float ln = FAST ? __builtin_amdgcn_logf((float)n) * 0.69314718f : logf((float)n);
+        scale += be * (FAST ? __builtin_amdgcn_exp2f(ga * __builtin_amdgcn_logf(ln)) : powf(ln, ga));
+      }
     }
     if (!valid) scale = 0.f;
     c = scale * (1.0f / sqrtf((float)D));
@@ -209,7 +216,7 @@ struct SeqRows : SeqRow {
     lane = threadIdx.x & 63;
     li = lane & 31;
     hh = lane >> 5;
-    SeqRow::init(g, v, hk, r0 + li, D);
+    SeqRow::init<sizeof(T) == 2>(g, v, hk, r0 + li, D);
     // (limits do not decrease from row to row)
     lim_min = __builtin_amdgcn_readfirstlane(lim);
     const int last = min(v.n * g.G - 1 - r0, 31);

@@ -287,7 +287,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
   vals.init(g, v, A.a.V, hk, true, sizeof(T));
   const int li = wave * 8 + oct;
   SeqRow row;
-  row.init(g, v, hk, b.r0 + wv * 32 + li, D);
+  row.init<true>(g, v, hk, b.r0 + wv * 32 + li, D);
   const float r = 1.0f / (g.alpha - 1.0f), a = row.a;
   const char* qrow = reinterpret_cast<const char*>(reinterpret_cast<const T*>(A.a.Q) + (long long)(v.row0 + row.t) * g.q_st + (long long)row.head * g.q_sh);
   OctetRow<D> qw;
@@ -328,7 +328,9 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
       }
       f = sum8(f);
       fp = sum8(fp);
-      if (f > 1.0f) t += (f - 1.0f) / (r * fp);
+      const bool up = f > 1.0f + 1e-5f;  // (what less would add is not worth a step)
+      if (__ballot(up) == 0ull) break;
+      if (up) t += (f - 1.0f) * __builtin_amdgcn_rcpf(r * fp);
     }
     lo = fmaxf(lo, t - 4e-6f * fmaxf(1.0f, fabsf(t)));
   }
@@ -448,7 +450,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
       y[k] = k < most ? ys[k * 64] : -kInf;
       y[k] = y[k] > -kInf ? a * (y[k] - top) : -kInf;
     }
-    float blo = -1.f, bhi = left_end(row.lim), tau = -1.f;
+    // (the bound is nearly the threshold where every group has one key that counts)
+    float blo = -1.f, bhi = left_end(row.lim), tau = fminf(fmaxf(lo - a * top - 1e-5f * fmaxf(1.f, fabsf(lo)), -1.f), bhi);
     bool done = !some;
     for (int it = 0; __ballot(!done) != 0ull && it < kMaxSolveIters; ++it) {
       RowSums sums;
