@@ -238,9 +238,10 @@ __device__ __forceinline__ float min8(float x) { return dpp_min<0x4E>(dpp_min<0x
 
 constexpr int kFinishSlots = 24;    // groups of a row that an octet can hold (eight keys each)
 constexpr int kFinishSupport = 32;  // support entries of a row noted before their values are gathered
-constexpr int kScanList = 256;      // candidates of a row that is looked through key by key
-constexpr int kScanKeys = 32768;    // ... of at most so many keys
-constexpr int kScanRows = 1;        // such rows of a wave (eight rows); with more the block is seq_tiled_kernel's
+constexpr int kScanList = 256;      // candidates of a row that all octets look through together
+constexpr int kHardRows = 3;        // such rows of a wave (eight rows): with more groups than an octet holds, or (one of them) looked through key by key
+constexpr int kScanGroups = 40;     // ... where the wave's other rows have at most so many groups together
+constexpr int kScanKeys = 8192;     // ... and at most so many keys
 
 template <int D>
 struct OctetRow {  // of a key/value row or query: the lane's 16-byte words
@@ -262,12 +263,13 @@ struct OctetRow {  // of a key/value row or query: the lane's 16-byte words
 
 // NS: parts of the sweep (ksplit <= NS)
 template <int D, int AM, int NS>
-__global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(SeqListArgs A) {
+__global__ __launch_bounds__(kThreads, 4) void seq_finish_kernel(SeqListArgs A) {
   using T = bf16_t;
-  constexpr int W = D / 64, NV = 3 * NS, kItems = 24 * NS;
-  __shared__ int items_[kWaves][8][kItems];
-  __shared__ float2 notes_[kWaves][kScanList];
-  __shared__ float scores_[kWaves][kFinishSlots * 64];
+  constexpr int W = D / 64, NV = 3 * NS;
+  // (how much of it decides how many workgroups a compute unit holds: the notes take the scores' place when those are in registers)
+  __shared__ int items_[kWaves][8][kFinishSlots];
+  __shared__ __attribute__((aligned(16))) float scores_[kWaves][kFinishSlots * 64];
+  static_assert(kScanList * 8 <= kFinishSlots * 64 * 4, "a wave's notes fit its scores");
   static_assert(kScanList >= 8 * kFinishSupport, "the octets' support notes and a scanned row's candidates take turns");
   const SeqGeom& g = A.a.g;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, oct = lane >> 3, c = lane & 7;
@@ -346,18 +348,21 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
   for (int k = 0; k < NV; ++k) {
     const bool above = live && tv[k] > -3.1e38f && gn.upper(tv[k]) > cut;
     const unsigned mask = (unsigned)(__ballot(above) >> (8 * oct)) & 0xffu;
-    if (above) items[n + (int)__popc(mask & ((1u << c) - 1u))] = (int)((__float_as_uint(tv[k]) & ~gn.keep) << 1) | (c & 1);
+    const int place = n + (int)__popc(mask & ((1u << c) - 1u));
+    if (above && place < kFinishSlots) items[place] = (int)((__float_as_uint(tv[k]) & ~gn.keep) << 1) | (c & 1);
     n += (int)__popc(mask);
   }
   const bool lost = live && max8(last > -3.1e38f && gn.upper(last) > cut ? 1.f : 0.f) > 0.f;
   const bool hard = lost || n > kFinishSlots;
-  const bool too_long = hard && row.lim > kScanKeys;
-  const unsigned long long hard_octets = __ballot(hard && c == 0);
-  int groups = c == 0 ? n : 0;  // of the wave's rows
+  const unsigned long long hard_octets = __ballot(hard && c == 0), lost_octets = __ballot(lost && c == 0);
+  int groups = c == 0 && !lost ? n : 0;  // of the wave's rows that remember all of theirs
 #pragma unroll
   for (int off = 8; off < 64; off <<= 1) groups += __shfl_xor(groups, off);
-  // Rescoring goes by the groups, the sweeps of the tiled kernel by the keys
-  if ((int)__popcll(hard_octets) > kScanRows || __ballot(too_long) != 0ull || __builtin_amdgcn_readfirstlane(groups) > SweepAgain<T>::most_groups(v.L) / 4) {
+  groups = __builtin_amdgcn_readfirstlane(groups);
+  // Rescoring goes by the groups, the sweeps of the tiled kernel by the keys.  One row that has lost groups among rows of few is an exception and
+  // looked through key by key; among rows of many it is one of several of its block.
+  if (groups > SweepAgain<T>::most_groups(v.L) / 4 || (int)__popcll(hard_octets) > kHardRows || (int)__popcll(lost_octets) > 1 ||
+      (lost_octets != 0ull && (groups > kScanGroups || __ballot(lost && row.lim > kScanKeys) != 0ull))) {
     if (lane == 0) A.dense[id] = kFlagWithBounds;
     return;  // (no barriers in this kernel)
   }
@@ -421,7 +426,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
   };
   auto left_end = [&](int lim) { return -__builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)max(lim, 1))); };
 
-  float2* notes = notes_[wave] + oct * kFinishSupport;
+  float2* const wave_notes = reinterpret_cast<float2*>(scores_[wave]);
+  float2* notes = wave_notes + oct * kFinishSupport;
   // ---- the groups' scores: slot k of this lane's row at ys[k * 64]
   float* ys = scores_[wave] + lane;
   float top = -kInf;
@@ -450,6 +456,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
       y[k] = k < most ? ys[k * 64] : -kInf;
       y[k] = y[k] > -kInf ? a * (y[k] - top) : -kInf;
     }
+    __builtin_amdgcn_wave_barrier();
     // (the bound is nearly the threshold where every group has one key that counts)
     float blo = -1.f, bhi = left_end(row.lim), tau = fminf(fmaxf(lo - a * top - 1e-5f * fmaxf(1.f, fabsf(lo)), -1.f), bhi);
     bool done = !some;
@@ -492,7 +499,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
   else
     finish(std::integral_constant<int, kFinishSlots>());
 
-  // ---- rows that are looked through, all octets together
+  // ---- rows that all octets look through together: their groups, or all of their keys
   for (unsigned long long rows = hard_octets; rows != 0ull; rows &= rows - 1ull) {
     const int from = __builtin_ctzll(rows);  // the octet's first lane
     const SeqRow hr = row.of_lane(from);
@@ -502,9 +509,39 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
     for (int k = 0; k < W; ++k)
 #pragma unroll
       for (int e = 0; e < 4; ++e) hq.w[k][e] = (uint32_t)__shfl((int)qw.w[k][e], from + c);
-    float2* list = notes_[wave];
+    float2* list = wave_notes;
     int total = 0;
     float top = -kInf;
+    // this lane's key j with raw product d
+    auto take = [&](int j, float d) {
+      const float x = fmaf(hr.w, (float)max(hr.pos - j, 0), hr.signed_dot(d));
+      const bool in = j < hr.lim && d > -3.0e38f && x > hcut;
+      const unsigned long long all = __ballot(in);
+      const int at = total + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u));
+      if (in) {
+        if (at < kScanList) list[at] = make_float2(__int_as_float(j), x);
+        top = fmaxf(top, x);
+      }
+      total += (int)__popcll(all);
+    };
+    if (((lost_octets >> from) & 1ull) == 0ull) {
+      int* wide = items_[wave][0];  // (nobody's any more)
+      static_assert(24 * NS <= 8 * kFinishSlots, "a row's groups fit the octets' lists");
+      int n_wide = 0;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const bool above = tv[k] > -3.1e38f && gn.upper(tv[k]) > cut;
+        const unsigned mask = (unsigned)(__ballot(above) >> from) & 0xffu;
+        if (above && oct == from >> 3) wide[n_wide + (int)__popc(mask & ((1u << c) - 1u))] = (int)((__float_as_uint(tv[k]) & ~gn.keep) << 1) | (c & 1);
+        n_wide += (int)__popc(mask);
+      }
+      __builtin_amdgcn_wave_barrier();
+      for (int k0 = 0; k0 < n_wide; k0 += 8) {
+        const int j = key_of(wide[min(k0 + oct, n_wide - 1)]);
+        const float d = eight(j - 8 * (c >> 2) - (c & 3), true, hq);
+        take(k0 + oct < n_wide ? j : 0x7fffffff, d);
+      }
+    } else {
     constexpr int U = W == 1 ? 4 : 2;  // octets' loads under way
 #pragma unroll 1
     for (int j8 = 0; j8 < hr.lim; j8 += 64 * U) {
@@ -512,18 +549,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 4 : 3) void seq_finish_kernel(S
 #pragma unroll
       for (int u = 0; u < U; ++u) d[u] = eight(j8 + 64 * u + 8 * oct, false, hq);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int j = j8 + 64 * u + 8 * oct + c;
-        const float x = fmaf(hr.w, (float)max(hr.pos - j, 0), hr.signed_dot(d[u]));
-        const bool in = j < hr.lim && d[u] > -3.0e38f && x > hcut;
-        const unsigned long long all = __ballot(in);
-        const int at = total + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0u));
-        if (in) {
-          if (at < kScanList) list[at] = make_float2(__int_as_float(j), x);
-          top = fmaxf(top, x);
-        }
-        total += (int)__popcll(all);
-      }
+      for (int u = 0; u < U; ++u) take(j8 + 64 * u + 8 * oct + c, d[u]);
+    }
     }
     if (total == 0 || total > kScanList) {  // (none: the bound came from sums in another order)
       if (lane == 0) A.dense[id] = kFlagWithBounds;
