@@ -279,8 +279,9 @@ size_t entmax_scale_proj_workspace_bytes(const entmax_scale_proj_params* p);
  * place j % page_size.  kv_len, int32 [nseq]: tokens of each sequence, its new ones (the last ones) included.
  * All of these live in device memory and are read by the kernels only, so that a captured graph serves other lengths and
  * pages on replay.  Nothing outside the tensors is touched whatever they hold:
- *   - A sequence is left out (its rows are not written) if cu_seqlens leads out of the T rows or decreases, if it has more than
- *     max_new new tokens, or more than max_keys keys, or kv_len is negative.
+ *   - A sequence is left out (its rows are not written) if its part of cu_seqlens leads out of the T rows or decreases, if it has more
+ *     than max_new new tokens, or more than max_keys keys, or kv_len is negative.  (Where cu_seqlens decreases further on, others may be
+ *     left out with it.)
  *   - A page number outside 0 .. num_pages - 1 is a hole: its keys are visible to no row, and tokens appended there are dropped.
  *
  * Attention (entmax_paged_attn_fwd, entmax_packed_attn_fwd): the operation of entmax_attn_fwd.  New token t of a sequence
