@@ -6,6 +6,8 @@
 //                      above it once more from memory (each lane then holds one key of every group), threshold, and the output from the
 //                      values of the support.  Rows that remember too few groups are looked through key by key; where a block has many of
 //                      those, or its rows are dense, it is left to seq_tiled_kernel.
+// Measured: 4 x 512 tokens, 4 x 4 heads of 128, against 2000 to 16384 keys: sweep 96 us (650 TFLOP/s: the vector work on the scores beside the matrix
+// work; 186 us without sharing out the keys), finish 49 to 54 us (dependent gathers: groups, keys, values).
 #pragma once
 #include "decode.hip.h"
 #include "fwd_sparse.hip.h"
@@ -239,6 +241,11 @@ __device__ __forceinline__ float min8(float x) { return dpp_min<0x4E>(dpp_min<0x
 constexpr int kFinishSlots = 24;    // groups of a row that an octet can hold (eight keys each)
 constexpr int kFinishSupport = 32;  // support entries of a row noted before their values are gathered
 constexpr int kScanList = 256;      // candidates of a row that all octets look through together
+// The rows that the finish kernel takes the long way instead of giving their whole block to the tiled kernel.  Blocks of 128 rows against 32000 keys,
+// alpha 1.7, no scale: 59 us here and nothing left for the tiled kernel; with none taken 51 us here and 1430 us there.  Where blocks are dense
+// anyway it costs time here (prompts of 300 to 2000 tokens without a scale: 46 us for 36; prompts with scales: 66 us for 62).  Rows looked through key by
+// key are rarer: with none of them the first case leaves 4 us more to the tiled kernel, and with groups up to 200 instead of 40 the prompts without a
+// scale cost 53 us here.
 constexpr int kHardRows = 3;        // such rows of a wave (eight rows): with more groups than an octet holds, or (one of them) looked through key by key
 constexpr int kScanGroups = 40;     // ... where the wave's other rows have at most so many groups together
 constexpr int kScanKeys = 8192;     // ... and at most so many keys

@@ -120,7 +120,6 @@ bool launch_seq(const SeqArgs& a_in, const SeqListArgs& l, const SeqDecodeArgs& 
     }
   }
   if (L.blocks) {
-    // many groups: small workgroups, whose starts and waits overlap; few: all waves of a compute unit on each
     const bool wide = (long long)a.nblk * a.g.Hkv < kSeqWideBelow;
     if (!(wide ? launch_seq_tiled<T, D, AM, true>(a, st) : launch_seq_tiled<T, D, AM, false>(a, st))) return false;
   }
