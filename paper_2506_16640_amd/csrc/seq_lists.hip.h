@@ -344,7 +344,7 @@ __global__ __launch_bounds__(kThreads, 4) void seq_finish_kernel(SeqListArgs A) 
     lo = fmaxf(lo, t - 4e-6f * fmaxf(1.0f, fabsf(t)));
   }
   const float cut = raw_cut(a, live, lo);
-  if (c == 0) A.bounds[(long long)id * kBlockRows + wv * 32 + li] = make_float2(lo, live ? y1 : -kInf);
+  if (c == 0) A.bounds[(long long)id * kBlockRows + wv * 32 + li] = make_float2(lo - y1, live ? m1 : -kInf);
   if (__builtin_amdgcn_readfirstlane(__hip_atomic_load(&A.dense[id], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) != 0)
     return;  // (others of the block's rows have given it up)
 

@@ -3,7 +3,7 @@
 //   1. bounds and a starting point for the threshold tau of
 //        f(tau) = sum_j [y_j - tau]_+^r - 1 = 0,   y = (alpha-1) s,  r = 1 / (alpha-1)
 //      from the list kernels, or from a sample of the key tiles
-//   2. sweeps over K that evaluate f and step (solve_step()); the first one notes which 32-key blocks can hold a positive term at all
+//   2. sweeps over K that evaluate f and step (SeqSearch); the first one notes which 32-key blocks can hold a positive term at all
 //   3. a sweep over K and V: O^T = V^T P^T on the matrix cores.  The accumulators of S^T are the second operand as they are; V^T comes out
 //      of row-major tiles through transposing LDS reads (ds_read_b64_tr_b16: sixteen lanes give four rows of sixteen
 //      elements, each lane gets a column), so that no transposed copy of V exists anywhere.
@@ -15,6 +15,7 @@
 #include "fwd.hip.h"
 #include "seq.hip.h"
 #include "seq_layout.h"
+#include "seq_search.h"
 
 namespace entmax {
 
@@ -33,7 +34,7 @@ struct SeqArgs {
   int mark_shift, mark_words;  // seq_tiled_kernel: a word of marks for every 1 << mark_shift key tiles
   const int* dense;  // NULL, or [Hkv * nblk]: only the groups that are marked, kFlagDense or kFlagWithBounds
   const SeqBlock* blocks;  // with dense: [Hkv * nblk]
-  const float2* bounds;  // with dense: [Hkv * nblk][128] of groups with bounds: (lower bound of the threshold, (alpha-1) x largest score)
+  const float2* bounds;  // with dense: [Hkv * nblk][128] of groups with bounds: (lower bound of the threshold relative to the largest y, largest raw score)
   int split;       // sequences with few rows are left to the kernels that split the keys
 };
 
@@ -68,17 +69,14 @@ struct SeqTiledCfg {
   static size_t lds_bytes(int mark_words) { return 4 * (size_t)kTileBytes + (size_t)mark_words * 4; }
 };
 
-// Partial sums of the threshold function over a lane's keys at tau, x = [y - tau]_+ (at most 1, for tau is never below the largest y by
-// more: the clamp of the multiply-add is the lower and the upper limit in one):  g = sum x^(r-1), h = sum x^r, and with CURV
-// k = sum x^(r-2) (alpha 1.5: the count; alpha 2 and general alpha: not formed).
-struct SeqSums {
-  float g, h, k;
-};
+// Adds a block of a lane's scores to the sums at tau (relative to the row's largest score, a ref), x = [y - tau]_+ at most 1, for tau is never below the
+// largest y by more: the clamp of the multiply-add is the lower and the upper limit in one.  CURV: k too (alpha 1.5: the count; alpha 2 and
+// general alpha: not formed).  The difference of the scores is exact where it counts: scores of a few thousand lose no bits of the probabilities.
 template <int AM, bool CURV>
-__device__ __forceinline__ void accumulate_keys(SeqSums& s, const f32x16_t& acc, float a, float tau, float r) {
+__device__ __forceinline__ void accumulate_keys(SeqSums& s, const f32x16_t& acc, float ref, float a, float tau, float r) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
-    const float x = __builtin_amdgcn_fmed3f(fmaf(acc[e], a, -tau), 0.f, 1.f);
+    const float x = __builtin_amdgcn_fmed3f(fmaf(acc[e] - ref, a, -tau), 0.f, 1.f);
     if (AM == 1) {
       s.g += x;
       s.h = fmaf(x, x, s.h);
@@ -98,42 +96,6 @@ __device__ __forceinline__ void accumulate_keys(SeqSums& s, const f32x16_t& acc,
     }
   }
 }
-
-// The search for a row's threshold from sums over all its keys, sweep by sweep.  f = h - 1, f' = -r g; the curvature comes from k
-// where it was formed, else from the change of g since the sweep before: the root of the quadratic model, inside the bracket.
-//   No sweep is spent on confirming the last step.  The model leaves out the third order: after a step t about t^3 w^2 is left, w the larger of g and
-// 2 B / A (both about one over the typical x), without a curvature t^2 w r / 2; a step that leaves less than 2^-20 by 64 times (16 times) that ends the
-// search.  (Rows of 40 to 4096 normal scores, alpha 1.25 to 1.7, from the list kernels' bounds: 1.5 sweeps, threshold within 2e-6; confirming would take one more.)
-// At alpha 2, where f is piecewise linear and its curvature jumps from key to key, the last step is confirmed.
-struct SeqSearch {
-  float tau, lo, hi, g_before, tau_before;
-  bool before;
-  __device__ __forceinline__ bool step(const SeqSums& s, float r, bool with_k, bool linear) {
-    const float f = s.h - 1.0f, A = r * s.g;
-    if (f >= 0.f) lo = fmaxf(lo, tau); else hi = fminf(hi, tau);
-    float B = 0.f;  // half of f''
-    bool curved = false;
-    if (with_k) {
-      B = 0.5f * r * (r - 1.0f) * s.k;
-      curved = true;
-    } else if (before && !linear && tau != tau_before) {
-      B = fmaxf(0.5f * r * (g_before - s.g) / (tau - tau_before), 0.f);
-      curved = true;
-    }
-    const float t = 2.0f * f / (A + __builtin_amdgcn_sqrtf(fmaxf(fmaf(A, A, -4.0f * B * f), 0.f)));
-    float to = tau + t;
-    const bool in = A > 0.f && to >= lo && to <= hi;
-    if (!in) to = hi < kInf ? 0.5f * (lo + hi) : lo;
-    const float at = fabsf(t), w = fmaxf(s.g, A > 0.f ? 2.0f * B / A : 0.f);
-    const float left = linear ? at : (curved ? 64.0f * at * (at * w) * (at * w) : 8.0f * at * (at * w) * r);
-    const bool fin = (in && left <= 0x1p-20f) || hi - lo <= 0x1p-22f;
-    before = true;
-    g_before = s.g;
-    tau_before = tau;
-    tau = to;
-    return fin;
-  }
-};
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint2 read_transposed(const char* lds) {
@@ -379,17 +341,17 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D, WIDE>::NT), (SeqTiledCfg<T, D, W
   };
 
   // ------------------------------------------------------------ 1. where to start
+  // (y, tau and the bracket are relative to a ref, the largest score known; the whole search is)
   const bool given = flag == kFlagWithBounds;
-  float m = -kInf, my = 0.f, lo = -1.f, hi = 0.f, tau = -1.f;
+  float m = -kInf, ref = 0.f, lo = -1.f, hi = kInf, tau = -1.f;
   const float below = q.lim > 0 ? __builtin_amdgcn_exp2f(-(g.alpha - 1.0f) * __builtin_amdgcn_logf((float)q.lim)) : 1.f;
   bool live, know_max = true;
   if (given) {
     const float2 bd = A.bounds[((long long)hk * A.nblk + blk) * kBlockRows + rg * 32 + q.li];
-    my = bd.y;
-    live = q.lim > 0 && my > -kInf;
-    if (!live) my = 0.f;
-    hi = my - below;
-    lo = live ? fminf(fmaxf(my - 1.0f, bd.x), hi) : my - 1.0f;
+    live = q.lim > 0 && bd.y > -3.0e38f;  // (-3e38: the list kernels' score of masked keys)
+    ref = live ? bd.y : 0.f;
+    hi = -below;
+    lo = live ? fminf(fmaxf(-1.0f, bd.x), hi) : -1.0f;
     tau = lo;
   } else {
     // a sample of about four tiles (all of them where there are no more, and where a tile may show a row no key at all)
@@ -424,20 +386,18 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D, WIDE>::NT), (SeqTiledCfg<T, D, W
     }
     live = q.lim > 0 && m > -kInf;
     know_max = every == 1;
-    my = live ? q.a * m : 0.f;
-    lo = my - 1.0f;  // (the largest score is at least the sample's)
-    hi = know_max ? my - below : kInf;
-    tau = lo;
+    ref = live ? m : 0.f;  // (the largest score is at least the sample's)
+    if (know_max) hi = -below;
     if (live && msn >= 64.f) {
       const float mean = ms1 / msn, var = ms2 / msn - mean * mean;
       float t0;
-      if (var > 0.f && gauss_start<AM>(q.a * mean, q.a * sqrtf(var), (float)q.lim, t0)) tau = fminf(fmaxf(t0, lo), hi);
+      if (var > 0.f && gauss_start<AM>(q.a * (mean - ref), q.a * sqrtf(var), (float)q.lim, t0)) tau = fminf(fmaxf(t0, lo), hi);
     }
   }
-  const float lo0 = lo;  // blocks without a term above it are zero for good
+  const float lo0 = lo, ref0 = ref;  // blocks without a term above lo0 are zero for good
 
   // ------------------------------------------------------------ 2. threshold
-  SeqSearch search{tau, lo, hi, 0.f, 0.f, false};
+  SeqSearch<AM> search{tau, lo, hi, 0.f, 0.f, false};
   bool done = !live;
   int iter = 0, more;
   auto sweep = [&](auto first_) {
@@ -452,11 +412,11 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D, WIDE>::NT), (SeqTiledCfg<T, D, W
                 if (FIRST) {
                   const float lm = max16(acc);
                   m = fmaxf(m, lm);
-                  const bool any = live && lm > -kInf && fmaf(lm, q.a, -lo0) > 0.f;
+                  const bool any = live && lm > -kInf && fmaf(lm - ref0, q.a, -lo0) > 0.f;
                   if (__ballot(any) == 0ull) return;
                   if (lane == 0) atomicOr(&marks[kt >> A.mark_shift], 1u << (8 * rg + sb));
                 }
-                accumulate_keys<AM, FIRST>(sums, acc, q.a, t_now, r);
+                accumulate_keys<AM, FIRST>(sums, acc, ref, q.a, t_now, r);
               });
             });
     sums.g += __shfl_xor(sums.g, 32);
@@ -474,11 +434,14 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D, WIDE>::NT), (SeqTiledCfg<T, D, W
       if (FIRST) m = fmaxf(m, x[3]);
     }
     if (FIRST && !know_max) {
-      my = live ? q.a * m : 0.f;
-      search.lo = fmaxf(search.lo, my - 1.0f);
-      search.hi = my - below;
+      // from the sample's largest score to the row's
+      const float up = live ? q.a * (m - ref) : 0.f;
+      ref = live ? m : 0.f;
+      search.tau -= up;
+      search.lo = fmaxf(search.lo - up, -1.0f);
+      search.hi = -below;
     }
-    if (!done) done = search.step(sums, r, FIRST && (AM == 1 || AM == 3), AM == 2);
+    if (!done) done = search.step(sums, r, FIRST && (AM == 1 || AM == 3));
     ++iter;
     more = __syncthreads_or(done ? 0 : 1);
   };
@@ -527,7 +490,7 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D, WIDE>::NT), (SeqTiledCfg<T, D, W
         float p[16], any = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          p[e] = pow_r<AM>(__builtin_amdgcn_fmed3f(fmaf(acc[e], q.a, -t_out), 0.f, 1.f), r);
+          p[e] = pow_r<AM>(__builtin_amdgcn_fmed3f(fmaf(acc[e] - ref, q.a, -t_out), 0.f, 1.f), r);
           any = fmaxf(any, p[e]);
         }
         if (__ballot(any > 0.f) == 0ull) return;  // every probability of the block is zero
