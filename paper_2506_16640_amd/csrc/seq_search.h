@@ -19,13 +19,23 @@ struct SeqSums {
 // y and tau are taken relative to the row's largest score, so that tau lies in [-1, 0) and its last place is 2^-24 whatever the size of the scores.
 // f = h - 1, f' = -r g; half the curvature, B, comes from k where it was formed, else from the change of g since the sweep before.  A step t goes to the
 // root of the quadratic model, inside the bracket [lo, hi].
-//   No sweep is spent on confirming the last step.  The model leaves out the third order: after a step t about t^3 w^2 is left, w the larger of g and
-// 2 B / A (both about one over the typical x), without a curvature t^2 w r / 2; a step that leaves less than 2^-20 by 64 times (16 times) that ends the
-// search.  At alpha 2, where f is piecewise linear and its curvature jumps from key to key, the last step is confirmed.
+//   A last step is not confirmed by another sweep where what it leaves is known to be less than 2^-19, from bounds of how the slope |f'| changes over it:
+//   r >= 2, the root between the last two points (gap apart): the slope is a convex function of tau (f'' = r (r-1) sum x^(r-2) falls as keys leave), so it lies
+//     below its chord, by at most twice the deficit of its integral (f's difference) over the gap; the model follows the chord;
+//   r = 2 (alpha 1.5) otherwise: over t the slope changes by at most 2 t times the keys that leave (t > 0: those that count now, or on average between the last
+//     two points) or enter (t < 0: the n that the row sees);
+//   r > 2 otherwise: the model leaves out the third order, about |t| (|t| w) (d w) with w the larger of g and 2 B / A (both about one over the typical x) and
+//     d = |t| where B was formed at this tau, else the larger of |t| and the gap; sixteen times that has to be below 2^-19;
+//   r < 2: a key's term has an unbounded curvature where it meets the threshold, and at r = 1 the slope jumps there: the step itself has to be that short.
+// (Rows of 17 to 1500 normal scores, deviations 0.3 to 1000, clusters of up to 290 equal ones, alpha 1.1 to 2, 1.5 million rows: threshold within 1.6e-6.
+// Sweeps a row from the list kernels' bounds: 1.7 at alpha 1.5, 1.8 at 2, 2.6 at 1.25, 2.5 at 1.7; from the left end 2.5, 2.6, 3.5 and 4.2.  At alpha 1.5
+// the third order alone, sixteen times with the gap as well, left up to 4.5e-6 near clusters; on t alone, for all alpha, up to 3e-5 at 1.7 and 1e-4 at
+// 1.95, and saved bf16 prompts without a scale 10 us of 133, a chunk of 4 x 512 tokens at alpha 1.25 64 of 1003.)
 template <int AM>
 struct SeqSearch {
   float tau, lo, hi;
-  float g_before, tau_before;
+  float n;  // keys that the row sees
+  float g_before, tau_before, f_before;
   bool before;
   // with_k: the sums hold k.  Returns whether tau is final.
   ENTMAX_BOTH_SIDES bool step(const SeqSums& s, float r, bool with_k) {
@@ -45,11 +55,25 @@ struct SeqSearch {
     float to = tau + t;
     const bool in = A > 0.f && to >= lo && to <= hi;
     if (!in) to = 0.5f * (lo + hi);
-    const float at = fabsf(t), w = fmaxf(s.g, A > 0.f ? 2.0f * B / A : 0.f);
-    const float left = AM == 2 ? at : (curved ? 64.0f * at * (at * w) * (at * w) : 8.0f * at * (at * w) * r);
-    const bool fin = (in && left <= 0x1p-20f) || hi - lo <= 0x1p-22f;
+    const float at = fabsf(t);
+    float left = at;
+    if (AM != 2 && r >= 2.0f && curved) {
+      const float Ab = r * g_before, gap = fabsf(back);
+      if (before && t * back > 0.f) {
+        const float deficit = fabsf(0.5f * (A + Ab) * gap - fabsf(f - f_before));
+        left = fminf(at, 2.0f * at * deficit / (gap * fminf(A, Ab)));
+      } else if (AM == 1) {
+        const float dA = 2.0f * (t >= 0.f ? B : n) * at;
+        if (dA < 0.5f * A) left = 0.5f * at * dA / (A - dA);
+      } else {
+        const float w = fmaxf(s.g, A > 0.f ? 2.0f * B / A : 0.f);
+        left = fminf(at, 16.0f * at * (at * w) * ((with_k ? at : fmaxf(at, gap)) * w));
+      }
+    }
+    const bool fin = (in && left <= 0x1p-19f) || hi - lo <= 0x1p-22f;
     before = true;
     g_before = s.g;
+    f_before = f;
     tau_before = tau;
     tau = to;
     return fin;

@@ -76,7 +76,7 @@ static void row(float alpha, int n, int cluster, float deviation, int start, See
   }
   vector<float> w(n);
   for (int i = 0; i < n; ++i) w[i] = y[i] - ref;
-  SeqSearch<AM> s{tau, lo, hi, 0.f, 0.f, false};
+  SeqSearch<AM> s{tau, lo, hi, (float)n, 0.f, 0.f, 0.f, false};
   int sweeps = 0;
   bool done = false;
   while (!done && sweeps < 48) {
@@ -97,17 +97,17 @@ static void row(float alpha, int n, int cluster, float deviation, int start, See
 }
 
 int main() {
-  const float alphas[] = {1.25f, 1.5f, 2.0f};
+  const float alphas[] = {1.1f, 1.25f, 1.4f, 1.5f, 1.7f, 1.8f, 1.9f, 1.95f, 1.99f, 2.0f};
   double mean15[3] = {0, 0, 0}, mean2[3] = {0, 0, 0};
   long rows = 0;
   bool good = true;
   printf("ok so far\n");  // (the line by line report follows)
   for (float alpha : alphas)
-    for (int start = 0; start < 3; ++start) {
+    for (int start = 0; start < 2; ++start) {
       Seen seen;
       for (float deviation : {0.3f, 1.0f, 5.0f, 15.0f, 40.0f, 1000.0f})
         for (int cluster : {1, 1, 8, 290})
-          for (int k = 0; k < 100; ++k) {
+          for (int k = 0; k < 40; ++k) {
             const int n = k % 8 == 0 ? 1500 : (k % 8 == 1 ? 17 : 300);
             if (alpha == 1.5f) row<1>(alpha, n, cluster, deviation, start, seen);
             else if (alpha == 2.0f) row<2>(alpha, n, cluster, deviation, start, seen);
@@ -119,9 +119,9 @@ int main() {
       if (alpha == 1.5f) mean15[start] = mean;
       if (alpha == 2.0f) mean2[start] = mean;
       rows += seen.rows;
-      good = good && (alpha != 2.0f || seen.worst <= 0x1p-19 + 0x1p-22) && seen.most < 24;
+      good = good && seen.worst <= 0x1p-19 + 0x1p-22 && seen.most < 24;
     }
-  for (int start = 0; start < 3; ++start) good = good && mean2[start] <= 1.5 * mean15[start];
+  for (int start = 0; start < 2; ++start) good = good && mean2[start] <= 1.5 * mean15[start];
   printf("%s %ld rows\n", good ? "ok" : "failed:", rows);
   return good ? 0 : 1;
 }

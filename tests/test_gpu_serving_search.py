@@ -1,4 +1,4 @@
-"""GPU tests of the serving attention's thresholds: scores far from zero, scores far apart."""
+"""GPU tests of the serving attention's thresholds: general alpha up to 2, scores far from zero, scores far apart."""
 import pytest
 import torch
 
@@ -22,8 +22,20 @@ def _within(p, got, ref, tol, label):
     assert excess <= 0.0, (label, "beyond the bound by", excess)
 
 
+@pytest.mark.parametrize("scale", ["head", "dense", "none"])
 @pytest.mark.parametrize("dtype", [FP32, BF16])
-@pytest.mark.parametrize("alpha", [1.25, 1.5, 2.0])
+@pytest.mark.parametrize("alpha", [1.7, 1.8, 1.9, 1.95, 1.99, 2.0])
+def test_alphas_up_to_two(binding, alpha, dtype, scale):
+    packed = Problem([(500, 500), (130, 130), (70, 70)], Hq=6, Hkv=3, paged=False, alpha=alpha, dtype=dtype, scale=scale, seed=41)
+    paged = Problem([(150, 600), (3, 900), (1, 333)], Hq=4, Hkv=2, alpha=alpha, dtype=dtype, scale=scale, seed=42)
+    for p in (packed, paged):
+        ref, tol = p.reference()
+        for path in (1, 0):
+            _within(p, p.run(binding, path=path), ref, tol, "alpha %g %s path %d" % (alpha, scale, path))
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("alpha", [1.25, 1.5, 1.7, 1.9, 2.0])
 @pytest.mark.parametrize("paged", [True, False])
 def test_scores_far_from_zero(binding, paged, alpha, dtype):
     """Products that 32 bits hold exactly, all of them 32768 off: entmax does not change with that, and the result must not lose bits to it.  The
