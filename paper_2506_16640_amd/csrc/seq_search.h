@@ -55,6 +55,8 @@ struct SeqSearch {
     float to = tau + t;
     const bool in = A > 0.f && to >= lo && to <= hi;
     if (!in) to = 0.5f * (lo + hi);
+    // (further below the largest score than 1, as after a sample that did not hold it, its term was cut off at 1: such sums tell the side, no more)
+    const bool whole = tau >= -1.0f;
     const float at = fabsf(t);
     float left = at;
     if (AM != 2 && r >= 2.0f && curved) {
@@ -70,8 +72,8 @@ struct SeqSearch {
         left = fminf(at, 16.0f * at * (at * w) * ((with_k ? at : fmaxf(at, gap)) * w));
       }
     }
-    const bool fin = (in && left <= 0x1p-19f) || hi - lo <= 0x1p-22f;
-    before = true;
+    const bool fin = (in && whole && left <= 0x1p-19f) || hi - lo <= 0x1p-22f;
+    before = whole;
     g_before = s.g;
     f_before = f;
     tau_before = tau;

@@ -103,7 +103,7 @@ int main() {
   bool good = true;
   printf("ok so far\n");  // (the line by line report follows)
   for (float alpha : alphas)
-    for (int start = 0; start < 2; ++start) {
+    for (int start = 0; start < 3; ++start) {
       Seen seen;
       for (float deviation : {0.3f, 1.0f, 5.0f, 15.0f, 40.0f, 1000.0f})
         for (int cluster : {1, 1, 8, 290})
@@ -121,7 +121,7 @@ int main() {
       rows += seen.rows;
       good = good && seen.worst <= 0x1p-19 + 0x1p-22 && seen.most < 24;
     }
-  for (int start = 0; start < 2; ++start) good = good && mean2[start] <= 1.5 * mean15[start];
+  for (int start = 0; start < 3; ++start) good = good && mean2[start] <= 1.5 * mean15[start];
   printf("%s %ld rows\n", good ? "ok" : "failed:", rows);
   return good ? 0 : 1;
 }
