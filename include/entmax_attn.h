@@ -297,8 +297,8 @@ size_t entmax_scale_proj_workspace_bytes(const entmax_scale_proj_params* p);
  * overlap in time (two streams, two captured graphs replayed together) need one each.
  */
 typedef struct {
-  int32_t nseq, T;              /* sequences; rows of Q and O (packed: of K and V too) */
-  int32_t Hq, Hkv, D;           /* Hq a multiple of Hkv; D in {64, 128} */
+  int32_t nseq, T;              /* sequences, at most 2^20; rows of Q and O (packed: of K and V too), at most 2^26 */
+  int32_t Hq, Hkv, D;           /* Hq a multiple of Hkv, at most 4096; D in {64, 128} */
   int32_t dtype;                /* ENTMAX_ATTN_BF16 or ENTMAX_ATTN_FP32: type of Q, K, V, O */
   int32_t causal, scale_layout, logn_mode, bias_mode; /* as in entmax_attn_params */
   int32_t path;                 /* 0: automatic; 1: tiled kernel only (test aid) */
@@ -330,7 +330,7 @@ size_t entmax_seq_workspace_bytes(const entmax_seq_params* p);
  * cache (a page that two sequences append to) leave either's bytes there.
  */
 typedef struct {
-  int32_t nseq, T, Hq, Hkv, D, dtype;
+  int32_t nseq, T, Hq, Hkv, D, dtype;  /* at most 2^20, 2^26 - 4, 4096, 4096 */
   int32_t page_size, num_pages, max_pages;
   int32_t rot, interleaved;     /* rot: a multiple of 16, 0 .. D */
   int64_t q_stride_t, q_stride_h, qo_stride_t, qo_stride_h;

@@ -28,7 +28,7 @@ struct AppendArgs {
   long long q_st, q_sh, qo_st, qo_sh, k_st, k_sh, v_st, v_sh, kc_sp, kc_sh, kc_sn, vc_sp, vc_sh, vc_sn;  // bytes
 };
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = kThreads;
 constexpr int kAppendPer = 4;      // units of a thread under way at a time
 
 // TB: tokens of a workgroup
@@ -190,13 +190,11 @@ inline bool off4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) !
 
 template <typename T, int D>
 void launch_append(const AppendArgs& a, hipStream_t st) {
-  // One token a workgroup while that leaves the chip room, then four, whose rows are under way together.  64 tokens x 24 heads of 128: 4.1 us
-  // with one, 5.7 with four; 13300 tokens of them: 36.4 us with one, 32.8 with four (5.0 TB/s
-  // read and written; a large copy reaches 5.15).
-  if (a.T <= 2048)
-    hipLaunchKernelGGL((cache_append_kernel<T, D, 1>), dim3((unsigned)a.T), dim3(kAppendThreads), 0, st, a);
+  const dim3 grid((unsigned)append_workgroups(a.T));
+  if (append_tokens(a.T) == 1)
+    hipLaunchKernelGGL((cache_append_kernel<T, D, 1>), grid, dim3(kAppendThreads), 0, st, a);
   else
-    hipLaunchKernelGGL((cache_append_kernel<T, D, 4>), dim3((unsigned)((a.T + 3) / 4)), dim3(kAppendThreads), 0, st, a);
+    hipLaunchKernelGGL((cache_append_kernel<T, D, 4>), grid, dim3(kAppendThreads), 0, st, a);
 }
 
 }  // namespace
