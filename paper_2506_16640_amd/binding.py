@@ -560,8 +560,8 @@ def paged_attn_fwd(q, k_cache, v_cache, cu_seqlens, kv_len, page_table, max_new=
     q [T,Hq,D]: the new tokens of all sequences, rows cu_seqlens[s] .. cu_seqlens[s+1]-1 those of sequence s; k_cache, v_cache
     [num_pages,Hkv,page_size,D]; kv_len [nseq]: keys of each sequence, new ones included; page_table [nseq,max_pages]; all int32 on the GPU.
     max_new, max_keys: bounds that no sequence passes (default: those of the shapes; close ones save workspace and launches).
-    beta, gamma: fp32 [Hq] or [Hq,T] or None; alibi_slopes: fp32 [Hq] or None.  Returns out [T,Hq,D]; rows that no sequence owns are left
-    as they are (zero in a tensor made here)."""
+    beta, gamma: fp32 [Hq] or [Hq,T] or None; alibi_slopes: fp32 [Hq] or None.  Returns out [T,Hq,D], which must not share
+    memory with q or the cache; rows that no sequence owns are left as they are (zero in a tensor made here)."""
     nseq, p = _paged_params(q, k_cache, v_cache, page_table, max_new, max_keys, alpha, beta, gamma, delta, causal, logn_mode, alibi_slopes,
                             bias_mode, path, out)
     _int_array("cu_seqlens", cu_seqlens, q, nseq + 1)

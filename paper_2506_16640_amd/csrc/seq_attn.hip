@@ -33,6 +33,7 @@ int seq_fwd(const SeqCall& c, bool paged, size_t workspace_bytes) {
   if (misaligned(c.Q) || misaligned(c.K) || misaligned(c.V) || misaligned(c.O) || misaligned(c.ws)) return ENTMAX_ATTN_MISALIGNED;
   if (off4(c.cu) || off4(c.kv_len) || off4(c.table) || off4(c.beta) || off4(c.gamma) || off4(c.slopes)) return ENTMAX_ATTN_MISALIGNED;
   if (workspace_bytes < seq_workspace_bytes_of(p)) return ENTMAX_ATTN_WORKSPACE_TOO_SMALL;
+  if (!seq_output_apart(p, c.Q, c.K, c.V, c.O)) return ENTMAX_ATTN_INVALID_ARG;
   if (p->dtype == ENTMAX_ATTN_BF16) return p->D == 64 ? run_seq<bf16_t, 64>(c) : run_seq<bf16_t, 128>(c);
   return p->D == 64 ? run_seq<float, 64>(c) : run_seq<float, 128>(c);
 }

@@ -2,6 +2,7 @@
 // sequences, paged cache).  Plain C++, no HIP types.
 #pragma once
 #include "host_layout.h"
+#include "seq_overlap.h"
 
 namespace entmax {
 
@@ -100,6 +101,21 @@ inline int check_append_params(const entmax_append_params* p) {
   if (p->kc_stride_n < p->D || p->vc_stride_n < p->D) return ENTMAX_ATTN_INVALID_ARG;
   if (p->Hq > 0 && (p->qo_stride_t < p->D || (p->Hq > 1 && p->qo_stride_h < p->D))) return ENTMAX_ATTN_INVALID_ARG;
   return ENTMAX_ATTN_OK;
+}
+
+// Of an attention call with checked parameters: whether O's rows are apart from each other and from what is read.  (A block of rows may be finished twice, by two
+// kernels that both read its queries; other blocks read the keys at any time.)
+inline bool seq_output_apart(const entmax_seq_params* p, const void* Q, const void* K, const void* V, const void* O) {
+  const int64_t es = p->dtype == ENTMAX_ATTN_BF16 ? 2 : 4;
+  const RowSet o{O, {p->T, p->Hq, 1}, {p->o_stride_t * es, p->o_stride_h * es, 0}, p->D * es};
+  const RowSet q{Q, {p->T, p->Hq, 1}, {p->q_stride_t * es, p->q_stride_h * es, 0}, p->D * es};
+  RowSet k{K, {p->T, p->Hkv, 1}, {p->k_stride_n * es, p->k_stride_h * es, 0}, p->D * es};
+  RowSet v{V, {p->T, p->Hkv, 1}, {p->v_stride_n * es, p->v_stride_h * es, 0}, p->D * es};
+  if (p->page_size != 0) {
+    k = RowSet{K, {p->num_pages, p->Hkv, p->page_size}, {p->k_stride_p * es, p->k_stride_h * es, p->k_stride_n * es}, p->D * es};
+    v = RowSet{V, {p->num_pages, p->Hkv, p->page_size}, {p->v_stride_p * es, p->v_stride_h * es, p->v_stride_n * es}, p->D * es};
+  }
+  return rows_apart(o) && !rows_meet(o, q) && !rows_meet(o, k) && !rows_meet(o, v);
 }
 
 // Paged sequences with at most this many folded rows (new tokens x heads of a group) go to the kernels that split the keys.

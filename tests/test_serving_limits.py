@@ -1,7 +1,9 @@
 """Sizes and layouts that the serving entry points refuse or take at their limits, before anything reaches a GPU."""
+import ctypes
 import os
 
 import pytest
+import torch
 
 from tests.test_sanitize_host import ROOT, _build_and_run
 from tests.test_serving_refusals import app, b, call_append, call_packed, call_paged, packed, seq  # noqa: F401
@@ -21,3 +23,58 @@ def test_many_key_heads_without_queries(b, Hkv):  # noqa: F811
 
 def test_append_of_more_tokens_than_a_launch_holds(b):  # noqa: F811
     assert call_append(b, app(b, T=1 << 26)) == -2
+
+
+def test_overlap_check_under_sanitizers(tmp_path):
+    out = _build_and_run(tmp_path, "g++", [os.path.join(ROOT, "tests", "sanitize", "overlap_check.cc")],
+                         ["-std=c++17", "-I", os.path.join(ROOT, "paper_2506_16640_amd", "csrc")])
+    assert int(out.split()[1]) > 1000
+
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="made-up addresses must not reach a GPU")
+AT = 1 << 32  # (addresses that nothing looks at before a GPU is asked for)
+
+
+def _at(x):
+    return ctypes.c_void_p(AT + x)
+
+
+def _refused(rc):
+    assert rc == -1
+
+
+def _passed(rc):  # the checks; without a GPU the launch fails
+    assert rc not in (-1, -2, -3, -4)
+
+
+@no_gpu
+def test_outputs_that_meet_what_is_read(b):  # noqa: F811
+    far = dict(Q=_at(0), K=_at(1 << 24), V=_at(2 << 24), O=_at(3 << 24))
+    T, token = 100, 512 * 2
+    # the queries, a token or a head further, their last row
+    for x in (0, token, 64 * 2, (T - 1) * token):
+        _refused(call_paged(b, seq(b), **dict(far, O=_at(x))))
+        _refused(call_packed(b, packed(b), **dict(far, O=_at(x))))
+    for name, base in (("K", 1), ("V", 2)):
+        _refused(call_paged(b, seq(b), **dict(far, O=_at((base << 24) + 64))))
+        _refused(call_packed(b, packed(b), **dict(far, O=_at(base << 24))))
+    # rows of O on top of each other
+    _refused(call_paged(b, seq(b, o_stride_t=64, o_stride_h=64), **far))
+    _refused(call_paged(b, seq(b, o_stride_t=512, o_stride_h=512), **far))
+
+
+@no_gpu
+def test_outputs_beside_what_is_read(b):  # noqa: F811
+    far = dict(Q=_at(0), K=_at(1 << 24), V=_at(2 << 24), O=_at(3 << 24))
+    _passed(call_paged(b, seq(b), **far))
+    _passed(call_packed(b, packed(b), **far))
+    _passed(call_paged(b, seq(b), **dict(far, O=_at(100 * 1024))))
+    # queries and output side by side in rows of one tensor, head by head in one tensor, halves of every row of one
+    for st, sh, off in ((1024, 64, 512), (64, 64 * 200, 64 * 100), (1024, 128, 64)):
+        p = seq(b, q_stride_t=st, o_stride_t=st, q_stride_h=sh, o_stride_h=sh)
+        _passed(call_paged(b, p, **dict(far, O=_at(2 * off))))
+        _refused(call_paged(b, p, **dict(far, O=_at(2 * (off - 8)))))
+    # queries, keys, values and output of a packed call in one tensor [T, 8 + 2 + 2 + 8, 64]
+    p = packed(b, q_stride_t=1280, o_stride_t=1280, k_stride_n=1280, v_stride_n=1280)
+    _passed(call_packed(b, p, Q=_at(0), K=_at(8 * 128), V=_at(10 * 128), O=_at(12 * 128)))
+    _refused(call_packed(b, p, Q=_at(0), K=_at(8 * 128), V=_at(10 * 128), O=_at(11 * 128)))
