@@ -326,7 +326,8 @@ size_t entmax_seq_workspace_bytes(const entmax_seq_params* p);
  *     Qout = R_P Q,   K page = R_P K,   V page = V
  * where R_P turns the pairs of the first `rot` features of every head: (x, y) -> (x cos - y sin, y cos + x sin) by the angle
  * P inv_freq[i].  Pair i is features (i, i + rot / 2), or (2 i, 2 i + 1) if `interleaved`.  Angles are formed in 64 bits.
- *   Q, Qout: [T, Hq, D], NULL together (Hq = 0) if there is nothing to rotate; Qout may be Q.  K, V: [T, Hkv, D].
+ *   Q, Qout: [T, Hq, D], NULL together (Hq = 0) if there is nothing to rotate; Qout may be Q, strides and all.  K, V: [T, Hkv, D].
+ *   Else the rows of Qout and of the caches must not meet each other, or those of Q, K, V: refused as in the attention.
  *   inv_freq: fp32 [rot / 2], ignored (may be NULL) for rot = 0.
  * A sequence with kv_len < n, or more keys than max_pages * page_size, is left out.  Two tokens with the same place in the
  * cache (a page that two sequences append to) leave either's bytes there.

@@ -212,6 +212,7 @@ extern "C" int entmax_cache_append(const entmax_append_params* p, const void* Q,
   if (off16(Q) || off16(K) || off16(V) || off16(Qout) || off16(Kcache) || off16(Vcache) || off4(cu_seqlens) || off4(kv_len) ||
       off4(page_table) || off4(inv_freq))
     return ENTMAX_ATTN_MISALIGNED;
+  if (!append_outputs_apart(p, Q, K, V, Qout, Kcache, Vcache)) return ENTMAX_ATTN_INVALID_ARG;
   AppendArgs a;
   a.nseq = p->nseq;
   a.T = p->T;

@@ -118,6 +118,28 @@ inline bool seq_output_apart(const entmax_seq_params* p, const void* Q, const vo
   return rows_apart(o) && !rows_meet(o, q) && !rows_meet(o, k) && !rows_meet(o, v);
 }
 
+// Of an append call with checked parameters: whether what it writes is apart in itself and from what it reads; the rotated queries may take the queries' place
+// (a thread writes what it has read).
+inline bool append_outputs_apart(const entmax_append_params* p, const void* Q, const void* K, const void* V, const void* Qout, const void* Kcache, const void* Vcache) {
+  const int64_t es = p->dtype == ENTMAX_ATTN_BF16 ? 2 : 4, row = p->D * es;
+  auto rows = [&](const void* x, int heads, int64_t st, int64_t sh) { return RowSet{x, {p->T, heads, 1}, {st * es, sh * es, 0}, row}; };
+  auto cache = [&](const void* x, int64_t sp, int64_t sh, int64_t sn) {
+    return RowSet{x, {p->num_pages, p->Hkv, p->page_size}, {sp * es, sh * es, sn * es}, row};
+  };
+  const RowSet out[3] = {rows(Qout, p->Hq, p->qo_stride_t, p->qo_stride_h), cache(Kcache, p->kc_stride_p, p->kc_stride_h, p->kc_stride_n),
+                         cache(Vcache, p->vc_stride_p, p->vc_stride_h, p->vc_stride_n)};
+  const RowSet in[3] = {rows(Q, p->Hq, p->q_stride_t, p->q_stride_h), rows(K, p->Hkv, p->k_stride_t, p->k_stride_h),
+                        rows(V, p->Hkv, p->v_stride_t, p->v_stride_h)};
+  for (int a = 0; a < 3; ++a) {
+    if (!rows_apart(out[a])) return false;
+    for (int c = a + 1; c < 3; ++c)
+      if (rows_meet(out[a], out[c])) return false;
+    for (int c = 0; c < 3; ++c)
+      if (!(a == 0 && c == 0 && same_rows(out[0], in[0])) && rows_meet(out[a], in[c])) return false;
+  }
+  return true;
+}
+
 // Paged sequences with at most this many folded rows (new tokens x heads of a group) go to the kernels that split the keys.
 // 16 sequences of 2500 to 7000 keys, 16 query heads on 4 of 128 features: with 20 folded rows 40 us there and 74 us by blocks of 128 rows, with 64
 // rows 70 us there and 85 us by blocks; with 68 rows (by blocks) 87 us.

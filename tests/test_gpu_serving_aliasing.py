@@ -46,3 +46,19 @@ def test_output_in_the_cache(binding):
         binding.paged_attn_fwd(p.q.cuda(), kc, vc, torch.tensor(p.cu, dtype=torch.int32).cuda(), torch.tensor([40], dtype=torch.int32).cuda(),
                                p.table.cuda(), out=out, **p.gpu_kw())
     assert torch.equal(kc, p.kc.cuda())
+
+
+def test_caches_in_one_tensor(binding):
+    """Keys and values of a page together; a cache whose heads or pages are one and the same is refused."""
+    p = Problem([(3, 40), (1, 17), (20, 20)], seed=53)
+    gen = torch.Generator().manual_seed(54)
+    k, v = (torch.randn(p.T, p.Hkv, p.D, generator=gen).to(BF16).cuda() for _ in range(2))
+    cu, kv = torch.tensor(p.cu, dtype=torch.int32).cuda(), torch.tensor([L for _, L in p.lens], dtype=torch.int32).cuda()
+    kc, vc = p.kc.cuda(), p.vc.cuda()
+    binding.cache_append(k, v, kc, vc, cu, kv, p.table.cuda())
+    both = torch.stack([p.kc, p.vc], 1).cuda()
+    binding.cache_append(k, v, both[:, 0], both[:, 1], cu, kv, p.table.cuda())
+    assert torch.equal(both[:, 0], kc) and torch.equal(both[:, 1], vc)
+    for a, b in ((kc, kc), (kc[:, :1].expand(-1, 2, -1, -1), vc), (kc, vc[:1].expand(p.pages, -1, -1, -1)), (both[:, 0], both[:, 0])):
+        with pytest.raises(binding.EntmaxAttnError):
+            binding.cache_append(k, v, a, b, cu, kv, p.table.cuda())

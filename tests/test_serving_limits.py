@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests.test_sanitize_host import ROOT, _build_and_run
-from tests.test_serving_refusals import app, b, call_append, call_packed, call_paged, packed, seq  # noqa: F401
+from tests.test_serving_refusals import NULL, app, b, call_append, call_packed, call_paged, packed, seq  # noqa: F401
 
 
 def test_append_checks_under_sanitizers(tmp_path):
@@ -78,3 +78,34 @@ def test_outputs_beside_what_is_read(b):  # noqa: F811
     p = packed(b, q_stride_t=1280, o_stride_t=1280, k_stride_n=1280, v_stride_n=1280)
     _passed(call_packed(b, p, Q=_at(0), K=_at(8 * 128), V=_at(10 * 128), O=_at(12 * 128)))
     _refused(call_packed(b, p, Q=_at(0), K=_at(8 * 128), V=_at(10 * 128), O=_at(11 * 128)))
+
+
+def _append_at(**kw):
+    base = dict(Q=_at(0), K=_at(1 << 24), V=_at(2 << 24), Qo=_at(3 << 24), Kc=_at(4 << 24), Vc=_at(5 << 24))
+    return dict(base, **{k: _at(x) for k, x in kw.items()})
+
+
+@no_gpu
+def test_appends_on_top_of_something(b):  # noqa: F811
+    cases = [({}, dict(Qo=128)), ({}, dict(Qo=1 << 24)), ({}, dict(Qo=2 << 24)), ({}, dict(Qo=4 << 24)), ({}, dict(Kc=5 << 24)), ({}, dict(Kc=0)),
+             ({}, dict(Vc=1 << 24)), ({}, dict(Kc=1 << 24)), ({}, dict(Vc=(4 << 24) + 4096)),
+             (dict(qo_stride_t=576), dict(Qo=0)),  # the queries' place, but other strides
+             (dict(kc_stride_p=0), {}), (dict(kc_stride_h=0), {}), (dict(vc_stride_h=512), {}), (dict(qo_stride_t=64), {})]
+    for kw, at in cases:
+        _refused(call_append(b, app(b, **kw), **_append_at(**at)))
+
+
+@no_gpu
+def test_appends_beside_something(b):  # noqa: F811
+    _passed(call_append(b, app(b), **_append_at()))
+    _passed(call_append(b, app(b), **_append_at(Qo=0)))
+    # a fused projection rotated in place: [T, 8 + 2 + 2, 64]
+    p = app(b, q_stride_t=768, qo_stride_t=768, k_stride_t=768, v_stride_t=768)
+    _passed(call_append(b, p, **_append_at(Q=0, Qo=0, K=8 * 128, V=10 * 128)))
+    _refused(call_append(b, p, **_append_at(Q=0, Qo=128, K=8 * 128, V=10 * 128)))
+    # keys and values of a page together: [pages, 2, 2, 16, 64]; token by token: [pages, 16, 2, 2, 64]
+    _passed(call_append(b, app(b, kc_stride_p=4096, vc_stride_p=4096), **_append_at(Vc=(4 << 24) + 4096)))
+    p = app(b, kc_stride_p=4096, vc_stride_p=4096, kc_stride_n=256, vc_stride_n=256, kc_stride_h=64, vc_stride_h=64)
+    _passed(call_append(b, p, **_append_at(Vc=(4 << 24) + 256)))
+    _passed(call_append(b, app(b, num_pages=1, kc_stride_p=0, vc_stride_p=0), **_append_at()))
+    _passed(call_append(b, app(b, Hq=0), **dict(_append_at(), Q=NULL, Qo=NULL)))
