@@ -25,7 +25,7 @@ int seq_fwd(const SeqCall& c, bool paged, size_t workspace_bytes) {
   if (paged != (p->page_size != 0)) return ENTMAX_ATTN_INVALID_ARG;
   if (p->nseq == 0 || p->T == 0 || p->max_new == 0) return ENTMAX_ATTN_OK;
   if (!c.Q || !c.O || !c.cu || !c.ws) return ENTMAX_ATTN_INVALID_ARG;
-  if (paged && (!c.kv_len || !c.table)) return ENTMAX_ATTN_INVALID_ARG;
+  if (paged && (!c.kv_len || (p->max_keys > 0 && !c.table))) return ENTMAX_ATTN_INVALID_ARG;  // (no keys: nothing is looked up)
   // (a cache without pages has no keys that could be read: every page number is a hole, and holes are read from page 0)
   if (paged && p->num_pages == 0 && p->max_keys > 0) return ENTMAX_ATTN_INVALID_ARG;
   if (p->max_keys > 0 && (!c.K || !c.V)) return ENTMAX_ATTN_INVALID_ARG;

@@ -109,3 +109,12 @@ def test_appends_beside_something(b):  # noqa: F811
     _passed(call_append(b, p, **_append_at(Vc=(4 << 24) + 256)))
     _passed(call_append(b, app(b, num_pages=1, kc_stride_p=0, vc_stride_p=0), **_append_at()))
     _passed(call_append(b, app(b, Hq=0), **dict(_append_at(), Q=NULL, Qo=NULL)))
+
+
+@no_gpu
+def test_a_cache_without_keys(b):  # noqa: F811
+    far = dict(Q=_at(0), O=_at(3 << 24))
+    p = seq(b, max_pages=0, max_keys=0)
+    _passed(call_paged(b, p, table=NULL, **far))
+    _passed(call_paged(b, seq(b, num_pages=0, max_pages=0, max_keys=0), table=NULL, K=NULL, V=NULL, **far))
+    _refused(call_paged(b, seq(b, max_keys=16), table=NULL, **far))
