@@ -389,6 +389,7 @@ _lib.entmax_cache_append.restype = ctypes.c_int
 _lib.entmax_cache_append.argtypes = [_vp] * 12
 
 _DTYPES = {torch.bfloat16: 0, torch.float32: 1}
+_INT32_MOST = 2 ** 31 - 1  # (more keys than any call takes: refused like other large bounds)
 
 
 def _rows_of(name, t):
@@ -512,7 +513,7 @@ def _paged_params(q, k_cache, v_cache, page_table, max_new, max_keys, *args):
             raise ValueError("v_cache must have the shape of k_cache")
     nseq, max_pages = _page_table(page_table, q)
     return nseq, _seq_params(q, rows, shape[1], nseq, (shape[2], shape[0], max_pages), rows[0] if max_new is None else max_new,
-                             max_pages * shape[2] if max_keys is None else max_keys, k_strides, v_strides, *args)
+                             min(max_pages * shape[2], _INT32_MOST) if max_keys is None else max_keys, k_strides, v_strides, *args)
 
 
 def _packed_params(q, k, v, nseq, max_len, *args):

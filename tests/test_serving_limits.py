@@ -118,3 +118,12 @@ def test_a_cache_without_keys(b):  # noqa: F811
     _passed(call_paged(b, p, table=NULL, **far))
     _passed(call_paged(b, seq(b, num_pages=0, max_pages=0, max_keys=0), table=NULL, K=NULL, V=NULL, **far))
     _refused(call_paged(b, seq(b, max_keys=16), table=NULL, **far))
+
+
+def test_a_page_table_wider_than_any_call(b):  # noqa: F811
+    q, cache = torch.zeros(1, 1, 64, dtype=torch.bfloat16), torch.zeros(1, 1, 65536, 64, dtype=torch.bfloat16)
+    table = torch.zeros(1, 40000, dtype=torch.int32)  # 2.6e9 places
+    cu, kv = torch.tensor([0, 1], dtype=torch.int32), torch.tensor([5], dtype=torch.int32)
+    with pytest.raises(ValueError, match="GPU"):  # (no GPU here: the last check)
+        b.paged_attn_fwd(q, cache, cache, cu, kv, table)
+    assert b._lib.entmax_seq_workspace_bytes(b._paged_params(q, cache, cache, table, None, None, *b._DEFAULTS)[1]) == 0
