@@ -397,7 +397,7 @@ __global__ __launch_bounds__((SeqTiledCfg<T, D, WIDE>::NT), (SeqTiledCfg<T, D, W
   const float lo0 = lo, ref0 = ref;  // blocks without a term above lo0 are zero for good
 
   // ------------------------------------------------------------ 2. threshold
-  SeqSearch<AM> search{tau, lo, hi, (float)q.lim, 0.f, 0.f, 0.f, false};
+  SeqSearch<AM> search{tau, lo, hi, (float)q.lim, 0.f, 0.f, 0.f, false, false};
   bool done = !live;
   int iter = 0, more;
   auto sweep = [&](auto first_) {

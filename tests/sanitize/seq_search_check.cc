@@ -76,7 +76,7 @@ static void row(float alpha, int n, int cluster, float deviation, int start, See
   }
   vector<float> w(n);
   for (int i = 0; i < n; ++i) w[i] = y[i] - ref;
-  SeqSearch<AM> s{tau, lo, hi, (float)n, 0.f, 0.f, 0.f, false};
+  SeqSearch<AM> s{tau, lo, hi, (float)n, 0.f, 0.f, 0.f, false, false};
   int sweeps = 0;
   bool done = false;
   while (!done && sweeps < 48) {
