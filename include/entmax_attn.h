@@ -296,7 +296,8 @@ size_t entmax_scale_proj_workspace_bytes(const entmax_scale_proj_params* p);
  * Packed: K, V [T, Hkv, D]; every sequence has as many keys as tokens; page_size, num_pages, max_pages and the page strides must be
  * 0, and max_keys = max_new.
  * Calls need entmax_seq_workspace_bytes(p) bytes of 256-byte aligned workspace whose contents do not matter; calls that may
- * overlap in time (two streams, two captured graphs replayed together) need one each.
+ * overlap in time (two streams, two captured graphs replayed together) need one each.  Paged calls need mostly room for scores, 4 bytes for each of
+ * nseq x Hkv x min(max_new Hq / Hkv, 64) x max_keys: bounds close to what the sequences have keep it small.  max_keys is at most 2^22.
  */
 typedef struct {
   int32_t nseq, T;              /* sequences, at most 2^20; rows of Q and O (packed: of K and V too), at most 2^26 */

@@ -435,7 +435,7 @@ __global__ __launch_bounds__(NT) void seq_solve_kernel(SeqDecodeArgs A, int stri
   }
 }
 
-// Keys of a wave's tile and bytes of LDS for it: two tiles of V per wave
+// Keys of a wave's tile of V and its bytes: one tile per wave in LDS, the next one waits in registers
 template <typename T, int D>
 struct SeqPvCfg {
   static constexpr int KT = 32;
@@ -466,7 +466,7 @@ __device__ __forceinline__ f32x4_t get_part(const float* at) {
 // piece of the keys; the waves' sums are added in their order, and the workgroup that comes last adds up the pieces in theirs.
 template <typename T, int D, int AM, int NQB>
 __global__ __launch_bounds__(kThreads) void seq_pv_kernel(SeqDecodeArgs A) {
-  constexpr int NM = D / 32, KT = 32;
+  constexpr int NM = D / 32, KT = SeqPvCfg<T, D>::KT;
   using Vals = SeqValues<T, D, KT>;
   __shared__ __attribute__((aligned(16))) char tiles[kWaves * SeqPvCfg<T, D>::kTileBytes];
   __shared__ int last;

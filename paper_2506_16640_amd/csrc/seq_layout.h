@@ -165,7 +165,7 @@ inline int seq_run(long long heads, int nblk, int rows) {
 }
 
 // The tiled kernel: below so many groups of 128 rows all waves of a compute unit go to each group, from there on small workgroups, whose starts and
-// waits overlap.  Some 400 groups of 300 to 6000 keys, D 64: 175 us wide, 317 us small; about 900 of 300 to 2000 keys, D 128: 239 us wide, 181 us small.
+// waits overlap.  Some 400 groups of 300 to 6000 keys, D 64: 182 us wide, 325 us small; about 900 of 300 to 2000 keys, D 128: 205 us wide, 189 us small.
 constexpr long long kSeqWideBelow = 512;
 
 struct SeqLayout {

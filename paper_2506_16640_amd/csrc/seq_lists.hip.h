@@ -242,7 +242,7 @@ constexpr int kFinishSlots = 24;    // groups of a row that an octet can hold (e
 constexpr int kFinishSupport = 32;  // support entries of a row noted before their values are gathered
 constexpr int kScanList = 256;      // candidates of a row that all octets look through together
 // The rows that the finish kernel takes the long way instead of giving their whole block to the tiled kernel.  Blocks of 128 rows against 32000 keys,
-// alpha 1.7, no scale: 59 us here and nothing left for the tiled kernel; with none taken 51 us here and 1430 us there.  Where blocks are dense
+// alpha 1.7, no scale: 59 us here and nothing left for the tiled kernel; with none taken 51 us here and 1720 us there.  Where blocks are dense
 // anyway it costs time here (prompts of 300 to 2000 tokens without a scale: 46 us for 36; prompts with scales: 66 us for 62).  Rows looked through key by
 // key are rarer: with none of them the first case leaves 4 us more to the tiled kernel, and with groups up to 200 instead of 40 the prompts without a
 // scale cost 53 us here.

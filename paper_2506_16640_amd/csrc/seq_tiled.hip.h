@@ -9,8 +9,8 @@
 //      elements, each lane gets a column), so that no transposed copy of V exists anywhere.
 // A block's sweeps follow one another, and few blocks may be left to this kernel: so a block has 8 or 16 waves, and KS of them share the
 // keys of each tile for the same 32 rows (their sums are added in their order).
-// Measured: 6 prompts of 300 to 2000 tokens, 4 x 4 heads of 128, logits without a scale: 181 us, of it starts and ends 20, the first evaluation 36, later
-// ones 55, P V 70 (all sweeps bound by the vector work on the scores: the products are 10 us at the rate of a large one).
+// Measured: 6 prompts of 300 to 2000 tokens, 4 x 4 heads of 128, logits without a scale: 189 us, of it starts and ends 18, the first evaluation 35, later
+// ones 61, P V 74 (all sweeps bound by the vector work on the scores: the products are 10 us at the rate of a large one).
 #pragma once
 #include "fwd.hip.h"
 #include "seq.hip.h"
