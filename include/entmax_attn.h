@@ -292,7 +292,7 @@ size_t entmax_scale_proj_workspace_bytes(const entmax_scale_proj_params* p);
  *   alibi_slopes: NULL or fp32 [Hq], with bias_mode, as in entmax_attn_fwd.  n in (ln n)^gamma: logn_mode 0 the sequence's keys L,
  *   1 the keys the row sees (holes counted).
  * O's rows must not meet each other or those of Q, K, V (parts of one tensor beside each other do not): such calls are refused with INVALID_ARG, and so are
- * tensors of different strides whose ranges of memory meet.
+ * tensors of different strides unless one lies wholly in the gaps of the other.
  * Packed: K, V [T, Hkv, D]; every sequence has as many keys as tokens; page_size, num_pages, max_pages and the page strides must be
  * 0, and max_keys = max_new.
  * Calls need entmax_seq_workspace_bytes(p) bytes of 256-byte aligned workspace whose contents do not matter; calls that may

@@ -42,14 +42,37 @@ inline bool rows_apart(const RowSet& x) {
   return true;
 }
 
+// Whether a row of x (from axis order o[k] on) meets the bytes lo .. hi - 1, counted from x's first.  Rows that are not apart: taken as meeting.
+inline bool rows_reach(const RowSet& x, const int (&o)[3], int k, __int128 lo, __int128 hi) {
+  if (k == 3 || x.n[o[k]] <= 1) return lo < x.row && hi > 0;
+  const __int128 s = x.s[o[k]];
+  __int128 inner = x.row;
+  for (int e = k + 1; e < 3; ++e) inner += x.n[o[e]] > 1 ? (__int128)(x.n[o[e]] - 1) * x.s[o[e]] : 0;
+  if (s < inner) return true;
+  // the blocks i s .. i s + inner - 1 that overlap the bytes; of three in a row the middle one begins inside them
+  __int128 first = lo < inner ? 0 : (lo - inner) / s + 1, last = hi <= 0 ? -1 : (hi - 1) / s;
+  if (last > x.n[o[k]] - 1) last = x.n[o[k]] - 1;
+  if (last - first >= 2) return true;
+  for (__int128 i = first; i <= last; ++i)
+    if (rows_reach(x, o, k + 1, lo - i * s, hi - i * s)) return true;
+  return false;
+}
+
 // Whether rows of x meet rows of out, whose own are apart.  Exact where the two have the same strides (parts of one tensor) and x is no longer than out along
-// any axis; else they meet if one's range of memory meets the other's.
+// any axis; else they are taken as meeting unless one's rows leave free the whole range of memory of the other's.
 inline bool rows_meet(const RowSet& out, const RowSet& x) {
   if (out.empty() || x.empty()) return false;
   const uintptr_t a = reinterpret_cast<uintptr_t>(out.at), b = reinterpret_cast<uintptr_t>(x.at);
   if ((__int128)a + out.extent() <= (__int128)b || (__int128)b + x.extent() <= (__int128)a) return false;
-  for (int k = 0; k < 3; ++k)
-    if (x.row != out.row || x.n[k] > out.n[k] || (x.n[k] > 1 && x.s[k] != out.s[k])) return true;
+  bool alike = x.row == out.row;
+  for (int k = 0; k < 3; ++k) alike = alike && x.n[k] <= out.n[k] && (x.n[k] <= 1 || x.s[k] == out.s[k]);
+  if (!alike) {
+    int ox[3], oo[3];
+    x.order(ox);
+    out.order(oo);
+    const __int128 from = (__int128)a - (__int128)b;
+    return rows_reach(x, ox, 0, from, from + out.extent()) && rows_reach(out, oo, 0, -from, -from + x.extent());
+  }
   int o[3];
   out.order(o);
   // axis by axis from the largest stride: out's row i and x's row j meet if what is left of their distance is shorter than a row; the axes further in reach

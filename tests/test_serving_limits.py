@@ -127,3 +127,22 @@ def test_a_page_table_wider_than_any_call(b):  # noqa: F811
     with pytest.raises(ValueError, match="GPU"):  # (no GPU here: the last check)
         b.paged_attn_fwd(q, cache, cache, cu, kv, table)
     assert b._lib.entmax_seq_workspace_bytes(b._paged_params(q, cache, cache, table, None, None, *b._DEFAULTS)[1]) == 0
+
+
+def test_overlap_of_ranges_under_sanitizers(tmp_path):
+    out = _build_and_run(tmp_path, "g++", [os.path.join(ROOT, "tests", "sanitize", "overlap_ranges_check.cc")],
+                         ["-std=c++17", "-I", os.path.join(ROOT, "paper_2506_16640_amd", "csrc")])
+    assert int(out.split()[3]) > 1000
+
+
+@no_gpu
+def test_outputs_in_the_gaps_of_a_pool(b):  # noqa: F811
+    # pages of 4096 elements of keys (and values behind them) in blocks of 1 MB, the output between two of them
+    far = dict(Q=_at(1 << 28), K=_at(0), V=_at(8192))
+    p = seq(b, k_stride_p=1 << 19, v_stride_p=1 << 19)
+    _passed(call_paged(b, p, **dict(far, O=_at((3 << 20) + (1 << 16)))))
+    _refused(call_paged(b, p, **dict(far, O=_at((4 << 20) - (1 << 16)))))
+    p = app(b, kc_stride_p=1 << 19, vc_stride_p=1 << 19)
+    at = dict(_append_at(), Kc=_at(0), Vc=_at(8192), Q=_at(1 << 28))
+    _passed(call_append(b, p, **dict(at, Qo=_at((3 << 20) + (1 << 16)), K=_at((5 << 20) + (1 << 16)), V=_at((7 << 20) + (1 << 16)))))
+    _refused(call_append(b, p, **dict(at, Qo=_at((4 << 20) - (1 << 16)), K=_at((5 << 20) + (1 << 16)), V=_at((7 << 20) + (1 << 16)))))
