@@ -35,6 +35,13 @@ struct bf16_t {
   uint16_t bits;
 };
 
+// The bits of a float, out of the compiler's sight: where NaN is taken not to occur, it turns tests of the exponent's bits into comparisons that NaN fails.
+__device__ __forceinline__ uint32_t opaque_bits(float x) {
+  uint32_t b = __float_as_uint(x);
+  asm("" : "+v"(b));
+  return b;
+}
+
 // ---------------------------------------------------------------- fragments
 
 template <typename T>

@@ -152,7 +152,7 @@ struct SeqValues {
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        bad = bad || (__float_as_uint(f.lo[k]) & 0x7f800000u) == 0x7f800000u || (__float_as_uint(f.hi[k]) & 0x7f800000u) == 0x7f800000u;
+        bad = bad || (opaque_bits(f.lo[k]) & 0x7f800000u) == 0x7f800000u || (opaque_bits(f.hi[k]) & 0x7f800000u) == 0x7f800000u;
     }
     return bad;
   }
