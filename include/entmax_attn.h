@@ -346,6 +346,77 @@ int entmax_cache_append(const entmax_append_params* p, const void* Q, const void
                         const int32_t* kv_len, const int32_t* page_table, const float* inv_freq, void* Qout, void* Kcache,
                         void* Vcache, void* hip_stream);
 
+/*
+ * The plan of a serving step: pages for its new tokens, and where everything lies.  What entmax_cache_append and the attention calls read
+ * (cu_seqlens, kv_len, page_table) is made on the device from the number of new tokens of every sequence, so that a captured step needs nothing from the host.
+ *   in : new_len [nseq]; release [nseq] or NULL; kv_len [nseq] and free_count [1] as the step before left them
+ *   in and out: page_table [nseq, max_pages]; free_pages [num_pages]: the first free_count entries are pages that nobody has
+ *   out: kv_len_out [nseq], free_count_out [1] (may be kv_len, free_count themselves); cu_seqlens [nseq + 1]; for each of the T rows, or NULL:
+ *        slots (int64) its place in the cache, page * page_size + place in the page; positions, sequences (int32).  Rows behind the last
+ *        sequence get -1 in all three, a row on a page that is none (see above) gets slot -1.
+ *   - release[s] != 0: sequence s has ended.  The pages of its kv_len keys go on top of the free ones (in the order of the sequences; entries
+ *     that are no page are passed over, and what does not fit num_pages is dropped) and it begins again with no keys.
+ *   - New pages are taken from the top of the free ones, in the order of the sequences, and entered into page_table; other entries stay.
+ *   - A sequence gets all of its new tokens or none (its part of cu_seqlens is then empty, its kv_len stays): none if it would have more keys
+ *     than max_pages * page_size, if the pages that it and those before it ask for are more than there are (sequences that need no page go on),
+ *     or if its tokens and those of the ones before it are more than T.  Negative numbers of new tokens count as none.
+ * What is written must not meet other arguments, but for the two outputs that may be their inputs: else INVALID_ARG.
+ * entmax_plan_workspace_bytes(p) bytes of 256-byte aligned workspace; contents do not matter; calls that may overlap need one each.
+ */
+typedef struct {
+  int32_t nseq, T;  /* at most 2^20, 2^26 */
+  int32_t page_size, num_pages, max_pages; /* max_pages * page_size < 2^31 */
+} entmax_plan_params;
+
+int entmax_cache_plan(const entmax_plan_params* p, const int32_t* new_len, const int32_t* release, const int32_t* kv_len,
+                      const int32_t* free_count, int32_t* page_table, int32_t* free_pages, int32_t* kv_len_out, int32_t* free_count_out,
+                      int32_t* cu_seqlens, int64_t* slots, int32_t* positions, int32_t* sequences, void* workspace, size_t workspace_bytes,
+                      void* hip_stream);
+/* Workspace bytes of entmax_cache_plan; 0 if the parameters are invalid. Host-only. */
+size_t entmax_plan_workspace_bytes(const entmax_plan_params* p);
+
+/*
+ * Softmax attention over the paged cache: entmax_paged_attn_fwd in the limit alpha -> 1, p_ij = exp(s_ij - lse_i), lse_i = log sum_j exp(s_ij), for the
+ * heads and models that the sparse ones stand beside or are compared with.  Parameters, sequences, holes, scales and bias as there, with p->alpha = 1 and
+ * p->path = 0.  cap: 0, or c > 0 for scores c tanh(s / c); with bias_mode 1 the bias is added after that (c tanh(scale z / c) + b), with bias_mode 0 it
+ * is part of s.
+ *   lse: NULL, or [Hq, T] fp32: the rows' lse (-infinity where a row sees no key); rows that no sequence owns are left as they are.
+ * Keys that a row does not see do not influence it whatever they hold; O, lse must not meet each other or what is read (INVALID_ARG).
+ * Calls need entmax_softmax_workspace_bytes(p) bytes of 256-byte aligned workspace; calls that may overlap in time need one each.
+ */
+int entmax_paged_softmax_fwd(const entmax_seq_params* p, float cap, const void* Q, const void* K, const void* V, const int32_t* cu_seqlens,
+                             const int32_t* kv_len, const int32_t* page_table, const float* beta, const float* gamma,
+                             const float* alibi_slopes, void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Workspace bytes of entmax_paged_softmax_fwd; 0 if the parameters are invalid. Host-only. */
+size_t entmax_softmax_workspace_bytes(const entmax_seq_params* p);
+
+/*
+ * Sampling: one token of each row of logits [rows, vocab] (element type `dtype`, rows `stride` elements apart, any alignment of the elements' own),
+ * from random numbers that the caller brings.  With x the logits of a row, m the largest, w_i = exp((x_i - m) / temperature):
+ *   1. top_k = k > 0: the k tokens of largest x stay (of equal ones those of lower index)
+ *   2. top_p = p < 1: of these in falling order (equal ones by index) a token stays while the w of those before it add up to less than p times the
+ *      w of all that step 1 left; the first stays in any case
+ *   3. min_p = f > 0: those with w_i >= min(f, 1) stay
+ *   4. the token is the first, by index, up to and with which the w that are left add up to more than uniform times their sum
+ * Sums and w are of 64 bits.  temperature <= 0 (or NaN): the largest logit, of equal ones the first, whatever the filters; logprob 0.
+ *   temperature, top_p, min_p fp32 [rows], top_k int32 [rows]: NULL where not wanted (temperature 1).  A top_k <= 0 or >= vocab, top_p >= 1 or
+ *   NaN, min_p <= 0 or NaN leave all; top_p <= 0 leaves the first.  uniform: fp32 [rows] in [0, 1); others count as the nearest (NaN as 0).
+ *   token: int32 [rows].  logprob: NULL, or fp32 [rows]: log of the probability with which the token was drawn.
+ * Logits of -infinity and NaN are never drawn; those of +infinity share all the probability.  A row without any other: token -1, logprob -infinity.
+ * entmax_sample_workspace_bytes(p) bytes of 256-byte aligned workspace; contents do not matter; calls that may overlap in time need one each.
+ */
+typedef struct {
+  int32_t rows, vocab; /* at most 2^20, 2^22 */
+  int32_t dtype;
+  int64_t stride;      /* elements, at least vocab */
+} entmax_sample_params;
+
+int entmax_sample(const entmax_sample_params* p, const void* logits, const float* uniform, const float* temperature, const int32_t* top_k,
+                  const float* top_p, const float* min_p, int32_t* token, float* logprob, void* workspace, size_t workspace_bytes,
+                  void* hip_stream);
+/* Workspace bytes of entmax_sample; 0 if the parameters are invalid. Host-only. */
+size_t entmax_sample_workspace_bytes(const entmax_sample_params* p);
+
 /* Scratch bytes the forward (is_bwd = 0) or backward (is_bwd != 0) needs for
  * these parameters; 0 if the parameters are invalid. Host-only, no GPU call. */
 size_t entmax_attn_workspace_bytes(const entmax_attn_params* p, int is_bwd);

@@ -4,6 +4,7 @@ Argument marshalling only: torch supplies device memory and the stream, every
 step of the computation runs in the HIP kernels of lib/libentmax_attn.so.
 There is no fallback: if the library is missing, importing this module fails.
 """
+import collections
 import ctypes
 import os
 import struct
@@ -460,6 +461,12 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+def _array(name, t, ref, dtype, want):
+    """A contiguous tensor of one dimension of `want` elements on ref's device."""
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != want or not t.is_contiguous() or t.get_device() != ref.get_device():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on the device of the others" % (name, str(dtype)[6:], want))
+
+
 class _DeviceOf:
     """The GPU of a tensor as the current one, for calls from another one."""
 
@@ -634,3 +641,164 @@ def cache_append(k, v, k_cache, v_cache, cu_seqlens, kv_len, page_table, q=None,
     if rc != 0:
         raise EntmaxAttnError(rc)
     return q_out
+
+
+# ------------------------------------------------- serving: the plan of a step, softmax attention, sampling
+
+class PlanParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("nseq", "T", "page_size", "num_pages", "max_pages")]
+
+
+class SampleParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("stride", ctypes.c_int64)]
+
+
+_plan_bytes = struct.Struct("@5i")
+_sample_bytes = struct.Struct("@3i4xq")
+assert _plan_bytes.size == ctypes.sizeof(PlanParams) and _sample_bytes.size == ctypes.sizeof(SampleParams)
+
+_lib.entmax_cache_plan.restype = ctypes.c_int
+_lib.entmax_cache_plan.argtypes = [_vp] * 14 + [ctypes.c_size_t, _vp]
+_lib.entmax_plan_workspace_bytes.restype = ctypes.c_size_t
+_lib.entmax_plan_workspace_bytes.argtypes = [_vp]
+_lib.entmax_paged_softmax_fwd.restype = ctypes.c_int
+_lib.entmax_paged_softmax_fwd.argtypes = [_vp, ctypes.c_float] + [_vp] * 12 + [ctypes.c_size_t, _vp]
+_lib.entmax_softmax_workspace_bytes.restype = ctypes.c_size_t
+_lib.entmax_softmax_workspace_bytes.argtypes = [_vp]
+_lib.entmax_sample.restype = ctypes.c_int
+_lib.entmax_sample.argtypes = [_vp] * 10 + [ctypes.c_size_t, _vp]
+_lib.entmax_sample_workspace_bytes.restype = ctypes.c_size_t
+_lib.entmax_sample_workspace_bytes.argtypes = [_vp]
+
+# What cache_plan makes: cu_seqlens [nseq + 1], kv_len [nseq], free_count [1], and for each row of the step slots (int64), positions and sequences
+Plan = collections.namedtuple("Plan", "cu_seqlens kv_len free_count slots positions sequences workspace")
+
+
+def new_plan(nseq, rows, device="cuda"):
+    """Outputs and workspace of cache_plan for steps of `rows` rows; kv_len and free_count begin at zero."""
+    ints = lambda n: torch.zeros(n, dtype=torch.int32, device=device)  # noqa: E731
+    need = int(_lib.entmax_plan_workspace_bytes(_plan_bytes.pack(nseq, rows, 16, 0, 0)))
+    return Plan(ints(nseq + 1), ints(nseq), ints(1), torch.zeros(rows, dtype=torch.int64, device=device), ints(rows), ints(rows),
+                torch.empty(max(need, 256), dtype=torch.uint8, device=device))
+
+
+def cache_plan(new_len, kv_len, page_table, free_pages, free_count, page_size, plan, release=None):
+    """Pages and places in the cache for the new tokens of a step; fills and returns `plan` (new_plan; slots, positions, sequences may be None in it).
+    new_len, kv_len [nseq]: new tokens and cached keys of each sequence; release [nseq] or None: sequences with a number other than 0 have ended and
+    give their pages back first.  page_table [nseq,max_pages] and free_pages [num_pages], whose first free_count [1] entries are the free pages, are
+    updated.  kv_len and free_count may be the plan's own: the next step goes on from there.  All int32 on the GPU.  A sequence that does not
+    get its pages (or whose tokens do not fit the plan's rows) gets no rows; those behind the last sequence have -1 everywhere."""
+    nseq, max_pages = _page_table(page_table, new_len)
+    i32 = torch.int32
+    for name, t, want in (("new_len", new_len, nseq), ("kv_len", kv_len, nseq), ("release", release, nseq), ("free_count", free_count, 1),
+                          ("plan.cu_seqlens", plan.cu_seqlens, nseq + 1), ("plan.kv_len", plan.kv_len, nseq), ("plan.free_count", plan.free_count, 1)):
+        if t is not None:
+            _array(name, t, new_len, i32, want)
+        elif name != "release":
+            raise ValueError("%s is missing" % name)
+    _array("free_pages", free_pages, new_len, i32, free_pages.shape[0] if free_pages.dim() else -1)
+    rows = None
+    for name, t, dtype in (("plan.slots", plan.slots, torch.int64), ("plan.positions", plan.positions, i32), ("plan.sequences", plan.sequences, i32)):
+        if t is not None:
+            rows = t.shape[0] if rows is None and t.dim() else rows
+            _array(name, t, new_len, dtype, rows)
+    if rows is None:
+        raise ValueError("the plan needs slots, positions or sequences: their length is the number of rows")
+    w = plan.workspace
+    if w.dtype != torch.uint8 or not w.is_contiguous() or w.get_device() != new_len.get_device():
+        raise ValueError("plan.workspace must be a contiguous uint8 tensor on the device of the others")
+    p = _plan_bytes.pack(nseq, rows, page_size, free_pages.shape[0], max_pages)
+    with _DeviceOf(new_len) as stream:
+        rc = _lib.entmax_cache_plan(p, new_len.data_ptr(), _at(release), kv_len.data_ptr(), free_count.data_ptr(), page_table.data_ptr(),
+                                    free_pages.data_ptr(), plan.kv_len.data_ptr(), plan.free_count.data_ptr(), plan.cu_seqlens.data_ptr(),
+                                    _at(plan.slots), _at(plan.positions), _at(plan.sequences), w.data_ptr(), w.numel(), stream)
+    if rc != 0:
+        raise EntmaxAttnError(rc)
+    return plan
+
+
+_SOFTMAX_DEFAULTS = (1.0,) + _DEFAULTS[1:]
+
+
+def _softmax_workspace(params, device):
+    return torch.empty(max(int(_lib.entmax_softmax_workspace_bytes(params)), 256), dtype=torch.uint8, device=device)
+
+
+def new_softmax_workspace(q, k_cache, page_table, max_new=None, max_keys=None):
+    """Workspace for paged_softmax_fwd calls of these shapes and bounds, whatever their other arguments."""
+    return _softmax_workspace(_paged_params(q, k_cache, k_cache, page_table, max_new, max_keys, *_SOFTMAX_DEFAULTS)[1], q.device)
+
+
+def paged_softmax_fwd(q, k_cache, v_cache, cu_seqlens, kv_len, page_table, max_new=None, max_keys=None, cap=0.0, beta=None, gamma=None,
+                      delta=1.0, causal=True, logn_mode=0, alibi_slopes=None, bias_mode=0, out=None, lse=None, workspace=None):
+    """Softmax attention of new tokens over a paged cache: paged_attn_fwd in the limit alpha -> 1, with the same arguments and result.
+    cap: 0, or c > 0 for scores c tanh(s / c).  lse: optional fp32 [Hq,T] tensor that receives the logarithm of each row's sum of exponentials."""
+    nseq, p = _paged_params(q, k_cache, v_cache, page_table, max_new, max_keys, 1.0, beta, gamma, delta, causal, logn_mode, alibi_slopes,
+                            bias_mode, 0, out)
+    _int_array("cu_seqlens", cu_seqlens, q, nseq + 1)
+    _int_array("kv_len", kv_len, q, nseq)
+    if lse is not None:
+        _floats("lse", lse, q, (q.shape[1], q.shape[0]))
+    with _DeviceOf(q) as stream:
+        if out is None:
+            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)  # (rows that no sequence owns)
+        if workspace is None:
+            workspace = _softmax_workspace(p, q.device)
+        elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != q.get_device():
+            raise ValueError("workspace must be a contiguous uint8 tensor on the device of q")
+        rc = _lib.entmax_paged_softmax_fwd(p, cap, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cu_seqlens.data_ptr(), kv_len.data_ptr(),
+                                           page_table.data_ptr(), _at(beta), _at(gamma), _at(alibi_slopes), out.data_ptr(), _at(lse),
+                                           workspace.data_ptr(), workspace.numel(), stream)
+    if rc != 0:
+        raise EntmaxAttnError(rc)
+    return out
+
+
+def _sample_params(logits):
+    if logits.dim() != 2:
+        raise ValueError("logits must be [rows,vocab]")
+    if logits.dtype not in _DTYPES:
+        raise TypeError("logits must be bfloat16 or float32")
+    rows, vocab = logits.shape
+    stride = vocab
+    if rows and vocab:
+        if vocab > 1 and logits.stride(1) != 1:
+            raise ValueError("the last dimension of logits must be contiguous")
+        if rows > 1:
+            stride = logits.stride(0)
+    return rows, _sample_bytes.pack(rows, vocab, _DTYPES[logits.dtype], stride)
+
+
+def _sample_workspace(params, device):
+    return torch.empty(max(int(_lib.entmax_sample_workspace_bytes(params)), 256), dtype=torch.uint8, device=device)
+
+
+def new_sample_workspace(logits):
+    """Workspace for sample calls with logits of this shape and type."""
+    return _sample_workspace(_sample_params(logits)[1], logits.device)
+
+
+def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logprob=None, workspace=None):
+    """One token of each row of logits [rows,vocab] (bf16 or fp32, rows any stride apart) as int32 [rows], drawn with the random numbers uniform
+    (fp32 [rows] in [0,1)) after temperature, top_k, top_p and min_p in this order.  temperature, top_p, min_p: fp32 [rows], top_k: int32 [rows]; None, or a
+    row's top_k <= 0, top_p >= 1, min_p <= 0: not wanted; temperature <= 0: the largest logit.  Of equal logits the first is the larger.
+    logprob: optional fp32 [rows] tensor that receives the log of the probability with which the token was drawn.  -1 for rows without a token to
+    draw (all -infinity or NaN)."""
+    rows, p = _sample_params(logits)
+    f32, i32 = torch.float32, torch.int32
+    for name, t, dtype in (("uniform", uniform, f32), ("temperature", temperature, f32), ("top_k", top_k, i32), ("top_p", top_p, f32),
+                           ("min_p", min_p, f32), ("token", token, i32), ("logprob", logprob, f32)):
+        if t is not None:
+            _array(name, t, logits, dtype, rows)
+    with _DeviceOf(logits) as stream:
+        if token is None:
+            token = torch.empty(rows, dtype=i32, device=logits.device)
+        if workspace is None:
+            workspace = _sample_workspace(p, logits.device)
+        elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != logits.get_device():
+            raise ValueError("workspace must be a contiguous uint8 tensor on the device of logits")
+        rc = _lib.entmax_sample(p, logits.data_ptr(), uniform.data_ptr(), _at(temperature), _at(top_k), _at(top_p), _at(min_p), token.data_ptr(),
+                                _at(logprob), workspace.data_ptr(), workspace.numel(), stream)
+    if rc != 0:
+        raise EntmaxAttnError(rc)
+    return token

@@ -29,10 +29,11 @@ HIPCC_FLAGS = [
 def translation_units():
     """(object name, source, extra flags) of every unit of the library."""
     units = [("api", "entmax_attn.hip", []), ("scale_proj", "scale_proj.hip", []), ("seq_attn", "seq_attn.hip", []),
-             ("cache_append", "cache_append.hip", [])]
+             ("cache_append", "cache_append.hip", []), ("cache_plan", "cache_plan.hip", []), ("sample", "sample.hip", []), ("softmax", "softmax.hip", [])]
     for tname, ctype in (("bf16", "bf16_t"), ("f32", "float")):
         for d in (64, 128):
-            units.append(("seq_%s_%d" % (tname, d), "seq_inst.hip", ["-DENTMAX_INST_T=%s" % ctype, "-DENTMAX_INST_D=%d" % d]))
+            inst = ["-DENTMAX_INST_T=%s" % ctype, "-DENTMAX_INST_D=%d" % d]
+            units += [("seq_%s_%d" % (tname, d), "seq_inst.hip", inst), ("softmax_%s_%d" % (tname, d), "softmax_inst.hip", inst)]
     for leg in ("FWD", "BWD"):
         for tname, ctype in (("bf16", "bf16_t"), ("f32", "float")):
             for d in (64, 128):

@@ -1,0 +1,65 @@
+// Host-side argument validation and workspace carving of entmax_sample (include/entmax_attn.h).  Plain C++, no HIP types.
+#pragma once
+#include "seq_layout.h"
+
+namespace entmax {
+
+constexpr int kSampleMostVocab = 1 << 22;   // (an index has 22 bits of a token's rank)
+constexpr int kSampleBins = 256;
+// Logits of a workgroup: a row is cut into slices of so many (the first one may begin up to 16 bytes in front of the row, where addresses are round)
+constexpr int kSampleSmallSlice = 8192, kSampleLargeSlice = 16384;
+inline int sample_slice(int rows, int vocab) { return (long long)rows * vocab <= (1 << 20) ? kSampleSmallSlice : kSampleLargeSlice; }
+
+constexpr int kSampleStatBytes = 24;  // what the kernels leave of a slice, twice
+
+struct SampleLayout {
+  int slice, nslices;
+  size_t off_stat, off_hist, off_kept, off_cand, total;
+};
+inline SampleLayout make_sample_layout(const entmax_sample_params* p) {
+  SampleLayout L{};
+  L.slice = sample_slice(p->rows, p->vocab);
+  L.nslices = ceil_div(p->vocab + 7, L.slice);
+  const size_t n = (size_t)p->rows * L.nslices;
+  size_t o = 0;
+  L.off_stat = o;
+  o += align_up(n * kSampleStatBytes);
+  L.off_hist = o;
+  o += align_up(n * kSampleBins * sizeof(float));
+  L.off_kept = o;
+  o += align_up(n * kSampleStatBytes);
+  L.off_cand = o;
+  o += align_up(n * L.slice * sizeof(uint16_t));
+  L.total = o < kAlign ? kAlign : o;
+  return L;
+}
+
+inline int check_sample_params(const entmax_sample_params* p) {
+  if (!p) return ENTMAX_ATTN_INVALID_ARG;
+  if (p->rows < 0 || p->vocab <= 0 || p->stride < p->vocab) return ENTMAX_ATTN_INVALID_ARG;
+  if (p->dtype != ENTMAX_ATTN_BF16 && p->dtype != ENTMAX_ATTN_FP32) return ENTMAX_ATTN_INVALID_ARG;
+  if (p->rows > (1 << 20) || p->vocab > kSampleMostVocab || p->stride > kMostStride) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  // (a launch has less than 2^32 threads)
+  if ((long long)p->rows * ceil_div(p->vocab + 7, sample_slice(p->rows, p->vocab)) * 1024 >= 1ll << 32) return ENTMAX_ATTN_UNSUPPORTED_SHAPE;
+  return ENTMAX_ATTN_OK;
+}
+
+// Whether what a call writes is apart in itself and from what it reads
+inline bool sample_outputs_apart(const entmax_sample_params* p, const void* logits, const void* uniform, const void* temperature, const void* top_k,
+                                 const void* top_p, const void* min_p, const void* token, const void* logprob, const void* workspace, size_t bytes) {
+  const int64_t es = p->dtype == ENTMAX_ATTN_BF16 ? 2 : 4;
+  auto one = [](const void* at, long long n) { return RowSet{at, {1, 1, 1}, {0, 0, 0}, n}; };
+  const long long n = 4ll * p->rows;
+  const RowSet out[3] = {one(token, n), one(logprob, n), one(workspace, (long long)bytes)};
+  const RowSet in[6] = {RowSet{logits, {p->rows, 1, 1}, {p->stride * es, 0, 0}, p->vocab * es}, one(uniform, n), one(temperature, n),
+                        one(top_k, n), one(top_p, n), one(min_p, n)};
+  for (int a = 0; a < 3; ++a) {
+    for (int c = a + 1; c < 3; ++c)
+      if (rows_meet(out[a], out[c])) return false;
+    for (int c = 0; c < 6; ++c)
+      if (rows_meet(out[a], in[c])) return false;
+  }
+  return true;
+}
+
+}  // namespace entmax

@@ -1,0 +1,71 @@
+// Host-side argument validation and workspace carving of entmax_paged_softmax_fwd (include/entmax_attn.h).  Plain C++, no HIP types.
+#pragma once
+#include "seq_layout.h"
+
+namespace entmax {
+
+inline int check_softmax_params(const entmax_seq_params* p) {
+  if (!p || p->alpha != 1.0f || p->path != 0) return ENTMAX_ATTN_INVALID_ARG;
+  entmax_seq_params q = *p;
+  q.alpha = 2.0f;  // (everything else is as in the entmax attention)
+  const int rc = check_seq_params(&q);
+  if (rc != ENTMAX_ATTN_OK) return rc;
+  return p->page_size == 0 ? ENTMAX_ATTN_INVALID_ARG : ENTMAX_ATTN_OK;
+}
+
+// Waves of a workgroup of the kernel that splits the keys; each has two tiles of 32 keys and values in LDS
+inline int softmax_waves(const entmax_seq_params* p) { return p->dtype == ENTMAX_ATTN_FP32 && p->D == 128 ? 2 : 4; }
+
+struct SoftmaxLayout {
+  bool split;   // the call may hold sequences of at most kSplitRows folded rows
+  bool blocks;  // it may hold others
+  int rows;     // rows of a head there is room for
+  int piece, splits;  // keys of a workgroup, workgroups of a head
+  size_t off_part, off_sums, total;
+};
+
+inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
+  SoftmaxLayout L{};
+  const int G = p->Hq / p->Hkv;
+  const long long most_rows = (long long)p->max_new * G;
+  L.split = G <= kSplitRows;
+  L.blocks = !L.split || most_rows > kSplitRows;
+  size_t o = 0;
+  if (L.split) {
+    const long long heads = (long long)p->nseq * p->Hkv;
+    const int step = 32 * softmax_waves(p);
+    L.rows = (int)(most_rows < kSplitRows ? most_rows : kSplitRows);
+    L.piece = 2 * step;
+    while (L.piece < (1 << 20) && heads * ((p->max_keys + L.piece - 1) / L.piece) > 1024) L.piece *= 2;
+    L.splits = p->max_keys > 0 ? ceil_div(p->max_keys, L.piece) : 1;
+    if (L.splits > 1) {
+      const size_t n = (size_t)heads * L.splits * L.rows;
+      L.off_part = o;
+      o += align_up(n * p->D * sizeof(float));
+      L.off_sums = o;
+      o += align_up(n * 2 * sizeof(float));
+    }
+  }
+  L.total = o < kAlign ? kAlign : o;
+  return L;
+}
+
+inline size_t softmax_workspace_bytes_of(const entmax_seq_params* p) {
+  return check_softmax_params(p) == ENTMAX_ATTN_OK ? make_softmax_layout(p).total : 0;
+}
+
+// Whether O and lse are apart from each other and from what is read
+inline bool softmax_outputs_apart(const entmax_seq_params* p, const void* Q, const void* K, const void* V, const void* O, const void* lse) {
+  if (!seq_output_apart(p, Q, K, V, O)) return false;
+  const int64_t es = p->dtype == ENTMAX_ATTN_BF16 ? 2 : 4, row = p->D * es;
+  const RowSet l{lse, {1, 1, 1}, {0, 0, 0}, 4ll * p->Hq * p->T};
+  const RowSet x[4] = {RowSet{O, {p->T, p->Hq, 1}, {p->o_stride_t * es, p->o_stride_h * es, 0}, row},
+                       RowSet{Q, {p->T, p->Hq, 1}, {p->q_stride_t * es, p->q_stride_h * es, 0}, row},
+                       RowSet{K, {p->num_pages, p->Hkv, p->page_size}, {p->k_stride_p * es, p->k_stride_h * es, p->k_stride_n * es}, row},
+                       RowSet{V, {p->num_pages, p->Hkv, p->page_size}, {p->v_stride_p * es, p->v_stride_h * es, p->v_stride_n * es}, row}};
+  for (int k = 0; k < 4; ++k)
+    if (rows_meet(l, x[k])) return false;
+  return true;
+}
+
+}  // namespace entmax
