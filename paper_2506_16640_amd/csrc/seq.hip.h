@@ -139,7 +139,8 @@ struct SeqTile {
       if (j0 + KT <= n) {
         load_to_lds(k.row_in(p.pg[it], j0 + row), (uint32_t)rl * (uint32_t)k.sn + chunk, dst);
       } else {
-        const char* src = k.row(min(j0 + row + rl, n - 1)) + chunk;
+        // (the load's rows that there are, and the last one, which the others repeat, lie on the page that was asked for)
+        const char* src = k.row_in(p.pg[it], min(j0 + row + rl, n - 1)) + chunk;
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
       }
     }

@@ -33,48 +33,154 @@ struct SoftmaxArgs {
   void* O;
   float* lse;
   float cap;
-  float* part;    // [nseq * Hkv][splits][rows][D]
-  float2* sums;   // [nseq * Hkv][splits][rows] (largest score in units of log 2, sum)
-  int rows, piece, splits;
+  float* part;    // [places][rows][D], a place for every piece: see SoftmaxShare
+  float2* sums;   // [places][rows] (largest score in units of log 2, sum)
+  int rows;
+  int shared;     // pieces from the lengths of all sequences (else of `piece` keys, `splits` to a sequence)
+  int budget;     // shared: tiles are dealt out to about so many workgroups
+  int piece, splits;
   int nblk;
   int split;      // sequences with few rows are left to softmax_split_kernel
 };
 
+// How a sequence's keys are cut up: n equal pieces of `len` keys, whole tiles of 32 (one piece of none if there are no keys).  Piece k of key/value head hk has place
+// (first + k) Hkv + hk.
+struct SoftmaxShare {
+  int first, n, len;
+  __device__ __forceinline__ void cut(int keys, int most_tiles) {
+    const int tiles = (keys + 31) >> 5;
+    n = max(1, (tiles + most_tiles - 1) / most_tiles);
+    const int each = (tiles + n - 1) / n;
+    if (each > 0) n = (tiles + each - 1) / each;
+    len = each * 32;
+  }
+};
+
+// The share of sequence x, or (BY_PLACE) of the sequence that has place x, with what it is; false: there is none.
+// Memory delivers as much as it can when all compute units ask for equal parts of it at the same time, and the host knows only a bound of the lengths: so
+// every wave adds up the tiles of all sequences (64 at a time, a lane each), divides them by the number of workgroups that fit the chip, and
+// numbers the pieces that come of it.  (48 sequences of 150 to 9000 keys, 2 heads of 128: 41 us with pieces by the bound, 27 so.)  With many
+// sequences that would take longer than it gives: pieces by the bound.
+template <bool BY_PLACE>
+__device__ __forceinline__ bool softmax_share(const SoftmaxArgs& A, int x, SeqView& v, SoftmaxShare& sh) {
+  const SeqGeom& g = A.g;
+  if (!A.shared) {
+    const int s = BY_PLACE ? x / A.splits : x;
+    if (s >= g.nseq || !load_seq(g, s, v) || !split_seq(g, v)) return false;
+    sh.cut(v.L, A.piece >> 5);
+    sh.first = s * A.splits;
+    return true;
+  }
+  const int lane = threadIdx.x & 63;
+  auto load = [&](int s, SeqView& t) {
+    const bool ok = s < g.nseq && load_seq(g, s, t) && split_seq(g, t);
+    return ok ? max(1, (t.L + 31) >> 5) : 0;
+  };
+  SeqView t;
+  int tiles = load(lane, t);
+  long long all = tiles;
+  for (int s0 = 64; s0 < g.nseq; s0 += 64) {
+    SeqView u;
+    all += load(s0 + lane, u);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) all += __shfl_xor(all, off);
+  const int most = max(kSoftmaxLeastTiles, (int)((all * g.Hkv + A.budget - 1) / A.budget));
+  int first = 0;
+  for (int s0 = 0; s0 < g.nseq; s0 += 64) {
+    if (s0) tiles = load(s0 + lane, t);
+    SoftmaxShare mine;
+    mine.cut(t.L, most);
+    if (tiles == 0) mine.n = 0;
+    int upto = mine.n;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(upto, off);
+      if (lane >= off) upto += y;
+    }
+    const unsigned long long here = __ballot(BY_PLACE ? first + upto > x : s0 + lane == x);
+    if (here) {
+      const int l = __builtin_ctzll(here);
+      v.s = s0 + l;
+      v.row0 = __builtin_amdgcn_readlane(t.row0, l);
+      v.n = __builtin_amdgcn_readlane(t.n, l);
+      v.L = __builtin_amdgcn_readlane(t.L, l);
+      sh.n = __builtin_amdgcn_readlane(mine.n, l);
+      sh.len = __builtin_amdgcn_readlane(mine.len, l);
+      sh.first = first + __builtin_amdgcn_readlane(upto, l) - sh.n;
+      return sh.n > 0;
+    }
+    first += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// A row's scores in units of log 2, and what it has seen so far.
+// From accumulators of the dot products to scores in units of log 2: score = unit * x, x the accumulator or, with a cap, what capped() makes of it.
+template <typename T, bool CAP>
+struct SoftmaxScale {
+  float unit;
+  float cap2, in2, late;  // CAP: cap in units of log 2; s / cap = in2 * accumulator; slope of a bias outside the cap
+  // a, w: as in SeqRow; w is zero afterwards if the bias is added late
+  __device__ __forceinline__ void init_scale(const SoftmaxArgs& A, float a, float& w) {
+    unit = CAP ? 1.f : a * kLog2e;
+    if (CAP) {
+      cap2 = A.cap * kLog2e;
+      in2 = a / A.cap;
+      late = 0.f;
+      if (A.g.bias_mode == 1) {
+        late = a * w * kLog2e;
+        w = 0.f;
+      }
+    }
+  }
+  __device__ __forceinline__ float capped(float acc, int dist) const {
+    // 1 - 2 / (1 + exp(2 x)): off by some 1.2e-7, of the cap.  fp32: near zero, where that is much of the value, the first five terms of the series
+    // (the sixth is 1e-8 of it at 1/4)
+    const float x = acc * in2;
+    float t = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
+    if constexpr (sizeof(T) == 4) {
+      const float x2 = x * x;
+      const float near = x * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+      t = x2 < 0.0625f ? near : t;
+    }
+    return fmaf(late, (float)max(dist, 0), cap2 * t);
+  }
+};
+
+// A wave's 32 rows, a lane pair each, and what they have seen so far.
 template <typename T, int D, bool CAP>
-struct SoftmaxRows : SeqRows<T, D> {
-  static constexpr int NM = D / 32;
-  float unit;        // score = unit * accumulator
-  float cap2, in2;   // CAP: cap in units of log 2; the accumulator's factor in exp2(2 s / cap)
-  float late;        // CAP, bias outside the cap: its slope
-  float top, sum;    // largest accumulator; sum of this lane's exp2(unit (acc - top))
+struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
+  static constexpr int kRows = 32, NC = D / 16, NM = D / 32;
+  static constexpr int kChunks = NM * 4;  // a lane's parts of the output, four features each
+  static constexpr int kProbs = 16;       // a lane's probabilities of 32 keys
+  float top, sum;    // largest x; sum of this lane's exp2(unit (x - top))
   f32x16_t oacc[NM];
   __device__ __forceinline__ void init(const SoftmaxArgs& A, const SeqView& v, int hk, int r0) {
     SeqRows<T, D>::init(A.g, v, A.Q, hk, r0);
-    unit = CAP ? 1.f : this->a * kLog2e;
-    if (CAP) {
-      cap2 = A.cap * kLog2e;
-      in2 = this->a / A.cap;
-      late = 0.f;
-      if (A.g.bias_mode == 1) {
-        late = this->a * this->w * kLog2e;
-        this->w = 0.f;
-        this->biased = false;
-      }
-    }
+    this->init_scale(A, this->a, this->w);
+    this->biased = __ballot(this->w != 0.f) != 0ull;
     top = -kInf;
     sum = 0.f;
 #pragma unroll
     for (int mm = 0; mm < NM; ++mm)
       oacc[mm] = f32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   }
+  __device__ __forceinline__ int row() const { return this->li; }
+  __device__ __forceinline__ bool first_lane() const { return this->hh == 0; }
+  __device__ __forceinline__ float total() const { return sum + __shfl_xor(sum, 32); }
+  __device__ __forceinline__ int feature(int chunk) const { return 8 * chunk + 4 * this->hh; }
+  __device__ __forceinline__ f32x4_t out(int chunk) const {
+    const f32x16_t& o = oacc[chunk >> 2];
+    const int e = 4 * (chunk & 3);
+    return f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]};
+  }
   // S^T of 32 keys as in SeqRows; fp32: sums of sixteen features each, one after the other so that few of them are held, added up as a tree
   template <class F>
   __device__ __forceinline__ f32x16_t scores(f32x16_t acc, F frag) const {
     if constexpr (sizeof(T) == 2) return this->dots(acc, frag);
-    else return acc + branch<0, D / 16>(frag);
+    else return acc + branch<0, NC>(frag);
   }
   template <int FROM, int N, class F>
   __device__ __forceinline__ f32x16_t branch(F frag) const {
@@ -89,22 +195,18 @@ struct SoftmaxRows : SeqRows<T, D> {
   }
   __device__ __forceinline__ void cap_scores(f32x16_t& acc, int j0) const {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float t;
-      if constexpr (sizeof(T) == 2)  // (1.2e-7 of the cap off: far below what rounding Q and K costs)
-        t = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(acc[e] * (2.f * kLog2e * in2)));
-      else
-        t = tanhf(acc[e] * in2);
-      acc[e] = fmaf(late, (float)max(this->pos - j0 - this->key_of(e), 0), cap2 * t);
-    }
+    for (int e = 0; e < 16; ++e) acc[e] = this->capped(acc[e], this->pos - j0 - this->key_of(e));
   }
-  // Takes in the 32 keys from j0 on, whose scores' accumulators acc are (masked ones -inf): p receives exp2(score - largest so far)
-  __device__ __forceinline__ void step(const f32x16_t& acc, float (&p)[16]) {
-    float m = max16(acc);
+  // Takes in blocks of 32 keys with scores x = acc (masked ones -inf): p receives exp2(score - largest so far)
+  template <int NB>
+  __device__ __forceinline__ void step(const f32x16_t (&acc)[NB], float (&p)[NB][16]) {
+    float m = max16(acc[0]);
+#pragma unroll
+    for (int b = 1; b < NB; ++b) m = fmaxf(m, max16(acc[b]));
     m = fmaxf(m, __shfl_xor(m, 32));
     const bool more = m > top;
     if (__ballot(more) != 0ull) {
-      const float f = more ? __builtin_amdgcn_exp2f((top - m) * unit) : 1.f;  // (0 from -inf)
+      const float f = more ? __builtin_amdgcn_exp2f((top - m) * this->unit) : 1.f;  // (0 from -inf)
       top = more ? m : top;
       sum *= f;
 #pragma unroll
@@ -112,209 +214,448 @@ struct SoftmaxRows : SeqRows<T, D> {
 #pragma unroll
         for (int e = 0; e < 16; ++e) oacc[mm][e] *= f;
     }
-    const float base = top > -kInf ? -top * unit : 0.f;
-    float s = 0.f;
+    const float base = top > -kInf ? -top * this->unit : 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(fmaf(acc[e], unit, base));
-      s += p[e];
+    for (int b = 0; b < NB; ++b) {
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[b][e] = __builtin_amdgcn_exp2f(fmaf(acc[b][e], this->unit, base));
+        s += p[b][e];
+      }
+      sum += s;
     }
-    sum += s;
   }
-  __device__ __forceinline__ float top2() const { return top > -kInf ? top * unit : -kInf; }
-};
+  __device__ __forceinline__ float top2() const { return top > -kInf ? top * this->unit : -kInf; }
 
-template <typename T, int D>
-struct SoftmaxSplitCfg {
-  static constexpr int NW = sizeof(T) == 4 && D == 128 ? 2 : 4;
-  static constexpr int KT = 32, kTileBytes = KT * D * (int)sizeof(T);
-  static constexpr int kWaveBytes = 4 * kTileBytes;  // two tiles of keys, two of values
-  static constexpr size_t kLdsBytes = (size_t)NW * kWaveBytes;
-};
-
-template <typename T, int D, int NQB, bool CAP>
-__global__ __launch_bounds__((SoftmaxSplitCfg<T, D>::NW * 64), 1) void softmax_split_kernel(SoftmaxArgs A) {
-  using Cfg = SoftmaxSplitCfg<T, D>;
-  constexpr int NW = Cfg::NW, NC = D / 16, NM = D / 32, TB = Cfg::kTileBytes;
+  // ---- the 32 keys and values of a wave's own tile
   using KTile = SeqTile<T, D, 32, false, 64>;
   using Vals = SeqValues<T, D, 32, 64>;
   using VTile = typename Vals::VT;
+  struct Places {
+    FragOff<T> k[NC];
+    Vals v;
+    __device__ __forceinline__ void init(int lane) {
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc) k[cc] = FragOff<T>::template make<typename KTile::Tile>(lane & 31, 2 * cc + (lane >> 5));
+      v.init(lane);
+    }
+  };
+  // whether some row does not see some key
+  __device__ __forceinline__ bool take_keys(const Places& at, const char* tile, int j0, const SeqKeys& keys, bool hole, float (&p)[kProbs]) {
+    f32x16_t acc[1] = {scores(this->start(j0), [&](int cc) { return at.k[cc].load(tile, 0); })};
+    if constexpr (CAP) cap_scores(acc[0], j0);
+    const bool masked = hole || j0 + 32 > this->lim_min;
+    if (masked) this->mask(acc[0], j0, keys, hole);
+    step<1>(acc, reinterpret_cast<float(&)[1][16]>(p));
+    return masked;
+  }
+  __device__ __forceinline__ void take_values(const Places& at, const char* tile, const float (&p)[kProbs], bool masked) {
+    at.v.accumulate(tile, 0, p, masked, oacc);
+  }
+};
+
+// A wave's 16 rows, four lanes each, on the matrix instructions of 16 x 16: half the work of SoftmaxRows where there are not more rows.
+// Lane l has row l % 16; of 32 keys those of 16 (e / 4) + 4 (l / 16) + e % 4, e = 0 .. 7, and of the output features 16 f + 4 (l / 16) + 0 .. 3.
+template <typename T, int D, bool CAP>
+struct SoftmaxRows16 : SeqRow, SoftmaxScale<T, CAP> {
+  static constexpr int kRows = 16, kChunks = D / 16, kProbs = 8;
+  static constexpr int NC = D * (int)sizeof(T) / 64;  // fragments of a row of queries or keys, 16 bytes of a lane
+  using KTile = SeqTile<T, D, 32, false, 64>;
+  using VTile = SeqTile<T, D, 32, sizeof(T) == 2, 64>;
+  int lane, li, quad, lim_min, lim_max;
+  bool biased;
+  u32x4_t qf[NC];
+  float top, sum;
+  f32x4_t oacc[kChunks];
+  __device__ __forceinline__ void init(const SoftmaxArgs& A, const SeqView& v, int hk, int r0) {
+    lane = threadIdx.x & 63;
+    li = lane & 15;
+    quad = lane >> 4;
+    SeqRow::init<sizeof(T) == 2>(A.g, v, hk, r0 + li, D);
+    this->init_scale(A, a, w);
+    biased = __ballot(w != 0.f) != 0ull;
+    lim_min = __builtin_amdgcn_readfirstlane(lim);  // (limits do not decrease from row to row)
+    const int last = min(v.n * A.g.G - 1 - r0, 15);
+    lim_max = last < 0 ? 0 : __builtin_amdgcn_readlane(lim, last);
+    const char* q = reinterpret_cast<const char*>(reinterpret_cast<const T*>(A.Q) + (long long)(v.row0 + t) * A.g.q_st + (long long)head * A.g.q_sh);
+    const uint32_t sign = c < 0.f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
+#pragma unroll
+    for (int cc = 0; cc < NC; ++cc) {
+      qf[cc] = *reinterpret_cast<const u32x4_t*>(q + 64 * cc + 16 * quad);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) qf[cc][e] = c != 0.f ? qf[cc][e] ^ sign : 0u;  // (0 beyond the last row, too)
+    }
+    top = -kInf;
+    sum = 0.f;
+#pragma unroll
+    for (int f = 0; f < kChunks; ++f) oacc[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ int row() const { return li; }
+  __device__ __forceinline__ bool first_lane() const { return quad == 0; }
+  __device__ __forceinline__ float total() const {
+    const float x = sum + __shfl_xor(sum, 16);
+    return x + __shfl_xor(x, 32);
+  }
+  __device__ __forceinline__ int feature(int chunk) const { return 16 * chunk + 4 * quad; }
+  __device__ __forceinline__ f32x4_t out(int chunk) const { return oacc[chunk]; }
+  __device__ __forceinline__ float top2() const { return top > -kInf ? top * this->unit : -kInf; }
+  __device__ __forceinline__ int key_of(int e) const { return 16 * (e >> 2) + 4 * quad + (e & 3); }
+  struct Places {
+    int k[NC], v[sizeof(T) == 2 ? kChunks : 1];
+    __device__ __forceinline__ void init(int lane) {
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc) k[cc] = KTile::off(lane & 15, 4 * cc + (lane >> 4));
+      if constexpr (sizeof(T) == 2) {  // (see SeqValues)
+        const int p = lane & 15, row = 4 * (lane >> 4) + (p >> 2);
+#pragma unroll
+        for (int f = 0; f < kChunks; ++f) v[f] = VTile::off(row, 2 * f + ((p & 3) >> 1)) + (p & 1) * 8;
+      }
+    }
+  };
+  template <int FROM, int N>
+  static __device__ __forceinline__ f32x4_t branch(const f32x4_t* x) {
+    if constexpr (N > 1) return branch<FROM, N / 2>(x) + branch<FROM + N / 2, N / 2>(x);
+    else return x[FROM];
+  }
+  // S^T of keys 16 b .. 16 b + 15 of the tile, on top of acc
+  __device__ __forceinline__ f32x4_t scores(const Places& at, const char* tile, int b, f32x4_t acc) const {
+    const char* from = tile + 16 * b * KTile::kRowBytes;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(from + at.k[cc])),
+                                                      __builtin_bit_cast(bf16x8_t, qf[cc]), acc, 0, 0, 0);
+      return acc;
+    } else {  // (sums of sixteen features each, added up as a tree: see SoftmaxRows)
+      f32x4_t part[NC];
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc) {
+        const f32x4_t k = *reinterpret_cast<const f32x4_t*>(from + at.k[cc]);
+        part[cc] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[cc] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[e], __uint_as_float(qf[cc][e]), part[cc], 0, 0, 0);
+      }
+      return acc + branch<0, NC>(part);
+    }
+  }
+  __device__ __forceinline__ bool take_keys(const Places& at, const char* tile, int j0, const SeqKeys& keys, bool hole, float (&p)[kProbs]) {
+    float x[kProbs];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+      if (biased) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = w * (float)max(pos - j0 - key_of(4 * b + e), 0);
+      }
+      acc = scores(at, tile, b, acc);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * b + e] = CAP ? this->capped(acc[e], pos - j0 - key_of(4 * b + e)) : acc[e];
+    }
+    const bool masked = hole || j0 + 32 > lim_min;
+    if (masked) {
+#pragma unroll
+      for (int e = 0; e < kProbs; ++e) {
+        const int j = j0 + key_of(e);
+        const bool seen = j < lim && !(hole && keys.is_hole(keys.page(j)));
+        x[e] = seen ? x[e] : -kInf;
+      }
+    }
+    float m = x[0];
+#pragma unroll
+    for (int e = 1; e < kProbs; ++e) m = fmaxf(m, x[e]);
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const bool more = m > top;
+    if (__ballot(more) != 0ull) {
+      const float f = more ? __builtin_amdgcn_exp2f((top - m) * this->unit) : 1.f;  // (0 from -inf)
+      top = more ? m : top;
+      sum *= f;
+#pragma unroll
+      for (int c4 = 0; c4 < kChunks; ++c4)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) oacc[c4][e] *= f;
+    }
+    const float base = top > -kInf ? -top * this->unit : 0.f;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < kProbs; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(fmaf(x[e], this->unit, base));
+      s += p[e];
+    }
+    sum += s;
+    return masked;
+  }
+  // a value of the tile
+  static __device__ __forceinline__ float value(const char* tile, int key, int feature) {
+    constexpr int E = 16 / (int)sizeof(T);
+    const char* at = tile + VTile::off(key, feature / E) + (feature % E) * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2)
+      return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16);
+    else
+      return *reinterpret_cast<const float*>(at);
+  }
+  // oacc += V^T P^T; as in SeqValues::accumulate() where some row does not see some key
+  __device__ __forceinline__ void take_values(const Places& at, const char* tile, const float (&p)[kProbs], bool masked) {
+    if (masked) {
+      bool bad = false;
+#pragma unroll 1
+      for (int e = 0; e < 32 * D / 64; ++e) {
+        const float x = value(tile, (64 * e + lane) / D, (64 * e + lane) % D);
+        bad = bad || (opaque_bits(x) & 0x7f800000u) == 0x7f800000u;
+      }
+      if (__ballot(bad) != 0ull) {
+        one_by_one(tile, p);
+        return;
+      }
+    }
+    if constexpr (sizeof(T) == 2) {
+      // (probabilities as the sum of two bf16 numbers: rounded to one, they would cost up to 2^-9 |v| of the output)
+      Frag<T> hi, lo;
+      Elem<T>::pack_split(p, hi, lo);
+#pragma unroll
+      for (int f = 0; f < kChunks; ++f) {
+        const uint2 x = read_transposed(tile + at.v[f]), y = read_transposed(tile + at.v[f] + 16 * VTile::kRowBytes);
+        const bf16x8_t v = __builtin_bit_cast(bf16x8_t, u32x4_t{x.x, x.y, y.x, y.y});
+        oacc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, hi.v), oacc[f], 0, 0, 0);
+        oacc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, lo.v), oacc[f], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kProbs; ++e)
+#pragma unroll
+        for (int f = 0; f < kChunks; ++f) oacc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(value(tile, key_of(e), 16 * f + li), p[e], oacc[f], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void one_by_one(const char* tile, const float (&p)[kProbs]) {
+#pragma unroll 1
+    for (int from = 0; from < 4; ++from) {
+#pragma unroll
+      for (int e = 0; e < kProbs; ++e) {
+        const float pk = __shfl(p[e], li + 16 * from);
+        if (pk > 0.f) {
+          const int key = 16 * (e >> 2) + 4 * from + (e & 3);
+#pragma unroll
+          for (int f = 0; f < kChunks; ++f)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) oacc[f][x] = fmaf(pk, value(tile, key, 16 * f + 4 * quad + x), oacc[f][x]);
+        }
+      }
+    }
+  }
+};
+
+// Waves of a workgroup of the kernel that splits the keys, and tiles of 32 keys and values that a wave has in LDS: 64 KB a workgroup, so that two share a
+// compute unit and one's start and end hide behind the other's loads.
+template <typename T, int D>
+struct SoftmaxSplitCfg {
+  static constexpr int NW = kSoftmaxWaves<(int)sizeof(T), D>;
+  static constexpr int ST = sizeof(T) == 2 && D == 64 ? 2 : 1;
+  static constexpr int kTileBytes = 32 * D * (int)sizeof(T);
+  static constexpr int kWaveBytes = 2 * ST * kTileBytes;
+  static constexpr size_t kLdsBytes = (size_t)NW * kWaveBytes;
+};
+
+// Rows: SoftmaxRows or SoftmaxRows16; NQB: blocks of them
+template <typename T, int D, class Rows, int NQB>
+__global__ __launch_bounds__((SoftmaxSplitCfg<T, D>::NW * 64), (NQB == 1 && (sizeof(T) == 2 || Rows::kRows == 16) ? 2 : 1)) void softmax_split_kernel(
+    SoftmaxArgs A) {
+  using Cfg = SoftmaxSplitCfg<T, D>;
+  constexpr int NW = Cfg::NW, ST = Cfg::ST, TB = Cfg::kTileBytes, RB = Rows::kRows, CH = Rows::kChunks;
+  using KTile = typename Rows::KTile;
+  using VTile = typename Rows::VTile;
   constexpr int LD = KTile::L;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ float tops[NW][NQB * 32], parts[NW][NQB * 32];
+  __shared__ float tops[NW][NQB * RB], parts[NW][NQB * RB];
   const SeqGeom& g = A.g;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, li = lane & 31, hh = lane >> 5;
-  const int split = blockIdx.x % A.splits, s = blockIdx.x / A.splits, hk = blockIdx.y;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int hk = blockIdx.x % g.Hkv;
   SeqView v;
-  if (!load_seq(g, s, v) || !split_seq(g, v)) return;
-  const int from = split * A.piece;
-  if (split > 0 && from >= v.L) return;
-  const int to = min(v.L, from + A.piece);
-  const int rbase = blockIdx.z * NQB * 32, R = v.n * g.G - rbase;  // first row, rows from there on
+  SoftmaxShare sh;
+  if (!softmax_share<true>(A, (int)blockIdx.x / g.Hkv, v, sh)) return;
+  const int split = (int)blockIdx.x / g.Hkv - sh.first;
+  if (split >= sh.n) return;
+  const int from = split * sh.len, to = min(v.L, from + sh.len);
+  const int rbase = blockIdx.z * NQB * RB, R = v.n * g.G - rbase;  // first row, rows from there on
   if (R <= 0) return;
   SeqKeys keys, vals;
   keys.init(g, v, A.K, hk, false, sizeof(T));
   vals.init(g, v, A.V, hk, true, sizeof(T));
   char* mine = smem + wave * Cfg::kWaveBytes;
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
-  // this wave's tiles: from + 32 (wave + NW i)
+  // this wave's tiles: from + 32 (wave + NW i); tile i lies in place i % ST
   const int tiles = (to - from + 31) >> 5, nt = tiles > wave ? (tiles - wave + NW - 1) / NW : 0;
   auto start = [&](int i) { return from + 32 * (wave + NW * i); };
   typename KTile::Pages pk;
   typename VTile::Pages pv;
-  bool holes[2] = {false, false};
+  bool holes[ST];
   auto ask = [&](int i) {
     pk.ask(keys, start(i), v.L, 0);
     pv.ask(vals, start(i), v.L, 0);
   };
-  auto issue_k = [&](int i, int buf) {
+  auto issue_k = [&](int i) {
     bool h = false;
 #pragma unroll
     for (int it = 0; it < LD; ++it) h = h || keys.is_hole(pk.pg[it]);
-    holes[buf] = h;
-    KTile::load(keys, pk, start(i), v.L, lds + (uint32_t)(2 * buf) * TB, 0, lane);
+    holes[i % ST] = h;
+    KTile::load(keys, pk, start(i), v.L, lds + (uint32_t)(2 * (i % ST)) * TB, 0, lane);
   };
-  auto issue_v = [&](int i, int buf) { VTile::load(vals, pv, start(i), v.L, lds + (uint32_t)(2 * buf + 1) * TB, 0, lane); };
-  if (nt > 0) {
-    ask(0);
-    issue_k(0, 0);
-    issue_v(0, 0);
-  }
-  if (nt > 1) {
-    ask(1);
-    issue_k(1, 1);
-    issue_v(1, 1);
-  }
-  if (nt > 2) ask(2);
-  SoftmaxRows<T, D, CAP> q[NQB];
+  auto issue_v = [&](int i) { VTile::load(vals, pv, start(i), v.L, lds + (uint32_t)(2 * (i % ST) + 1) * TB, 0, lane); };
 #pragma unroll
-  for (int qb = 0; qb < NQB; ++qb) q[qb].init(A, v, hk, rbase + qb * 32);
-  FragOff<T> koff[NC];
+  for (int i = 0; i < ST; ++i) {
+    holes[i] = false;
+    if (i < nt) {
+      ask(i);
+      issue_k(i);
+      issue_v(i);
+    }
+  }
+  if (nt > ST) ask(ST);
+  Rows q[NQB];
 #pragma unroll
-  for (int cc = 0; cc < NC; ++cc) koff[cc] = FragOff<T>::template make<typename KTile::Tile>(li, 2 * cc + hh);
-  Vals vv;
-  vv.init(lane);
+  for (int qb = 0; qb < NQB; ++qb) q[qb].init(A, v, hk, rbase + qb * RB);
+  typename Rows::Places places;
+  places.init(lane);
+  // A tile's keys, then its values, are waited for; the loads issued after them stay under way: those of the ST - 1 next tiles, and in between the
+  // values of this one or the keys of the one that takes its place.
   for (int i = 0; i < nt; ++i) {
-    const int buf = i & 1, left = nt - 1 - i, j0 = start(i);
-    const char* tile = mine + 2 * buf * TB;
-    if (left > 0)
-      lds_loads_wait<3 * LD>();
+    const int left = nt - 1 - i, j0 = start(i);
+    const char* tile = mine + 2 * (i % ST) * TB;
+    if (ST > 1 && left >= ST - 1)
+      lds_loads_wait<(2 * ST - 1) * LD>();
     else
       lds_loads_wait<LD>();
-    float p[NQB][16];
+    float p[NQB][Rows::kProbs];
     bool masked[NQB], sees[NQB];
-    const bool hole = holes[buf];
+    const bool hole = holes[i % ST];
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb) {
-      sees[qb] = qb * 32 < R && j0 < q[qb].lim_max;
-      if (!sees[qb]) continue;
-      f32x16_t acc = q[qb].scores(q[qb].start(j0), [&](int cc) { return koff[cc].load(tile, 0); });
-      if constexpr (CAP) q[qb].cap_scores(acc, j0);
-      masked[qb] = hole || j0 + 32 > q[qb].lim_min;
-      if (masked[qb]) q[qb].mask(acc, j0, keys, hole);
-      q[qb].step(acc, p[qb]);
+      sees[qb] = qb * RB < R && j0 < q[qb].lim_max;
+      if (sees[qb]) masked[qb] = q[qb].take_keys(places, tile, j0, keys, hole, p[qb]);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile has been read)
-    if (left > 1) issue_k(i + 2, buf);
-    if (left > 1)
-      lds_loads_wait<3 * LD>();
-    else if (left > 0)
-      lds_loads_wait<2 * LD>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the keys have been read)
+    const bool next = left >= ST;
+    if (next) issue_k(i + ST);
+    if (next)
+      lds_loads_wait<(2 * ST - 1) * LD>();
+    else if (ST > 1 && left > 0)
+      lds_loads_wait<2 * (ST - 1) * LD>();
     else
       lds_loads_wait<0>();
 #pragma unroll
     for (int qb = 0; qb < NQB; ++qb)
-      if (sees[qb]) vv.accumulate(tile + TB, 0, p[qb], masked[qb], q[qb].oacc);
+      if (sees[qb]) q[qb].take_values(places, tile + TB, p[qb], masked[qb]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (left > 1) issue_v(i + 2, buf);
-    if (left > 2) ask(i + 3);
+    if (next) issue_v(i + ST);
+    if (left > ST) ask(i + ST + 1);
   }
   // the waves' outputs in units of their largest score, added in their order
 #pragma unroll
   for (int qb = 0; qb < NQB; ++qb) {
-    const float l = q[qb].sum + __shfl_xor(q[qb].sum, 32);
-    if (hh == 0) {
-      tops[wave][qb * 32 + li] = q[qb].top2();
-      parts[wave][qb * 32 + li] = l;
+    const float l = q[qb].total();
+    if (q[qb].first_lane()) {
+      tops[wave][qb * RB + q[qb].row()] = q[qb].top2();
+      parts[wave][qb * RB + q[qb].row()] = l;
     }
   }
   __syncthreads();  // (no tile is read any more)
-  const int pieces = max(1, (v.L + A.piece - 1) / A.piece);
-  const long long head = (long long)s * g.Hkv + hk;
+  const int pieces = sh.n;
 #pragma unroll
   for (int qb = 0; qb < NQB; ++qb) {
-    if (qb * 32 >= R) break;
+    if (qb * RB >= R) break;
+    const int row = qb * RB + q[qb].row();
     float most = -kInf, l = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) most = fmaxf(most, tops[w][qb * 32 + li]);
-    auto factor = [&](int w) { return most > -kInf ? __builtin_amdgcn_exp2f(tops[w][qb * 32 + li] - most) : 0.f; };
+    for (int w = 0; w < NW; ++w) most = fmaxf(most, tops[w][row]);
+    auto factor = [&](int w) { return most > -kInf ? __builtin_amdgcn_exp2f(tops[w][row] - most) : 0.f; };
 #pragma unroll
-    for (int w = 0; w < NW; ++w) l += parts[w][qb * 32 + li] * factor(w);
+    for (int w = 0; w < NW; ++w) l += parts[w][row] * factor(w);
     const float f = factor(wave);
-    f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);  // [waves][NM * 4][64]
+    f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);  // [waves][CH][64]
+    static_assert(CH * 1024 <= Cfg::kWaveBytes, "a wave's outputs fit its tiles");
     if (qb) __syncthreads();
 #pragma unroll
-    for (int mm = 0; mm < NM; ++mm)
+    for (int u = 0; u < CH; ++u) {
+      f32x4_t o = q[qb].out(u);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        f32x4_t o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = q[qb].oacc[mm][4 * x + e] * f;
-        red[(wave * NM * 4 + mm * 4 + x) * 64 + lane] = o;
-      }
+      for (int e = 0; e < 4; ++e) o[e] *= f;
+      red[(wave * CH + u) * 64 + lane] = o;
+    }
     __syncthreads();
-    const int row = qb * 32 + li;
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    for (int u = wave; u < NM * 4; u += NW) {  // features 8 u + 4 hh on of this lane's row
+    for (int u = wave; u < CH; u += NW) {
       f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        const f32x4_t x = red[(w * NM * 4 + u) * 64 + lane];
+        const f32x4_t x = red[(w * CH + u) * 64 + lane];
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += x[e];
       }
       if (row >= R) continue;
+      const int feature = q[qb].feature(u);
       if (pieces > 1) {
-        *reinterpret_cast<f32x4_t*>(A.part + ((head * A.splits + split) * A.rows + rbase + row) * D + 8 * u + 4 * hh) = o;
+        *reinterpret_cast<f32x4_t*>(A.part + ((long long)blockIdx.x * A.rows + rbase + row) * D + feature) = o;
       } else {
-        T* dst = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + q[qb].t) * g.o_st + (long long)q[qb].head * g.o_sh + 8 * u + 4 * hh;
+        T* dst = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + q[qb].t) * g.o_st + (long long)q[qb].head * g.o_sh + feature;
         store4<T>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
       }
     }
-    if (wave == 0 && hh == 0 && row < R) {
+    if (wave == 0 && q[qb].first_lane() && row < R) {
       if (pieces > 1)
-        A.sums[(head * A.splits + split) * A.rows + rbase + row] = make_float2(most, l);
+        A.sums[(long long)blockIdx.x * A.rows + rbase + row] = make_float2(most, l);
       else if (A.lse)
         A.lse[(long long)q[qb].head * g.T + v.row0 + q[qb].t] = l > 0.f ? (most + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
     }
   }
 }
 
-// A thread has four features of a row.
+// A row's pieces are shared out among `slices` groups of D / 4 threads, each thread with four features; what they have found meets in LDS.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void softmax_join_kernel(SoftmaxArgs A) {
-  constexpr int LR = D / 4, RW = kThreads / LR;  // threads of a row, rows of a workgroup
+__global__ __launch_bounds__(kThreads) void softmax_join_kernel(SoftmaxArgs A, int slices) {
+  constexpr int LR = D / 4;
+  __shared__ f32x4_t outs[kThreads];
+  __shared__ float2 found[kThreads / LR];
   const SeqGeom& g = A.g;
-  const int per = (A.rows + RW - 1) / RW;
-  const int row = (int)(blockIdx.x % per) * RW + (int)threadIdx.x / LR, s = blockIdx.x / per, hk = blockIdx.y, f = ((int)threadIdx.x % LR) * 4;
+  const int tid = threadIdx.x, group = tid / LR, slice = group % slices, f = (tid % LR) * 4, per_wg = kThreads / (LR * slices);
+  const int per = (A.rows + per_wg - 1) / per_wg, s = blockIdx.x / per, hk = blockIdx.y;
+  const int row = (int)(blockIdx.x % per) * per_wg + group / slices;
   SeqView v;
-  if (!load_seq(g, s, v) || !split_seq(g, v) || row >= v.n * g.G) return;
-  const int pieces = (v.L + A.piece - 1) / A.piece;
-  if (pieces <= 1) return;
-  const long long at = ((long long)s * g.Hkv + hk) * A.splits * A.rows + row;
+  SoftmaxShare sh;
+  if (!softmax_share<false>(A, s, v, sh) || sh.n <= 1) return;  // (the same for the workgroup)
+  const int pieces = sh.n;
+  const bool mine = row < v.n * g.G;
+  const long long at = ((long long)sh.first * g.Hkv + hk) * A.rows + (mine ? row : 0), step = (long long)g.Hkv * A.rows;
   float most = -kInf, l = 0.f;
-#pragma unroll 8
-  for (int k = 0; k < pieces; ++k) most = fmaxf(most, A.sums[at + (long long)k * A.rows].x);
+#pragma unroll 4
+  for (int k = slice; k < pieces; k += slices) most = fmaxf(most, A.sums[at + k * step].x);
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int k = 0; k < pieces; ++k) {
-    const float2 x = A.sums[at + (long long)k * A.rows];
-    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(A.part + (at + (long long)k * A.rows) * D + f);
+  for (int k = slice; k < pieces; k += slices) {
+    const float2 x = A.sums[at + k * step];
+    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(A.part + (at + k * step) * D + f);
     const float w = x.y > 0.f ? __builtin_amdgcn_exp2f(x.x - most) : 0.f;
     l = fmaf(x.y, w, l);
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
   }
+  if (slices > 1) {
+    outs[tid] = o;
+    if (f == 0) found[group] = make_float2(most, l);
+    __syncthreads();
+    if (slice != 0) return;
+    for (int k = 0; k < slices; ++k) most = fmaxf(most, found[group + k].x);
+    l = 0.f;
+    o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < slices; ++k) {
+      const float2 x = found[group + k];
+      const float w = x.y > 0.f ? __builtin_amdgcn_exp2f(x.x - most) : 0.f;
+      l = fmaf(x.y, w, l);
+      const f32x4_t y = outs[tid + k * LR];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
+    }
+  }
+  if (!mine) return;
   const int t = row / g.G, qh = hk * g.G + row - t * g.G;
   const float inv = l > 0.f ? 1.f / l : 0.f;
   T* dst = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + t) * g.o_st + (long long)qh * g.o_sh + f;
@@ -328,12 +669,13 @@ struct SoftmaxTiledCfg {
   static constexpr int kTileBytes = KT * D * (int)sizeof(T);
   static constexpr size_t kLdsBytes = 4 * (size_t)kTileBytes;
   static constexpr int kWavesPerSimd = sizeof(T) == 4 && D == 128 ? 1 : 2;
+  static constexpr int NB = sizeof(T) == 2 ? 2 : 1;  // blocks of 32 keys that a wave takes in together
 };
 
 template <typename T, int D, bool CAP>
 __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) void softmax_tiled_kernel(SoftmaxArgs A) {
   using Cfg = SoftmaxTiledCfg<T, D>;
-  constexpr int KT = Cfg::KT, NC = D / 16, NM = D / 32, TB = Cfg::kTileBytes;
+  constexpr int KT = Cfg::KT, NB = Cfg::NB, NC = D / 16, NM = D / 32, TB = Cfg::kTileBytes;
   using KTile = SeqTile<T, D, KT, false>;
   using Vals = SeqValues<T, D, KT>;
   using VTile = typename Vals::VT;
@@ -386,17 +728,25 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
     }
     const char* tile = smem + cur * 2 * TB;
 #pragma unroll 1
-    for (int sb = 0; sb < KT / 32; ++sb) {
-      const int j0 = t * KT + sb * 32;
+    for (int sb0 = 0; sb0 < KT / 32; sb0 += NB) {
+      const int j0 = t * KT + sb0 * 32;
       if (j0 >= q.lim_max) break;
-      const char* at = tile + sb * 32 * KTile::kRowBytes;
-      f32x16_t acc = q.scores(q.start(j0), [&](int cc) { return koff[cc].load(at, 0); });
-      if constexpr (CAP) q.cap_scores(acc, j0);
-      const bool masked = holes || j0 + 32 > q.lim_min;
-      if (masked) q.mask(acc, j0, keys, holes);
-      float p[16];
-      q.step(acc, p);
-      vv.accumulate(tile + TB, sb, p, masked, q.oacc);
+      f32x16_t acc[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const char* at = tile + (sb0 + b) * 32 * KTile::kRowBytes;
+        acc[b] = q.scores(q.start(j0 + 32 * b), [&](int cc) { return koff[cc].load(at, 0); });
+      }
+      const bool masked = holes || j0 + 32 * NB > q.lim_min;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        if constexpr (CAP) q.cap_scores(acc[b], j0 + 32 * b);
+        if (masked) q.mask(acc[b], j0 + 32 * b, keys, holes);
+      }
+      float p[NB][16];
+      q.template step<NB>(acc, p);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) vv.accumulate(tile + TB, sb0 + b, p[b], masked, q.oacc);
     }
     lds_loads_wait<0>();
     __syncthreads();
@@ -420,13 +770,13 @@ int run_softmax(const SoftmaxCall& c);
 
 namespace {
 
-// NQB: blocks of 32 rows of a workgroup
-template <typename T, int D, int NQB, bool CAP>
-bool launch_softmax_split(const SoftmaxArgs& a, hipStream_t st) {
+template <typename T, int D, class Rows, int NQB>
+bool launch_softmax_split(const SoftmaxArgs& a, long long places, hipStream_t st) {
   using Cfg = SoftmaxSplitCfg<T, D>;
-  constexpr auto kern = softmax_split_kernel<T, D, NQB, CAP>;
+  constexpr auto kern = softmax_split_kernel<T, D, Rows, NQB>;
   if (!ensure_dynamic_lds<kern>(Cfg::kLdsBytes)) return false;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(a.g.nseq * a.splits), (unsigned)a.g.Hkv, (unsigned)ceil_div(a.rows, NQB * 32)), dim3(Cfg::NW * 64), Cfg::kLdsBytes, st, a);
+  const dim3 grid((unsigned)places, 1, (unsigned)ceil_div(a.rows, NQB * Rows::kRows));
+  hipLaunchKernelGGL(kern, grid, dim3(Cfg::NW * 64), Cfg::kLdsBytes, st, a);
   return launch_ok();
 }
 
@@ -442,10 +792,15 @@ bool launch_softmax(const SoftmaxArgs& a, const SoftmaxLayout& L, hipStream_t st
   if (!L.split) return true;
   // (two blocks of fp32 rows of 128 features do not fit the registers)
   constexpr int kMostBlocks = sizeof(T) == 4 && D == 128 ? 1 : 2;
-  if (!(a.rows <= 32 ? launch_softmax_split<T, D, 1, CAP>(a, st) : launch_softmax_split<T, D, kMostBlocks, CAP>(a, st))) return false;
-  if (a.splits > 1) {
-    constexpr int RW = kThreads / (D / 4);
-    hipLaunchKernelGGL((softmax_join_kernel<T, D>), dim3((unsigned)(a.g.nseq * ceil_div(a.rows, RW)), (unsigned)a.g.Hkv), dim3(kThreads), 0, st, a);
+  const bool ok = a.rows <= 16   ? launch_softmax_split<T, D, SoftmaxRows16<T, D, CAP>, 1>(a, L.places, st)
+                  : a.rows <= 32 ? launch_softmax_split<T, D, SoftmaxRows<T, D, CAP>, 1>(a, L.places, st)
+                                 : launch_softmax_split<T, D, SoftmaxRows<T, D, CAP>, kMostBlocks>(a, L.places, st);
+  if (!ok) return false;
+  if (L.most_pieces > 1) {
+    int slices = 1;  // (a power of two: two pieces or more to each)
+    while (2 * slices <= kThreads / (D / 4) && 4 * slices <= L.most_pieces) slices *= 2;
+    const int per = ceil_div(a.rows, kThreads / (D / 4) / slices);
+    hipLaunchKernelGGL((softmax_join_kernel<T, D>), dim3((unsigned)(a.g.nseq * per), (unsigned)a.g.Hkv), dim3(kThreads), 0, st, a, slices);
     return launch_ok();
   }
   return true;
@@ -471,6 +826,8 @@ int run_softmax(const SoftmaxCall& c) {
   a.part = reinterpret_cast<float*>(c.ws + L.off_part);
   a.sums = reinterpret_cast<float2*>(c.ws + L.off_sums);
   a.rows = L.rows;
+  a.shared = L.shared ? 1 : 0;
+  a.budget = L.budget;
   a.piece = L.piece;
   a.splits = L.splits;
   a.nblk = (int)seq_blocks(p->nseq, p->T, a.g.G);

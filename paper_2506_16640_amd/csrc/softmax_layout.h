@@ -13,14 +13,26 @@ inline int check_softmax_params(const entmax_seq_params* p) {
   return p->page_size == 0 ? ENTMAX_ATTN_INVALID_ARG : ENTMAX_ATTN_OK;
 }
 
-// Waves of a workgroup of the kernel that splits the keys; each has two tiles of 32 keys and values in LDS
-inline int softmax_waves(const entmax_seq_params* p) { return p->dtype == ENTMAX_ATTN_FP32 && p->D == 128 ? 2 : 4; }
+// Waves of a workgroup of the kernel that splits the keys (element size, head dimension)
+template <int ES, int D>
+constexpr int kSoftmaxWaves = ES == 4 && D == 128 ? 2 : 4;
+
+// Workgroups of that kernel that are on the chip at a time: two on each compute unit
+constexpr int kSoftmaxSlots = 512;
+// Fewest 32-key tiles of a piece
+constexpr int kSoftmaxLeastTiles = 4;
+// With at most so many sequences their lengths decide how the keys are cut up (every wave looks at all of them), else the bound of the lengths
+constexpr int kSoftmaxSharedSeqs = 512;
 
 struct SoftmaxLayout {
   bool split;   // the call may hold sequences of at most kSplitRows folded rows
   bool blocks;  // it may hold others
   int rows;     // rows of a head there is room for
-  int piece, splits;  // keys of a workgroup, workgroups of a head
+  bool shared;  // see softmax_share()
+  int budget;
+  int piece, splits;   // keys of a piece, pieces of a sequence, where they are not shared
+  int most_pieces;     // of a sequence
+  long long places;    // workgroups
   size_t off_part, off_sums, total;
 };
 
@@ -33,13 +45,20 @@ inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
   size_t o = 0;
   if (L.split) {
     const long long heads = (long long)p->nseq * p->Hkv;
-    const int step = 32 * softmax_waves(p);
+    const int tiles = p->max_keys > 0 ? ceil_div(p->max_keys, 32) : 1;
     L.rows = (int)(most_rows < kSplitRows ? most_rows : kSplitRows);
-    L.piece = 2 * step;
-    while (L.piece < (1 << 20) && heads * ((p->max_keys + L.piece - 1) / L.piece) > 1024) L.piece *= 2;
-    L.splits = p->max_keys > 0 ? ceil_div(p->max_keys, L.piece) : 1;
-    if (L.splits > 1) {
-      const size_t n = (size_t)heads * L.splits * L.rows;
+    L.shared = p->nseq <= kSoftmaxSharedSeqs;
+    // (pieces are rounded up, by half a piece a head on average)
+    L.budget = heads < kSoftmaxSlots ? (int)(kSoftmaxSlots - heads / 2) : kSoftmaxSlots / 2;
+    L.piece = kSoftmaxLeastTiles * 32;
+    while (L.piece < (1 << 22) && heads * ceil_div(tiles, L.piece / 32) > 2 * kSoftmaxSlots) L.piece *= 2;
+    L.splits = ceil_div(tiles, L.piece / 32);
+    L.most_pieces = L.shared ? ceil_div(tiles, kSoftmaxLeastTiles) : L.splits;
+    L.places = heads * L.most_pieces;
+    // (shared: the sum of tiles / piece over the heads is at most the budget, and each of them is rounded up)
+    if (L.shared && L.places > L.budget + heads) L.places = L.budget + heads;
+    if (L.most_pieces > 1) {
+      const size_t n = (size_t)L.places * L.rows;
       L.off_part = o;
       o += align_up(n * p->D * sizeof(float));
       L.off_sums = o;
