@@ -17,6 +17,7 @@
 
 #include "common.hip.h"
 #include "sample_layout.h"
+#include "wave_ops.hip.h"
 
 using namespace entmax;
 
@@ -25,17 +26,15 @@ namespace {
 typedef unsigned long long u64;
 
 struct SliceStat {
-  double sum;   // of w relative to the slice's own largest logit
+  double sum;   // of w relative to the slice's own largest logit (rows without top-k)
   float top;
-  int arg;      // its lowest index
-  int finite;   // tokens that can be drawn
-  int pad;
+  int arg;      // its lowest index (rows that take the largest logit)
 };
 struct SliceKept {
   double all, sum;  // w of the tokens that are surely left by top-k and top-p; of those among them that min-p leaves
-  int listed, pad;
+  int listed, pad;  // tokens that have to be looked at
 };
-static_assert(sizeof(SliceStat) == kSampleStatBytes && sizeof(SliceKept) == kSampleStatBytes, "as in make_sample_layout()");
+static_assert(sizeof(SliceStat) == kSampleStatBytes && sizeof(SliceKept) == kSampleKeptBytes, "as in make_sample_layout()");
 
 struct SampleArgs {
   const void* logits;
@@ -48,19 +47,22 @@ struct SampleArgs {
   SliceStat* stat;
   float* hist;
   SliceKept* kept;
-  uint16_t* cand;
+  double* blocks;  // [slices][blocks of a slice] w of the tokens of each block, as in SliceKept::sum or SliceStat::sum
+  char* cand;   // [slices][tokens of a slice] Listed<T>
 };
 
 // What a row asks for.
 struct RowAsk {
   bool greedy, has_k, has_p, has_m;
   int k;
-  double inv, p, f, grid;
+  double scale, p, f;  // log2(w) of a logit of 1; top_p, min_p
+  float grid;          // bins of a logit of 1
   __device__ __forceinline__ void init(const SampleArgs& A, int row) {
     auto nan = [](float x) { return (opaque_bits(x) & 0x7fffffffu) > 0x7f800000u; };
     const float t = A.temperature ? A.temperature[row] : 1.f;
     greedy = nan(t) || !(t > 0.f);
-    inv = greedy ? 1.0 : 1.0 / (double)t;
+    const double inv = greedy ? 1.0 : 1.0 / (double)t;
+    scale = inv * 1.4426950408889634;
     k = A.top_k ? A.top_k[row] : 0;
     has_k = k > 0 && k < A.vocab;
     const float pp = A.top_p ? A.top_p[row] : 1.f, mm = A.min_p ? A.min_p[row] : 0.f;
@@ -68,42 +70,95 @@ struct RowAsk {
     p = has_p ? fmax((double)pp, 0.0) : 1.0;
     has_m = !nan(mm) && mm > 0.f;
     f = has_m ? fmin((double)mm, 1.0) : 0.0;
-    // Bins of a twelfth of the temperature: 256 of them reach down to 6e-10 of the largest w, and one holds a few per cent of the tokens of a flat
-    // row at most.  Not less than a twelfth of a logit, for top-k at low temperatures.
-    grid = greedy ? 0.0 : fmin(12.0 * inv, 12.0);
+    // top-p: bins of 1/24 of the temperature: 256 of them reach down to 2e-5 of the largest w, and the bin of the cut holds a few per cent of the
+    // tokens of a flat row at most.  top-k: 1/12 of it, but not less than 1/12 of a logit, for low temperatures.
+    grid = greedy ? 0.f : (float)fmin(has_k ? fmin(12.0 * inv, 12.0) : 24.0 * inv, 1e30);
   }
+  // 2^t, t <= 0, to 4e-14 of it and 1 for 0: the whole part goes to the exponent; the rest f, at most 1/2, through 1 + f p(f), p interpolating (2^f - 1) / f at the
+  // nine zeros of a Chebyshev polynomial.  (-infinity: undefined)
+  static __device__ __forceinline__ double power(double t) {
+    const double k = rint(t), f = t - k;
+    double p = 1.0203121172135084e-07;
+    p = fma(p, f, 1.3255224874051843e-06);
+    p = fma(p, f, 1.5252686845751599e-05);
+    p = fma(p, f, 0.00015403455852473414);
+    p = fma(p, f, 0.0013333558179043862);
+    p = fma(p, f, 0.009618129159402536);
+    p = fma(p, f, 0.055504108664760424);
+    p = fma(p, f, 0.2402265069581299);
+    p = fma(p, f, 0.6931471805599453);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)k);
+  }
+  // w of a logit x next to the largest, m
   __device__ __forceinline__ double weight(float x, float m) const {
-    if (x == m) return x == -kInf ? 0.0 : 1.0;  // (m may be infinite)
-    if (x == -kInf || m == kInf) return 0.0;
-    return exp(((double)x - (double)m) * inv);
+    if (m == kInf || m == -kInf) return x == m && x > 0.f ? 1.0 : 0.0;  // (uniform)
+    const double w = power(((double)x - (double)m) * scale);
+    return x == -kInf ? 0.0 : w;
   }
+  // The logit's place on the row's grid of bins.  (That it never falls as x rises is all that matters: bins of a row's slices are the same ones.)
   __device__ __forceinline__ int cell(float x) const {
     if (x == kInf) return 1 << 29;
     if (x == -kInf) return -(1 << 29);
-    return (int)fmax(fmin(floor((double)x * grid), (double)(1 << 29)), -(double)(1 << 29));
+    return (int)fminf(fmaxf(floorf(x * grid), -(float)(1 << 29)), (float)(1 << 29));
+  }
+  // The smallest logit of cell c or above (-inf: all of them are)
+  __device__ __forceinline__ float edge(int c) const {
+    if (c <= -(1 << 29)) return -kInf;
+    if (grid == 0.f) return c <= 0 ? -kInf : kInf;
+    float x = fminf(fmaxf((float)c / grid, -3.4e38f), 3.4e38f);
+    // (the quotient is rounded, and so are products: a few steps of a float away at most; with a step of zero nothing but infinity is left)
+    for (int k = 0; k < 8 && cell(x) >= c && x > -3.4e38f; ++k) x = next(x, -1);
+    for (int k = 0; k < 16 && cell(x) < c; ++k) x = next(x, 1);
+    return x;
+  }
+  static __device__ __forceinline__ float next(float x, int way) {  // the neighbour of a finite number (3.4e38's: infinity)
+    const int b = (int)__float_as_uint(x), order = b < 0 ? (int)(0x80000000u - (uint32_t)b) : b;
+    const int n = order + way;
+    return __uint_as_float(n < 0 ? 0x80000000u - (uint32_t)n : (uint32_t)n);
   }
 };
 
 // Falling order of logits, and of equal ones by index: larger numbers first.
 template <typename T>
 struct Rank {
-  static constexpr int kBits = 22 + 8 * (int)sizeof(T);
-  static __device__ __forceinline__ u64 of(float x, int index) {
+  static __device__ __forceinline__ uint32_t key(float x) {
     uint32_t b = __float_as_uint(x);
     if (b == 0x80000000u) b = 0u;  // (the two zeros are equal)
     b = (b & 0x80000000u) ? ~b : b | 0x80000000u;
-    if (sizeof(T) == 2) b >>= 16;
-    return (u64)b << 22 | (u64)(kSampleMostVocab - 1 - index);
+    return sizeof(T) == 2 ? b >> 16 : b;
+  }
+  static __device__ __forceinline__ u64 of(uint32_t key, int index) { return (u64)key << 22 | (u64)(kSampleMostVocab - 1 - index); }
+  static __device__ __forceinline__ u64 of(float x, int index) { return of(key(x), index); }
+  static __device__ __forceinline__ float logit(uint32_t key) {
+    if (sizeof(T) == 2) key = key << 16 | ((key & 0x8000u) ? 0u : 0xffffu);
+    return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
   }
 };
+// A listed token: key and place in its slice
+template <typename T>
+struct Listed {
+  typedef u64 Word;
+  static __device__ __forceinline__ Word pack(uint32_t key, int place) { return (u64)key << 16 | (u64)place; }
+  static __device__ __forceinline__ uint32_t key(Word w) { return (uint32_t)(w >> 16); }
+  static __device__ __forceinline__ int place(Word w) { return (int)(w & 0xffffu); }
+};
+template <>
+struct Listed<bf16_t> {
+  typedef uint32_t Word;
+  static __device__ __forceinline__ Word pack(uint32_t key, int place) { return key << 16 | (uint32_t)place; }
+  static __device__ __forceinline__ uint32_t key(Word w) { return w >> 16; }
+  static __device__ __forceinline__ int place(Word w) { return (int)(w & 0xffffu); }
+};
 
-constexpr int kSampleThreads = 1024;
+constexpr int kSampleThreads = 1024, kSampleWaves = kSampleThreads / 64;
 
 // A row's slice: thread t has the 16-byte chunks t, t + NT, ..; the slices' addresses are round, so that slice 0 may begin in front of the row.
 template <typename T, int NCH>
 struct Slice {
   static constexpr int NT = kSampleThreads;
   static constexpr int E = 16 / (int)sizeof(T), N = NCH * E, kSize = NT * N;
+  static constexpr int kBlock = 64 * E, kBlocks = kSize / kBlock;  // what a wave loads at a time: block c kSampleWaves + wave
   const T* row;
   int vocab, from;  // index of the slice's first place
   __device__ __forceinline__ void init(const SampleArgs& A, int r, int slice) {
@@ -119,9 +174,7 @@ struct Slice {
     else
       return clean(x);
   }
-  __device__ __forceinline__ float at(int i) const { return value(row[i]); }
-  __device__ __forceinline__ void load_chunk(int c, float* x) const {
-    const int i0 = index(c, 0);
+  __device__ __forceinline__ void load_chunk(int i0, float* x) const {
     if (i0 >= 0 && i0 + E <= vocab) {
       const u32x4_t v = *reinterpret_cast<const u32x4_t*>(row + i0);
 #pragma unroll
@@ -134,75 +187,42 @@ struct Slice {
   }
   __device__ __forceinline__ void load(float (&x)[N]) const {
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) load_chunk(c, x + c * E);
+    for (int c = 0; c < NCH; ++c) load_chunk(index(c, 0), x + c * E);
   }
 };
 
-// Sums, largest values over the workgroup, in a fixed order; buf: a number per wave.  (Two barriers.)
-template <int NT, typename V, class Op>
-__device__ __forceinline__ V reduce(V x, V* buf, Op op) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x = op(x, __shfl_xor(x, off));
+// A number below 2^52 as a whole one, by the place where the sum's bits end
+__device__ __forceinline__ u64 whole(double x) { return (u64)__double_as_longlong(x + 4503599627370496.0) & 0xfffffffffffffull; }
+// The sums of a workgroup's blocks, `part` a thread's w of each of its chunks; returns their sum, the same in every thread.  (Two barriers.)
+template <int NCH>
+__device__ __forceinline__ double sum_blocks(const double (&part)[NCH], double (&sums)[NCH * kSampleWaves], double* out) {
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  static_assert(NCH * kSampleWaves <= 64, "a lane each");
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = x;
-  __syncthreads();
-  V r = buf[threadIdx.x & (NT / 64 - 1)];
 #pragma unroll
-  for (int off = NT / 128; off >= 1; off >>= 1) r = op(r, __shfl_xor(r, off));
-  return r;
-}
-struct Add {
-  template <typename V>
-  __device__ __forceinline__ V operator()(V a, V b) const {
-    return a + b;
-  }
-};
-struct Most {
-  template <typename V>
-  __device__ __forceinline__ V operator()(V a, V b) const {
-    return a > b ? a : b;
-  }
-};
-struct Least {
-  template <typename V>
-  __device__ __forceinline__ V operator()(V a, V b) const {
-    return a < b ? a : b;
-  }
-};
-
-// Sums over the threads up to and with this one.
-template <int NT>
-__device__ __forceinline__ double scan(double x, double* buf, double& total) {
-  constexpr int NW = NT / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double y = __shfl_up(x, off);
-    if (lane >= off) x += y;
+  for (int c = 0; c < NCH; ++c) {
+    const double x = wave_reduce(part[c], 0.0, Add());
+    if (lane == 0) sums[c * kSampleWaves + wave] = x;
   }
   __syncthreads();
-  if (lane == 63) buf[wave] = x;
-  __syncthreads();
-  double w = buf[lane & (NW - 1)];
-#pragma unroll
-  for (int off = 1; off < NW; off <<= 1) {
-    const double y = __shfl_up(w, off);
-    if ((lane & (NW - 1)) >= off) w += y;
-  }
-  total = __shfl(w, NW - 1);
-  const double before = __shfl(w, wave > 0 ? wave - 1 : 0);
-  return x + (wave > 0 ? before : 0.0);
+  const double x = lane < NCH * kSampleWaves ? sums[lane] : 0.0;
+  if (out && wave == 0 && lane < NCH * kSampleWaves) out[lane] = x;
+  return wave_reduce(x, 0.0, Add());
 }
 
-// w in whole steps of 2^-44: a slice's sum stays below 2^58
+// What the rounding of w and of sums of them stays far below: numbers that are nearer to each other than this part of them are taken as equal
+constexpr double kRounding = 2.3e-13;
+// w in whole steps of 2^-44 where slices' bins are added up: a slice's sum stays below 2^58
 constexpr double kSliceSteps = 17592186044416.0;
 
+// (two workgroups to a compute unit: at most 64 registers)
 template <typename T, int NCH>
-__global__ __launch_bounds__(kSampleThreads) void sample_slices_kernel(SampleArgs A) {
+__global__ __launch_bounds__(kSampleThreads, 8) void sample_slices_kernel(SampleArgs A) {
   constexpr int NT = kSampleThreads;
   using S = Slice<T, NCH>;
-  __shared__ u64 buf[NT / 64];
+  __shared__ u64 buf[kSampleWaves];
   __shared__ u64 bins[kSampleBins];
+  __shared__ double sums[S::kBlocks];
   const int row = blockIdx.x / A.nslices, slice = blockIdx.x - row * A.nslices, tid = threadIdx.x;
   S sl;
   sl.init(A, row, slice);
@@ -210,156 +230,267 @@ __global__ __launch_bounds__(kSampleThreads) void sample_slices_kernel(SampleArg
   sl.load(x);
   RowAsk ask;
   ask.init(A, row);
-  u64 best = 0;
-  int finite = 0;
+  const bool binned = !ask.greedy && (ask.has_k || ask.has_p);
+  if (binned && tid < kSampleBins) bins[tid] = 0;
+  float top = x[0];
 #pragma unroll
-  for (int c = 0; c < NCH; ++c)
-#pragma unroll
-    for (int e = 0; e < S::E; ++e) {
-      const float v = x[c * S::E + e];
-      if (v == -kInf) continue;
-      ++finite;
-      const u64 r = Rank<float>::of(v, sl.index(c, e));
-      best = r > best ? r : best;
-    }
-  best = reduce<NT>(best, buf, Most());
-  finite = reduce<NT>(finite, reinterpret_cast<int*>(buf), Add());
-  float top = -kInf;
-  if (best) {
-    const uint32_t b = (uint32_t)(best >> 22);
-    top = __uint_as_float((b & 0x80000000u) ? b & 0x7fffffffu : ~b);
-  }
+  for (int e = 1; e < S::N; ++e) top = fmaxf(top, x[e]);
+  top = block_reduce<kSampleWaves>(top, -kInf, reinterpret_cast<float*>(buf), Most());
   const long long at = (long long)row * A.nslices + slice;
   double sum = 0.0;
-  if (!ask.greedy && best) {  // (uniform)
-    const bool binned = ask.has_k || ask.has_p;
-    if (binned) {
-      if (tid < kSampleBins) bins[tid] = 0;
-      __syncthreads();
-    }
-    const int cell = ask.cell(top);
+  int arg = kSampleMostVocab;
+  if (ask.greedy) {  // (uniform, like the other ways here)
 #pragma unroll
-    for (int e = 0; e < S::N; ++e) {
-      if (x[e] == -kInf) continue;
-      const double w = ask.has_k ? 0.0 : ask.weight(x[e], top);
-      sum += w;
-      const int b = binned ? cell - ask.cell(x[e]) : kSampleBins;
-      if (b < kSampleBins - 1) atomicAdd(&bins[b], ask.has_k ? 1ull : (u64)(w * kSliceSteps + 0.5));
+    for (int c = NCH - 1; c >= 0; --c)
+#pragma unroll
+      for (int e = S::E - 1; e >= 0; --e) arg = x[c * S::E + e] == top ? sl.index(c, e) : arg;
+    arg = block_reduce<kSampleWaves>(arg, kSampleMostVocab, reinterpret_cast<int*>(buf), Least());
+  } else if (top > -kInf && (binned || !ask.has_m)) {  // (with min-p alone the next kernel sums up what it leaves)
+    const int cell = ask.cell(top);
+    if (ask.has_k) {
+#pragma unroll
+      for (int e = 0; e < S::N; ++e) {
+        const int b = cell - ask.cell(x[e]);
+        if (b < kSampleBins - 1) atomicAdd(&bins[b], 1ull);
+      }
+      __syncthreads();
+    } else {
+      double part[NCH];
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) {
+        part[c] = 0.0;
+#pragma unroll
+        for (int e = 0; e < S::E; ++e) {
+          const float v = x[c * S::E + e];
+          const double w = ask.weight(v, top);
+          part[c] += w;
+          if (binned) {
+            const int b = cell - ask.cell(v);
+            if (b < kSampleBins - 1) atomicAdd(&bins[b], whole(w * kSliceSteps));
+          }
+        }
+      }
+      sum = sum_blocks<NCH>(part, sums, binned ? nullptr : A.blocks + at * S::kBlocks);
     }
-    sum = reduce<NT>(sum, reinterpret_cast<double*>(buf), Add());
     if (binned && tid < kSampleBins) A.hist[at * kSampleBins + tid] = ask.has_k ? (float)bins[tid] : (float)((double)bins[tid] / kSliceSteps);
   }
-  if (tid == 0) A.stat[at] = SliceStat{sum, top, best ? kSampleMostVocab - 1 - (int)(best & (kSampleMostVocab - 1)) : -1, finite, 0};
+  if (tid == 0) A.stat[at] = SliceStat{sum, top, arg};
 }
 
-// What the slices say of a row, the same in every thread.
+// What the slices say of a row; the lanes of one wave together.
 struct RowStat {
   float top;
-  int finite;
   double sum;  // of w, relative to the row's largest (rows without top-k)
 };
-template <int NT>
-__device__ __forceinline__ RowStat row_stat(const SampleArgs& A, const RowAsk& ask, int row, u64* buf) {
+__device__ __forceinline__ RowStat row_stat(const SampleArgs& A, const RowAsk& ask, int row) {
   const SliceStat* st = A.stat + (long long)row * A.nslices;
-  float top = -kInf;
-  int finite = 0;
-  for (int s = threadIdx.x; s < A.nslices; s += NT) {
-    top = fmaxf(top, st[s].top);
-    finite += st[s].finite;
-  }
-  RowStat r;
-  r.top = reduce<NT>(top, reinterpret_cast<float*>(buf), Most());
-  r.finite = reduce<NT>(finite, reinterpret_cast<int*>(buf), Add());
-  double sum = 0.0;
+  const int lane = threadIdx.x & 63;
+  RowStat r{-kInf, 0.0};
+  for (int s = lane; s < A.nslices; s += 64) r.top = fmaxf(r.top, st[s].top);
+  r.top = wave_reduce(r.top, -kInf, Most());
   if (!ask.greedy && !ask.has_k)
-    for (int s = threadIdx.x; s < A.nslices; s += NT) sum += st[s].sum * ask.weight(st[s].top, r.top);
-  r.sum = reduce<NT>(sum, reinterpret_cast<double*>(buf), Add());
+    for (int s = lane; s < A.nslices; s += 64) r.sum += st[s].sum * ask.weight(st[s].top, r.top);
+  r.sum = wave_reduce(r.sum, 0.0, Add());
   return r;
 }
 
+constexpr int kSampleMostSlices = kSampleMostVocab / kSampleLargeSlice + 1;
+
 template <typename T, int NCH>
-__global__ __launch_bounds__(kSampleThreads) void sample_bracket_kernel(SampleArgs A) {
+__global__ __launch_bounds__(kSampleThreads, 8) void sample_bracket_kernel(SampleArgs A) {
   constexpr int NT = kSampleThreads;
   using S = Slice<T, NCH>;
-  __shared__ u64 buf[NT / 64];
-  __shared__ int listed;
-  const int row = blockIdx.x / A.nslices, slice = blockIdx.x - row * A.nslices, tid = threadIdx.x;
+  using L = Listed<T>;
+  __shared__ double sums[2][S::kBlocks];
+  __shared__ double bins[4][kSampleBins], factor[kSampleMostSlices];
+  __shared__ int shift[kSampleMostSlices], listed;
+  const int row = blockIdx.x / A.nslices, slice = blockIdx.x - row * A.nslices, tid = threadIdx.x, lane = tid & 63;
   RowAsk ask;
   ask.init(A, row);
   if (ask.greedy || !(ask.has_k || ask.has_p || ask.has_m)) return;
   S sl;
   sl.init(A, row, slice);
-  float x[S::N];
-  sl.load(x);
-  const RowStat r = row_stat<NT>(A, ask, row, buf);
-  const int cell = ask.cell(r.top);
-  int b0 = kSampleBins, b1 = -1;  // tokens in bins below b0 are surely kept, those of b0 .. b1 listed
-  if (ask.has_k || ask.has_p) {
-    // the row's bins: thread b adds up its bin over the slices, in their order; what lies in no bin is in the last
+  float x[S::E];
+  sl.load_chunk(sl.index(0, 0), x);
+  // What belongs to the row is worked out by the first wave alone: every wave at it, they would wait for each other's turn to issue
+  __shared__ RowStat stat;
+  __shared__ int b0_, b1_;  // tokens in bins below b0 are surely kept, those of b0 .. b1 listed
+  __shared__ float sure_, list_;  // sure ones are at least `sure`, listed ones at least `list`
+  const bool binned = ask.has_k || ask.has_p;
+  if (tid < 64) {
+    const RowStat r = row_stat(A, ask, row);
+    const int cell = ask.cell(r.top);
     const SliceStat* st = A.stat + (long long)row * A.nslices;
-    const float* hist = A.hist + (long long)row * A.nslices * kSampleBins;
-    double mine = 0.0;
-    if (tid < kSampleBins - 1)
-      for (int s = 0; s < A.nslices; ++s) {
+    if (binned)
+      for (int s = lane; s < A.nslices; s += 64) {
         const float top = st[s].top;
-        if (top == -kInf) continue;
-        const int b = tid - (cell - ask.cell(top));
-        if (b >= 0) mine += (double)hist[s * kSampleBins + b] * (ask.has_k ? 1.0 : ask.weight(top, r.top));
+        factor[s] = top == -kInf ? 0.0 : (ask.has_k ? 1.0 : ask.weight(top, r.top));
+        shift[s] = top == -kInf ? kSampleBins : cell - ask.cell(top);
       }
-    double all;
-    const double upto = scan<NT>(mine, reinterpret_cast<double*>(buf), all);
-    // where the sum reaches what is to be kept.  Sums of w: a little less and a little more of it, for the rounding of the bins
-    const double least = ask.has_k ? (double)ask.k : ask.p * r.sum * (1.0 - 1e-5), most = ask.has_k ? (double)ask.k : ask.p * r.sum * (1.0 + 1e-5);
-    const int n0 = __syncthreads_count(tid < kSampleBins - 1 && upto < least), n1 = __syncthreads_count(tid < kSampleBins - 1 && upto < most);
-    b0 = ask.has_k ? 0 : n0;  // (what top-p takes its part of is the w of top-k's tokens: they are all listed)
-    b1 = n1;
+    if (lane == 0) {
+      stat = r;
+      listed = 0;
+    }
   }
-  if (tid == 0) listed = 0;
   __syncthreads();
-  double sum_all = 0.0, sum = 0.0;
+  const RowStat r = stat;
+  if (binned) {
+    // the row's bins: four threads to each add it up over a quarter of the slices; what lies in no bin is in the last
+    const float* hist = A.hist + (long long)row * A.nslices * kSampleBins;
+    static_assert(NT == 4 * kSampleBins, "a quarter each");
+    const int bin = tid & (kSampleBins - 1);
+    double mine = 0.0;
+#pragma unroll 4
+    for (int s = tid / kSampleBins; s < A.nslices; s += 4) {
+      const int b = bin - shift[s];
+      if (b >= 0 && bin < kSampleBins - 1) mine += (double)hist[s * kSampleBins + b] * factor[s];
+    }
+    bins[tid / kSampleBins][bin] = mine;
+    __syncthreads();
+  }
+  if (tid < 64) {
+    int b0 = kSampleBins, b1 = -1;
+    if (binned) {
+      // where the sum reaches what is to be kept, four bins a lane.  Sums of w: a little less and a little more of it, for the rounding of the bins
+      const double least = ask.has_k ? (double)ask.k : ask.p * r.sum * (1.0 - 1e-5), most = ask.has_k ? (double)ask.k : ask.p * r.sum * (1.0 + 1e-5);
+      double v[4], upto = 0.0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int b = 4 * lane + j;
+        v[j] = (bins[0][b] + bins[1][b]) + (bins[2][b] + bins[3][b]);
+        upto += v[j];
+      }
+      const double mine = upto;
+      upto = wave_scan(upto, 0.0, Add()) - mine;
+      int n0 = 0, n1 = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        upto += v[j];
+        const bool in = 4 * lane + j < kSampleBins - 1;
+        n0 += (int)__popcll(__ballot(in && upto < least));
+        n1 += (int)__popcll(__ballot(in && upto < most));
+      }
+      b0 = ask.has_k ? 0 : n0;  // (what top-p takes its part of is the w of top-k's tokens: they are all listed)
+      b1 = n1;
+    }
+    const int cell = ask.cell(r.top);
+    float sure = b0 == 0 ? kInf : (b0 == kSampleBins ? -kInf : ask.edge(cell - b0 + 1));
+    // min-p without top-p: of what is a little below its bound no w is wanted
+    if (ask.has_m && !ask.has_p && r.top < kInf) sure = fmaxf(sure, RowAsk::next((float)((double)r.top + (log2(ask.f) - 1e-3) / ask.scale), -1));
+    if (lane == 0) {
+      b0_ = b0;
+      b1_ = b1;
+      sure_ = sure;
+      list_ = b1 == kSampleBins - 1 ? -kInf : ask.edge(cell - b1);
+    }
+  }
+  __syncthreads();
+  const int b0 = b0_, b1 = b1_;
+  const float sure = sure_, list = list_;
   const long long at = (long long)row * A.nslices + slice;
-  uint16_t* cand = A.cand + at * S::kSize;
+  typename L::Word* cand = reinterpret_cast<typename L::Word*>(A.cand) + at * S::kSize;
+#pragma unroll 1
+  for (int c = 0; c < NCH; ++c) {  // (one chunk at a time, the next one under way: two workgroups fit a compute unit)
+    float v[S::E];
 #pragma unroll
-  for (int c = 0; c < NCH; ++c)
+    for (int e = 0; e < S::E; ++e) v[e] = x[e];
+    if (c + 1 < NCH) sl.load_chunk(sl.index(c + 1, 0), x);
+    double part_all = 0.0, part = 0.0;
 #pragma unroll
-    for (int e = 0; e < S::E; ++e) {
-      const float v = x[c * S::E + e];
-      const int b = v == -kInf ? kSampleBins : min(cell - ask.cell(v), kSampleBins - 1);
-      if (b < b0) {
-        const double w = ask.weight(v, r.top);
-        sum_all += w;
-        sum += w >= ask.f ? w : 0.0;
-      } else if (b <= b1) {
-        cand[atomicAdd(&listed, 1)] = (uint16_t)((c * NT + tid) * S::E + e);
+    for (int e = 0; e < S::E; ++e) {  // (branches that a wave takes as one)
+      const bool in = v[e] > -kInf, kept = in && b0 > 0 && v[e] >= sure;
+      if (__ballot(kept)) {
+        const double w = kept ? ask.weight(v[e], r.top) : 0.0;
+        part_all += w;
+        part += w >= ask.f ? w : 0.0;
+      }
+      const bool open = in && !kept && b1 >= 0 && v[e] >= list;
+      const u64 lanes = __ballot(open);
+      if (lanes) {
+        int first = 0;
+        if (lane == 0) first = atomicAdd(&listed, (int)__popcll(lanes));
+        first = lane_value(first, 0) + (int)__popcll(lanes & ((1ull << lane) - 1));
+        if (open) cand[first] = L::pack(Rank<T>::key(v[e]), (c * NT + tid) * S::E + e);
       }
     }
-  sum_all = reduce<NT>(sum_all, reinterpret_cast<double*>(buf), Add());
-  sum = reduce<NT>(sum, reinterpret_cast<double*>(buf), Add());
-  if (tid == 0) A.kept[at] = SliceKept{sum_all, sum, listed, 0};
+    if (b0 > 0) {  // (uniform)
+      part_all = wave_reduce(part_all, 0.0, Add());
+      part = ask.has_m ? wave_reduce(part, 0.0, Add()) : part_all;
+      if (lane == 0) {
+        sums[0][c * kSampleWaves + (tid >> 6)] = part_all;
+        sums[1][c * kSampleWaves + (tid >> 6)] = part;
+      }
+    }
+  }
+  __syncthreads();
+  if (tid < 64) {
+    const double all = b0 > 0 && lane < S::kBlocks ? sums[0][lane] : 0.0, sum = b0 > 0 && lane < S::kBlocks ? sums[1][lane] : 0.0;
+    if (lane < S::kBlocks) A.blocks[at * S::kBlocks + lane] = sum;
+    const double total_all = wave_reduce(all, 0.0, Add()), total = wave_reduce(sum, 0.0, Add());
+    if (lane == 0) A.kept[at] = SliceKept{total_all, total, listed, 0};
+  }
 }
 
-constexpr int kPickList = 6144;    // listed tokens that stay in LDS; longer lists are looked up again for every pass
+constexpr int kPickList = 7680;    // listed tokens that stay in LDS; longer lists are looked up again for every pass
 
 struct PickLds {
-  u64 buf[kSampleThreads / 64];
-  u64 bins[kSampleBins];
+  u64 buf[kSampleWaves];
+  u64 bins[2][kSampleBins];        // in use, and cleared meanwhile: these four
+  uint32_t least_key[2], most_key[2];
+  int few[2];
+  ulonglong2 few_of[64];           // (rank, amount)
+  u64 above[64];                   // amount, number of the others above each of them: zero but while in use
+  int place[64];
+  u64 lo, hi, before, result;
   u64 rank[kPickList];
-  u64 steps[kPickList];   // w in steps
-  int cut_bin;
-  u64 before;
+  u64 steps[kPickList];            // w in steps
+  uint16_t slice[kPickList];
+  int first[kSampleMostSlices + 1];  // the slices' first places in the list
+  u64 kept[kSampleMostSlices];     // steps of the listed tokens that are left
+  u64 block[64];                   // the same of the blocks of the chosen slice
+  u64 total;
+  double sums[kSampleMostSlices];  // w of the slices that is left
 };
 
 template <typename T, int NCH>
 __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs A, int filtered) {
   constexpr int NT = kSampleThreads;
   using S = Slice<T, NCH>;
+  using L = Listed<T>;
   __shared__ PickLds lds;
-  const int row = blockIdx.x, tid = threadIdx.x;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   RowAsk ask;
   ask.init(A, row);
-  const RowStat r = row_stat<NT>(A, ask, row, lds.buf);
   const long long at = (long long)row * A.nslices;
-  if (r.finite == 0) {
+  const bool cuts = filtered && !ask.greedy && (ask.has_k || ask.has_p), sums = filtered && (cuts || ask.has_m);
+  int listed = 0;
+  if (cuts) {  // how many each slice has listed, and what they have surely kept
+    for (int s = tid; s < A.nslices; s += NT) {
+      lds.first[s + 1] = A.kept[at + s].listed;
+      lds.sums[s] = A.kept[at + s].all;
+      lds.kept[s] = 0;
+    }
+    if (tid < 64) {
+      lds.block[tid] = 0;
+      lds.above[tid] = 0;
+      lds.place[tid] = 0;
+    }
+    if (tid < 2) {
+      lds.least_key[tid] = ~0u;
+      lds.most_key[tid] = 0;
+      lds.few[tid] = 0;
+    }
+    for (int b = tid; b < 2 * kSampleBins; b += NT) (&lds.bins[0][0])[b] = 0;
+    if (tid == 0) lds.first[0] = 0, lds.total = 0;
+  }
+  __shared__ RowStat stat;
+  if (tid < 64) {  // (see the kernel before)
+    const RowStat r = row_stat(A, ask, row);
+    if (lane == 0) stat = r;
+  }
+  __syncthreads();
+  const RowStat r = stat;
+  if (r.top == -kInf) {
     if (tid == 0) {
       A.token[row] = -1;
       if (A.logprob) A.logprob[row] = -kInf;
@@ -368,125 +499,177 @@ __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs 
   }
   if (ask.greedy) {
     int arg = kSampleMostVocab;
-    for (int s = tid; s < A.nslices; s += NT)
+    for (int s = lane; s < A.nslices; s += 64)
       if (A.stat[at + s].top == r.top) arg = min(arg, A.stat[at + s].arg);
-    arg = reduce<NT>(arg, reinterpret_cast<int*>(lds.buf), Least());
+    arg = wave_reduce(arg, kSampleMostVocab, Least());
     if (tid == 0) {
       A.token[row] = arg;
       if (A.logprob) A.logprob[row] = 0.f;
     }
     return;
   }
-  const bool cuts = filtered && (ask.has_k || ask.has_p), sums = filtered && (cuts || ask.has_m);
   u64 cut = 0;  // tokens of this rank and above are left by top-k and top-p
-  int listed = 0;
   double steps = 1.0;  // steps of w that make 1
-  // every listed token: fn(rank, w in steps)
+  if (cuts) {
+    if (tid < 64) {  // sums up to and with each slice
+      int run = 0;
+      for (int s0 = 0; s0 < A.nslices; s0 += 64) {
+        const int s = s0 + lane;
+        const int n = wave_scan(s < A.nslices ? lds.first[s + 1] : 0, 0, Add());
+        if (s < A.nslices) lds.first[s + 1] = run + n;
+        run += lane_value(n, 63);
+      }
+    }
+    __syncthreads();
+    listed = lds.first[A.nslices];
+    steps = exp2((double)(62 - (32 - __clz(listed | 1))));  // (w <= 1: sums stay below 2^63)
+  }
+  const bool held = listed <= kPickList;
+  const int from0 = -(int)((reinterpret_cast<uintptr_t>(reinterpret_cast<const T*>(A.logits) + (long long)row * A.stride) & 15u) / sizeof(T));
+  auto in_steps = [&](float x) { return (u64)(ask.weight(x, r.top) * steps + 0.5); };
+  // every listed token: fn(rank, w in steps, slice)
   auto each = [&](auto fn) {
-    if (listed <= kPickList) {
-      for (int i = tid; i < listed; i += NT) fn(lds.rank[i], lds.steps[i]);
+    if (held) {
+      for (int i = tid; i < listed; i += NT) fn(lds.rank[i], lds.steps[i], (int)lds.slice[i]);
       return;
     }
     for (int s = 0; s < A.nslices; ++s) {
-      S sl;
-      sl.init(A, row, s);
-      const int n = A.kept[at + s].listed;
-      const uint16_t* cand = A.cand + (at + s) * S::kSize;
+      const int n = lds.first[s + 1] - lds.first[s];
+      const typename L::Word* cand = reinterpret_cast<const typename L::Word*>(A.cand) + (at + s) * S::kSize;
+#pragma unroll 4
       for (int i = tid; i < n; i += NT) {
-        const int j = sl.from + cand[i];
-        const float x = sl.at(j);
-        fn(Rank<T>::of(x, j), (u64)(ask.weight(x, r.top) * steps + 0.5));
+        const typename L::Word w = cand[i];
+        fn(Rank<T>::of(L::key(w), from0 + s * S::kSize + L::place(w)), in_steps(Rank<T>::logit(L::key(w))), s);
       }
     }
   };
+  int turn = 0;  // which of the two sets of bins and limits is in use
   // Of the listed tokens of rank >= least and with an amount: the rank of the last one in falling order before which the amounts add up to less than
-  // `target` (at least 1).
+  // `target` (at least 1).  Bins over the ranks narrow them down to at most 64, which are compared with each other.
   auto select = [&](u64 target, u64 least, auto amount) {
-    u64 lo = ~0ull, hi = 0;
-    each([&](u64 k, u64 w) {
-      if (k < least || amount(w) == 0) return;
-      lo = k < lo ? k : lo;
-      hi = k > hi ? k : hi;
-    });
-    lo = reduce<NT>(lo, lds.buf, Least());
-    hi = reduce<NT>(hi, lds.buf, Most());
-    if (lo > hi) return least;  // (none has)
-    u64 before = 0;  // amount of the ranks above hi
-    while (lo < hi) {  // the rank is in lo .. hi, which agree above bit `shift + 8`
-      const int shift = max(0, 64 - __clzll((long long)(lo ^ hi)) - 8);
-      __syncthreads();
-      if (tid < kSampleBins) lds.bins[tid] = 0;
-      __syncthreads();
-      each([&](u64 k, u64 w) {
-        if (k >= lo && k <= hi) atomicAdd(&lds.bins[(k >> shift) & 255], amount(w));
+    u64 before = 0;  // amount of the ranks above those that are left
+    bool few = listed <= 64;
+    int n = listed;
+    if (!few) {
+      uint32_t least_key = ~0u, most_key = 0;
+      each([&](u64 k, u64 w, int) {
+        if (k < least || amount(w) == 0) return;
+        const uint32_t key = (uint32_t)(k >> 22);
+        least_key = min(least_key, key);
+        most_key = max(most_key, key);
       });
-      __syncthreads();
-      // bins from the highest down: the last one with something in it, before which the sum is below the target
-      if (tid < 64) {
-        u64 v[4], mine = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[j] = lds.bins[255 - 4 * tid - j];
-          mine += v[j];
-        }
-        u64 upto = mine;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-          const u64 y = __shfl_up(upto, off);
-          if (tid >= off) upto += y;
-        }
-        u64 sum = before + upto - mine, b_before = 0;
-        int b = -1;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (v[j] != 0 && sum < target) {
-            b = 255 - 4 * tid - j;
-            b_before = sum;
-          }
-          sum += v[j];
-        }
-        const u64 lanes = __ballot(b >= 0);
-        const int lane = 63 - __clzll((long long)lanes);
-        if (tid == lane) {
-          lds.cut_bin = b;
-          lds.before = b_before;
-        }
+      least_key = wave_reduce(least_key, ~0u, Least());
+      most_key = wave_reduce(most_key, 0u, Most());
+      if (lane == 0) {
+        atomicMin(&lds.least_key[turn], least_key);
+        atomicMax(&lds.most_key[turn], most_key);
       }
       __syncthreads();
-      const u64 base = ((lo >> shift) & ~255ull) + (u64)lds.cut_bin;
-      before = lds.before;
-      // the ranks of that bin, closed in on
-      const u64 from = max(lo, base << shift), to = min(hi, ((base + 1) << shift) - 1);
-      u64 l = ~0ull, h = 0;
-      each([&](u64 k, u64 w) {
-        if (k < from || k > to || amount(w) == 0) return;
-        l = k < l ? k : l;
-        h = k > h ? k : h;
-      });
-      lo = reduce<NT>(l, lds.buf, Least());
-      hi = reduce<NT>(h, lds.buf, Most());
+      least_key = lds.least_key[turn];
+      most_key = lds.most_key[turn];
+      if (least_key > most_key) return least;  // (none has an amount; nothing was changed)
+      u64 lo = (u64)least_key << 22, hi = ((u64)most_key << 22) | (kSampleMostVocab - 1);
+      while (!few) {  // the rank is in lo .. hi, which agree above bit `shift + 8`
+        const int shift = max(0, 64 - __clzll((long long)(lo ^ hi)) - 8);
+        each([&](u64 k, u64 w, int) {
+          if (k >= lo && k <= hi && k >= least) atomicAdd(&lds.bins[turn][(k >> shift) & 255], amount(w));
+        });
+        if (tid < kSampleBins) lds.bins[turn ^ 1][tid] = 0;
+        if (tid == 0) {
+          lds.least_key[turn ^ 1] = ~0u;
+          lds.most_key[turn ^ 1] = 0;
+          lds.few[turn ^ 1] = 0;
+        }
+        __syncthreads();
+        // bins from the highest down: the last one with something in it, before which the sum is below the target
+        if (tid < 64) {
+          u64 v[4], mine = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v[j] = lds.bins[turn][255 - 4 * lane - j];
+            mine += v[j];
+          }
+          u64 sum = before + wave_scan(mine, (u64)0, Add()) - mine, b_before = 0;
+          int b = -1;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (v[j] != 0 && sum < target) {
+              b = 255 - 4 * lane - j;
+              b_before = sum;
+            }
+            sum += v[j];
+          }
+          const int last = 63 - __clzll((long long)__ballot(b >= 0));
+          if (lane == last) {
+            const u64 base = ((lo >> shift) & ~255ull) + (u64)b;
+            lds.before = b_before;
+            lds.lo = max(lo, base << shift);
+            lds.hi = min(hi, ((base + 1) << shift) - 1);
+          }
+        }
+        __syncthreads();
+        before = lds.before;
+        lo = lds.lo;
+        hi = lds.hi;
+        each([&](u64 k, u64 w, int) {
+          if (k < lo || k > hi || k < least || amount(w) == 0) return;
+          const int at = atomicAdd(&lds.few[turn], 1);
+          if (at < 64) lds.few_of[at] = make_ulonglong2(k, amount(w));
+        });
+        __syncthreads();
+        n = lds.few[turn];
+        few = n <= 64;
+        turn ^= 1;
+      }
     }
-    return lo;
+    auto of = [&](int i) {
+      if (listed > 64) return lds.few_of[i];
+      return make_ulonglong2(lds.rank[i], lds.rank[i] < least ? 0 : amount(lds.steps[i]));
+    };
+    const ulonglong2 mine = lane < n ? of(lane) : make_ulonglong2(0, 0);
+    u64 above = 0;
+    int place = 0;
+    for (int j = tid >> 6; j < n; j += kSampleWaves) {
+      const ulonglong2 x = of(j);
+      above += x.x > mine.x ? x.y : 0;
+      place += x.x > mine.x && x.y != 0 ? 1 : 0;
+    }
+    if (lane < n) {
+      atomicAdd(&lds.above[lane], above);
+      atomicAdd(&lds.place[lane], place);
+    }
+    __syncthreads();
+    if (tid < 64) {
+      above = before + lds.above[lane];
+      place = lds.place[lane];
+      lds.above[lane] = 0;
+      lds.place[lane] = 0;
+      const u64 kept = __ballot(mine.y != 0 && above < target);  // the first ones in falling order
+      const bool end = mine.y != 0 && place == (int)__popcll(kept) - 1;
+      if (kept == 0 ? lane == 0 : end) lds.result = kept == 0 ? least : mine.x;
+    }
+    __syncthreads();
+    return lds.result;
+  };
+  // steps of a listed token that top-k, top-p and min-p leave
+  auto left_of = [&](u64 k, u64 w) -> u64 {
+    if (k < cut) return 0;
+    return !ask.has_m || ask.weight(Rank<T>::logit((uint32_t)(k >> 22)), r.top) >= ask.f ? w : 0;
   };
   if (cuts) {
-    int n = 0;
-    for (int s = tid; s < A.nslices; s += NT) n += A.kept[at + s].listed;
-    listed = reduce<NT>(n, reinterpret_cast<int*>(lds.buf), Add());
-    steps = exp2((double)(62 - (32 - __clz(listed | 1))));  // (w <= 1: sums stay below 2^63)
-    if (listed <= kPickList) {
-      int first = 0;
-      for (int s = 0; s < A.nslices; ++s) {
-        S sl;
-        sl.init(A, row, s);
-        const int m = A.kept[at + s].listed;
-        const uint16_t* cand = A.cand + (at + s) * S::kSize;
-        for (int i = tid; i < m; i += NT) {
-          const int j = sl.from + cand[i];
-          const float x = sl.at(j);
-          lds.rank[first + i] = Rank<T>::of(x, j);
-          lds.steps[first + i] = (u64)(ask.weight(x, r.top) * steps + 0.5);
+    if (held) {
+      for (int i = tid; i < listed; i += NT) {
+        int lo = 0, n = A.nslices;  // the last slice with first <= i
+        while (n > 1) {
+          const int half = n >> 1;
+          const bool up = lds.first[lo + half] <= i;
+          lo += up ? half : 0;
+          n = up ? n - half : half;
         }
-        first += m;
+        const typename L::Word w = reinterpret_cast<const typename L::Word*>(A.cand)[(at + lo) * S::kSize + (i - lds.first[lo])];
+        lds.rank[i] = Rank<T>::of(L::key(w), from0 + lo * S::kSize + L::place(w));
+        lds.steps[i] = in_steps(Rank<T>::logit(L::key(w)));
+        lds.slice[i] = (uint16_t)lo;
       }
       __syncthreads();
     }
@@ -495,119 +678,137 @@ __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs 
       double total = r.sum, before = 0.0;  // of what top-k leaves, and of what is surely kept
       if (ask.has_k) {
         u64 t = 0;
-        each([&](u64 k, u64 w) { t += k >= cut ? w : 0; });
-        total = (double)reduce<NT>(t, lds.buf, Add()) / steps;
+        each([&](u64 k, u64 w, int) { t += k >= cut ? w : 0; });
+        t = wave_reduce(t, (u64)0, Add());
+        if (lane == 0) atomicAdd(&lds.total, t);
+        __syncthreads();
+        total = (double)lds.total / steps;
       } else {
-        double b = 0.0;
-        for (int s = tid; s < A.nslices; s += NT) b += A.kept[at + s].all;
-        before = reduce<NT>(b, reinterpret_cast<double*>(lds.buf), Add());
+        for (int s = lane; s < A.nslices; s += 64) before += lds.sums[s];
+        before = wave_reduce(before, 0.0, Add());
       }
-      // (whole steps before a token are fewer than the target's if they are fewer than it rounded up; the first token stays)
-      const double target = ceil((ask.p * total - before) * steps);
+      // (whole steps before a token are fewer than the target's if they are fewer than it rounded up; the first token stays.  Sums that are equal, as among
+      // equal logits, must not be told apart by their rounding: a little less than the target)
+      const double target = ceil((ask.p * total * (1.0 - kRounding) - before) * steps);
       if (listed > 0) cut = max(cut, select(target >= 1.0 ? (u64)target : 1ull, cut, [](u64 w) { return w; }));
     }
-  }
-  // ---------------------------------------------------------------- the slice that the random number falls into
-  const float un = A.uniform[row];
-  const double u = (opaque_bits(un) & 0x7fffffffu) > 0x7f800000u ? 0.0 : fmin(fmax((double)un, 0.0), 1.0);
-  const int wave = tid >> 6, lane = tid & 63;
-  // w of slice s that is left; all lanes of a wave together
-  auto slice_sum = [&](int s) {
-    if (!sums) return A.stat[at + s].sum * ask.weight(A.stat[at + s].top, r.top);
-    double sum = A.kept[at + s].sum;
-    if (cuts) {
-      u64 t = 0;
-      S sl;
-      sl.init(A, row, s);
-      const int n = A.kept[at + s].listed;
-      const uint16_t* cand = A.cand + (at + s) * S::kSize;
-      for (int i = lane; i < n; i += 64) {
-        const int j = sl.from + cand[i];
-        const float x = sl.at(j);
-        const double w = ask.weight(x, r.top);
-        if (Rank<T>::of(x, j) >= cut && w >= ask.f) t += (u64)(w * steps + 0.5);
+    if (held) {  // (a slice's tokens follow one another: a wave sums them up)
+      for (int s = tid >> 6; s < A.nslices; s += kSampleWaves) {
+        u64 t = 0;
+        for (int i = lds.first[s] + lane; i < lds.first[s + 1]; i += 64) t += left_of(lds.rank[i], lds.steps[i]);
+        t = wave_reduce(t, (u64)0, Add());
+        if (lane == 0) lds.kept[s] = t;
       }
-#pragma unroll
-      for (int off = 32; off >= 1; off >>= 1) t += __shfl_xor(t, off);
-      sum += (double)t / steps;
+    } else {
+      each([&](u64 k, u64 w, int s) {
+        const u64 t = left_of(k, w);
+        if (t) atomicAdd(&lds.kept[s], t);
+      });
     }
-    return sum;
-  };
-  __shared__ double slice_sums[kSampleMostVocab / kSampleLargeSlice + 1];
-  __shared__ int chosen, first, found;
+    __syncthreads();
+  }
+  // ---------------------------------------------------------------- the slice that the random number falls into (the first wave)
+  __shared__ int chosen;
   __shared__ double left;  // of the random number's share in the chosen slice
   __shared__ double all;
-  for (int s = wave; s < A.nslices; s += NT / 64) {
-    const double x = slice_sum(s);
-    if (lane == 0) slice_sums[s] = x;
-  }
-  __syncthreads();
-  if (tid == 0) {
+  if (tid < 64) {
+    const float un = A.uniform[row];
+    const double u = (opaque_bits(un) & 0x7fffffffu) > 0x7f800000u ? 0.0 : fmin(fmax((double)un, 0.0), 1.0);
     double total = 0.0;
-    for (int s = 0; s < A.nslices; ++s) total += slice_sums[s];
-    const double want = u * total;
-    double sum = 0.0;
-    int pick = -1;
-    for (int s = 0; s < A.nslices; ++s) {
-      if (slice_sums[s] > 0.0) {
-        pick = s;
-        left = want - sum;
-        if (sum + slice_sums[s] > want) break;
+    for (int s0 = 0; s0 < A.nslices; s0 += 64) {
+      const int s = s0 + lane;
+      double x = 0.0;
+      if (s < A.nslices) {
+        x = sums ? A.kept[at + s].sum : A.stat[at + s].sum * ask.weight(A.stat[at + s].top, r.top);
+        if (cuts) x += (double)lds.kept[s] / steps;
+        lds.sums[s] = x;
       }
-      sum += slice_sums[s];
+      total += wave_reduce(x, 0.0, Add());
     }
-    chosen = pick;
-    all = total;
-    found = -1;
-    first = NT;
+    const double want = u * total * (1.0 + kRounding);
+    double run = 0.0, rest = 0.0;
+    int pick = -1;
+    bool done = false;
+    for (int s0 = 0; s0 < A.nslices && !done; s0 += 64) {  // the first slice up to and with which the sum is more; else the last with something in it
+      const int s = s0 + lane;
+      const double x = s < A.nslices ? lds.sums[s] : 0.0;
+      const double upto = wave_scan(x, 0.0, Add());
+      const double before = run + (upto - x);
+      const u64 over = __ballot(x > 0.0 && run + upto > want), some = __ballot(x > 0.0);
+      const int l = over ? __builtin_ctzll(over) : 63 - __clzll((long long)some);
+      if (over || some) {
+        pick = s0 + l;
+        rest = want - lane_value(before, l);
+      }
+      done = over != 0;
+      run += lane_value(upto, 63);
+    }
+    if (lane == 0) {
+      chosen = pick;
+      left = rest;
+      all = total;
+    }
   }
   __syncthreads();
-  // ---------------------------------------------------------------- the token in it
-  S sl;
-  sl.init(A, row, chosen);
-  const double want = left;
-  double before = 0.0;
-  int last = -1;  // the last token of this thread that is left
-  for (int c = 0; c < NCH; ++c) {
-    float x[S::E];
-    sl.load_chunk(c, x);
+  // ---------------------------------------------------------------- the block in it, and the token
+  if (cuts && held) {
+    for (int i = lds.first[chosen] + tid; i < lds.first[chosen + 1]; i += NT) {
+      const u64 t = left_of(lds.rank[i], lds.steps[i]);
+      const int index = kSampleMostVocab - 1 - (int)(lds.rank[i] & (kSampleMostVocab - 1));
+      if (t) atomicAdd(&lds.block[(index - from0 - chosen * S::kSize) / S::kBlock], t);
+    }
+  } else if (cuts) {
+    const typename L::Word* cand = reinterpret_cast<const typename L::Word*>(A.cand) + (at + chosen) * S::kSize;
+    for (int i = tid; i < lds.first[chosen + 1] - lds.first[chosen]; i += NT) {
+      const float x = Rank<T>::logit(L::key(cand[i]));
+      const u64 t = left_of(Rank<T>::of(L::key(cand[i]), from0 + chosen * S::kSize + L::place(cand[i])), in_steps(x));
+      if (t) atomicAdd(&lds.block[L::place(cand[i]) / S::kBlock], t);
+    }
+  }
+  if (cuts) __syncthreads();
+  if (tid >= 64) return;
+  double want = left, x = 0.0;
+  if (lane < S::kBlocks) {
+    x = A.blocks[(at + chosen) * S::kBlocks + lane] * (sums ? 1.0 : ask.weight(A.stat[at + chosen].top, r.top));
+    if (cuts) x += (double)lds.block[lane] / steps;
+  }
+  {
+    const double upto = wave_scan(x, 0.0, Add());
+    const u64 over = __ballot(x > 0.0 && upto > want), some = __ballot(x > 0.0);
+    const int l = over ? __builtin_ctzll(over) : 63 - __clzll((long long)some);  // (else the sum of the blocks fell just short of the slice's)
+    want -= lane_value(upto - x, l);
+    x = lane_value(x, l);
+    const int i0 = from0 + chosen * S::kSize + l * S::kBlock + lane * S::E;
+    S sl;
+    sl.init(A, row, chosen);
+    float v[S::E];
+    sl.load_chunk(i0, v);
     double w[S::E], sum = 0.0;
 #pragma unroll
     for (int e = 0; e < S::E; ++e) {
-      w[e] = ask.weight(x[e], r.top);
-      if (!(w[e] >= ask.f) || Rank<T>::of(x[e], sl.index(c, e)) < cut) w[e] = 0.0;
-      if (w[e] > 0.0) last = sl.index(c, e);
+      w[e] = ask.weight(v[e], r.top);
+      if (!(w[e] >= ask.f) || Rank<T>::of(v[e], i0 + e) < cut) w[e] = 0.0;
       sum += w[e];
     }
-    double total;
-    double upto = before + scan<NT>(sum, reinterpret_cast<double*>(lds.buf), total);
-    if (sum > 0.0 && upto > want) atomicMin(&first, tid);
-    __syncthreads();
-    if (first < NT) {  // (uniform)
-      if (tid == first) {
-        double t = upto - sum;
-        int pick = -1;
-        bool over = false;
+    const double to = wave_scan(sum, 0.0, Add());
+    const u64 past = __ballot(sum > 0.0 && to > want), any = __ballot(sum > 0.0);
+    const int mine = past ? __builtin_ctzll(past) : 63 - __clzll((long long)any);
+    if (lane == mine) {
+      double t = to - sum, drawn = 0.0;
+      int token = -1;
+      bool done = false;
 #pragma unroll
-        for (int e = 0; e < S::E; ++e) {
-          t += w[e];
-          if (w[e] > 0.0 && !over) {
-            pick = sl.index(c, e);
-            over = t > want;
-          }
+      for (int e = 0; e < S::E; ++e) {
+        t += w[e];
+        if (w[e] > 0.0 && !done) {
+          token = i0 + e;
+          drawn = w[e];
+          done = t > want;
         }
-        found = pick;
       }
-      break;
+      A.token[row] = token;
+      if (A.logprob) A.logprob[row] = (float)log(drawn / all);
     }
-    before += total;
-  }
-  __syncthreads();
-  int token = found;
-  if (token < 0) token = reduce<NT>(last, reinterpret_cast<int*>(lds.buf), Most());  // (a sum that rounding left just short)
-  if (tid == 0) {
-    A.token[row] = token;
-    if (A.logprob) A.logprob[row] = token < 0 ? -kInf : (float)log(ask.weight(sl.at(token), r.top) / all);
   }
 }
 
@@ -662,12 +863,15 @@ int entmax_sample(const entmax_sample_params* p, const void* logits, const float
   a.logprob = logprob;
   a.rows = p->rows;
   a.vocab = p->vocab;
-  a.nslices = L.nslices;
+  // (rows that begin at round addresses need no room for slices that do not)
+  const bool round = (reinterpret_cast<uintptr_t>(logits) & 15u) == 0 && (p->rows == 1 || p->stride * (int64_t)es % 16 == 0);
+  a.nslices = round ? ceil_div(p->vocab, L.slice) : L.nslices;
   a.stride = p->stride;
   a.stat = reinterpret_cast<SliceStat*>(ws + L.off_stat);
   a.hist = reinterpret_cast<float*>(ws + L.off_hist);
   a.kept = reinterpret_cast<SliceKept*>(ws + L.off_kept);
-  a.cand = reinterpret_cast<uint16_t*>(ws + L.off_cand);
+  a.blocks = reinterpret_cast<double*>(ws + L.off_blocks);
+  a.cand = ws + L.off_cand;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   const bool small = L.slice == kSampleSmallSlice;
   bool ok;

@@ -8,13 +8,16 @@ constexpr int kSampleMostVocab = 1 << 22;   // (an index has 22 bits of a token'
 constexpr int kSampleBins = 256;
 // Logits of a workgroup: a row is cut into slices of so many (the first one may begin up to 16 bytes in front of the row, where addresses are round)
 constexpr int kSampleSmallSlice = 8192, kSampleLargeSlice = 16384;
-inline int sample_slice(int rows, int vocab) { return (long long)rows * vocab <= (1 << 20) ? kSampleSmallSlice : kSampleLargeSlice; }
+// small ones where large ones would not give most of the chip's 512 places for workgroups something to do
+inline int sample_slice(int rows, int vocab) {
+  return (long long)rows * ceil_div(vocab, kSampleLargeSlice) < 384 && vocab <= kSampleMostVocab / 2 ? kSampleSmallSlice : kSampleLargeSlice;
+}
 
-constexpr int kSampleStatBytes = 24;  // what the kernels leave of a slice, twice
+constexpr int kSampleStatBytes = 16, kSampleKeptBytes = 24;  // what the kernels leave of a slice
 
 struct SampleLayout {
   int slice, nslices;
-  size_t off_stat, off_hist, off_kept, off_cand, total;
+  size_t off_stat, off_hist, off_kept, off_blocks, off_cand, total;
 };
 inline SampleLayout make_sample_layout(const entmax_sample_params* p) {
   SampleLayout L{};
@@ -27,9 +30,11 @@ inline SampleLayout make_sample_layout(const entmax_sample_params* p) {
   L.off_hist = o;
   o += align_up(n * kSampleBins * sizeof(float));
   L.off_kept = o;
-  o += align_up(n * kSampleStatBytes);
+  o += align_up(n * kSampleKeptBytes);
+  L.off_blocks = o;
+  o += align_up(n * 64 * sizeof(double));  // (64 blocks at most)
   L.off_cand = o;
-  o += align_up(n * L.slice * sizeof(uint16_t));
+  o += align_up(n * L.slice * (p->dtype == ENTMAX_ATTN_BF16 ? 4 : 8));  // (listed tokens: all of them at worst)
   L.total = o < kAlign ? kAlign : o;
   return L;
 }
