@@ -6,7 +6,9 @@
 //                         goes through 32-key tiles of its own, brought to LDS by loads that it alone waits for; the waves meet at the end.
 //                         Bound by the one read of K and V.
 //   softmax_join_kernel   adds up the pieces' outputs, each in units of its own largest score
-//   softmax_tiled_kernel  others: a workgroup per 128 folded rows, tiles of keys and values shared by its waves
+//   softmax_tiled_kernel  others: a workgroup per 128 folded rows and piece of the keys, tiles of keys and values shared by its waves; bound by the matrix
+//                         products, of which the one with V is made twice in bf16
+//   softmax_tiled_join_kernel  adds up such pieces
 #pragma once
 #include "launch.hip.h"
 #include "seq.hip.h"
@@ -41,17 +43,20 @@ struct SoftmaxArgs {
   int piece, splits;
   int nblk;
   int split;      // sequences with few rows are left to softmax_split_kernel
+  float* tpart;   // softmax_tiled_kernel: [nblk][Hkv][tsplits][128][D], [..][128], as part and sums
+  float2* tsums;
+  int tpiece, tsplits;  // keys of a workgroup (a multiple of 64) and the most pieces of a group
 };
 
 // How a sequence's keys are cut up: n equal pieces of `len` keys, whole tiles of 32 (one piece of none if there are no keys).  Piece k of key/value head hk has place
 // (first + k) Hkv + hk.
 struct SoftmaxShare {
   int first, n, len;
-  __device__ __forceinline__ void cut(int keys, int most_tiles) {
+  __device__ __forceinline__ void cut(int keys, int most_tiles, int step = 1) {  // (pieces of whole steps of tiles)
     const int tiles = (keys + 31) >> 5;
     n = max(1, (tiles + most_tiles - 1) / most_tiles);
-    const int each = (tiles + n - 1) / n;
-    if (each > 0) n = (tiles + each - 1) / each;
+    const int each = ((tiles + n - 1) / n + step - 1) / step * step;
+    if (each > 0) n = max(1, (tiles + each - 1) / each);
     len = each * 32;
   }
 };
@@ -120,11 +125,12 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // From accumulators of the dot products to scores in units of log 2: score = unit * x, x the accumulator or, with a cap, what capped() makes of it.
 template <typename T, bool CAP>
 struct SoftmaxScale {
-  float unit;
+  float unit, slack;      // slack: x of a factor of 2^24
   float cap2, in2, late;  // CAP: cap in units of log 2; s / cap = in2 * accumulator; slope of a bias outside the cap
   // a, w: as in SeqRow; w is zero afterwards if the bias is added late
   __device__ __forceinline__ void init_scale(const SoftmaxArgs& A, float a, float& w) {
     unit = CAP ? 1.f : a * kLog2e;
+    slack = fminf(24.f / unit, 1e30f);
     if (CAP) {
       cap2 = A.cap * kLog2e;
       in2 = a / A.cap;
@@ -149,13 +155,39 @@ struct SoftmaxScale {
   }
 };
 
+// An address that is the same in all lanes, as one
+__device__ __forceinline__ const char* uniform(const char* at) {
+  const unsigned long long x = (unsigned long long)at;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (const char*)((unsigned long long)hi << 32 | lo);
+}
+
+// Eight numbers as sums of two bf16 ones each, in pairs
+__device__ __forceinline__ void split_pairs(const float* x, Frag<bf16_t>& hi, Frag<bf16_t>& lo) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{x[2 * e], x[2 * e + 1]}), bf16x2_t));
+    const f32x2_t rest = {x[2 * e] - __uint_as_float(h << 16), x[2 * e + 1] - __uint_as_float(h & 0xffff0000u)};
+    hi.v[e] = h;
+    lo.v[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2_t));
+  }
+}
+
+// The larger of x in this lane and in the one 32 lanes away
+__device__ __forceinline__ float other_half_max(float x) {
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+
 // A wave's 32 rows, a lane pair each, and what they have seen so far.
 template <typename T, int D, bool CAP>
 struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
   static constexpr int kRows = 32, NC = D / 16, NM = D / 32;
   static constexpr int kChunks = NM * 4;  // a lane's parts of the output, four features each
   static constexpr int kProbs = 16;       // a lane's probabilities of 32 keys
-  float top, sum;    // largest x; sum of this lane's exp2(unit (x - top))
+  float top, sum;    // x that none of the scores so far is above; sum of this lane's exp2(unit (x - top))
   f32x16_t oacc[NM];
   __device__ __forceinline__ void init(const SoftmaxArgs& A, const SeqView& v, int hk, int r0) {
     SeqRows<T, D>::init(A.g, v, A.Q, hk, r0);
@@ -197,34 +229,50 @@ struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = this->capped(acc[e], this->pos - j0 - this->key_of(e));
   }
-  // Takes in blocks of 32 keys with scores x = acc (masked ones -inf): p receives exp2(score - largest so far)
+  // Moves `top` to 2^24 times the largest score if some score x = acc (masked ones -inf) is above it.  No probability is above 1 then, so nothing overflows
+  // that the formula does not, the largest is 2^-24 at least, so none that counts is lost at 2^-126, and the sums are rarely scaled anew.
   template <int NB>
-  __device__ __forceinline__ void step(const f32x16_t (&acc)[NB], float (&p)[NB][16]) {
-    float m = max16(acc[0]);
-#pragma unroll
-    for (int b = 1; b < NB; ++b) m = fmaxf(m, max16(acc[b]));
-    m = fmaxf(m, __shfl_xor(m, 32));
+  __device__ __forceinline__ void raise(const f32x16_t (&acc)[NB]) {
+    const float m = other_half_max(most(acc));
     const bool more = m > top;
     if (__ballot(more) != 0ull) {
-      const float f = more ? __builtin_amdgcn_exp2f((top - m) * this->unit) : 1.f;  // (0 from -inf)
-      top = more ? m : top;
+      const float to = m + this->slack, f = more ? __builtin_amdgcn_exp2f((top - to) * this->unit) : 1.f;  // (0 from -inf)
+      top = more ? to : top;
       sum *= f;
 #pragma unroll
       for (int mm = 0; mm < NM; ++mm)
 #pragma unroll
         for (int e = 0; e < 16; ++e) oacc[mm][e] *= f;
     }
+  }
+  // whether raise() would
+  template <int NB>
+  __device__ __forceinline__ bool rises(const f32x16_t (&acc)[NB]) const {
+    return __ballot(most(acc) > top) != 0ull;
+  }
+  template <int NB>
+  static __device__ __forceinline__ float most(const f32x16_t (&acc)[NB]) {
+    float m = max16(acc[0]);
+#pragma unroll
+    for (int b = 1; b < NB; ++b) m = fmaxf(m, max16(acc[b]));
+    return m;
+  }
+  // p = exp2(score - top) of eight of a block's scores, added to the sum
+  __device__ __forceinline__ void probs8(const f32x16_t& acc, int from, float* p) {
     const float base = top > -kInf ? -top * this->unit : 0.f;
+    float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p[b][e] = __builtin_amdgcn_exp2f(fmaf(acc[b][e], this->unit, base));
-        s += p[b][e];
-      }
-      sum += s;
+    for (int e = 0; e < 8; e += 2) {
+      p[e] = __builtin_amdgcn_exp2f(fmaf(acc[from + e], this->unit, base));
+      p[e + 1] = __builtin_amdgcn_exp2f(fmaf(acc[from + e + 1], this->unit, base));
+      s0 += p[e];
+      s1 += p[e + 1];
     }
+    sum += s0 + s1;
+  }
+  __device__ __forceinline__ void probs(const f32x16_t& acc, float (&p)[16]) {
+    probs8(acc, 0, p);
+    probs8(acc, 8, p + 8);
   }
   __device__ __forceinline__ float top2() const { return top > -kInf ? top * this->unit : -kInf; }
 
@@ -247,7 +295,8 @@ struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
     if constexpr (CAP) cap_scores(acc[0], j0);
     const bool masked = hole || j0 + 32 > this->lim_min;
     if (masked) this->mask(acc[0], j0, keys, hole);
-    step<1>(acc, reinterpret_cast<float(&)[1][16]>(p));
+    raise<1>(acc);
+    probs(acc[0], p);
     return masked;
   }
   __device__ __forceinline__ void take_values(const Places& at, const char* tile, const float (&p)[kProbs], bool masked) {
@@ -364,12 +413,11 @@ struct SoftmaxRows16 : SeqRow, SoftmaxScale<T, CAP> {
     float m = x[0];
 #pragma unroll
     for (int e = 1; e < kProbs; ++e) m = fmaxf(m, x[e]);
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const bool more = m > top;
+    m = other_half_max(fmaxf(m, __shfl_xor(m, 16)));
+    const bool more = m > top;  // (as SoftmaxRows::raise)
     if (__ballot(more) != 0ull) {
-      const float f = more ? __builtin_amdgcn_exp2f((top - m) * this->unit) : 1.f;  // (0 from -inf)
-      top = more ? m : top;
+      const float to = m + this->slack, f = more ? __builtin_amdgcn_exp2f((top - to) * this->unit) : 1.f;
+      top = more ? to : top;
       sum *= f;
 #pragma unroll
       for (int c4 = 0; c4 < kChunks; ++c4)
@@ -412,7 +460,7 @@ struct SoftmaxRows16 : SeqRow, SoftmaxScale<T, CAP> {
     if constexpr (sizeof(T) == 2) {
       // (probabilities as the sum of two bf16 numbers: rounded to one, they would cost up to 2^-9 |v| of the output)
       Frag<T> hi, lo;
-      Elem<T>::pack_split(p, hi, lo);
+      split_pairs(p, hi, lo);
 #pragma unroll
       for (int f = 0; f < kChunks; ++f) {
         const uint2 x = read_transposed(tile + at.v[f]), y = read_transposed(tile + at.v[f] + 16 * VTile::kRowBytes);
@@ -609,58 +657,98 @@ __global__ __launch_bounds__((SoftmaxSplitCfg<T, D>::NW * 64), (NQB == 1 && (siz
   }
 }
 
-// A row's pieces are shared out among `slices` groups of D / 4 threads, each thread with four features; what they have found meets in LDS.
+// Adds up the pieces of a row: piece k's output at part + k step D, its (largest score, sum) at sums[k step].  `slices` groups of D / 4 threads share them, each
+// thread with four features; what they have found meets in LDS.  f: this thread's first feature; slice 0's threads end with the row's output and lse.
+template <int D>
+struct SoftmaxJoin {
+  static constexpr int LR = D / 4;
+  f32x4_t outs[kThreads];
+  float2 found[kThreads / LR];
+  __device__ __forceinline__ float add_up(const float* part, const float2* sums, int pieces, long long step, int slice, int slices, int f, f32x4_t& o) {
+    const int tid = threadIdx.x, group = tid / LR;
+    float most = -kInf, l = 0.f;
+    o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = slice; k < pieces; k += slices) most = fmaxf(most, sums[k * step].x);
+#pragma unroll 8
+    for (int k = slice; k < pieces; k += slices) {
+      const float2 x = sums[k * step];
+      const f32x4_t y = *reinterpret_cast<const f32x4_t*>(part + k * step * D + f);
+      const float w = x.y > 0.f ? __builtin_amdgcn_exp2f(x.x - most) : 0.f;
+      l = fmaf(x.y, w, l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
+    }
+    if (slices > 1) {
+      outs[tid] = o;
+      if (f == 0) found[group] = make_float2(most, l);
+      __syncthreads();
+      if (slice != 0) return 0.f;
+      for (int k = 0; k < slices; ++k) most = fmaxf(most, found[group + k].x);
+      l = 0.f;
+      o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < slices; ++k) {
+        const float2 x = found[group + k];
+        const float w = x.y > 0.f ? __builtin_amdgcn_exp2f(x.x - most) : 0.f;
+        l = fmaf(x.y, w, l);
+        const f32x4_t y = outs[tid + k * LR];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
+      }
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= inv;
+    return l > 0.f ? (most + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
+  }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void store_joined(const SoftmaxArgs& A, const SeqView& v, int hk, int row, int f, const f32x4_t& o, float lse) {
+  const SeqGeom& g = A.g;
+  const int t = row / g.G, qh = hk * g.G + row - t * g.G;
+  T* dst = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + t) * g.o_st + (long long)qh * g.o_sh + f;
+  store4<T>(dst, o[0], o[1], o[2], o[3]);
+  if (f == 0 && A.lse) A.lse[(long long)qh * g.T + v.row0 + t] = lse;
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void softmax_join_kernel(SoftmaxArgs A, int slices) {
-  constexpr int LR = D / 4;
-  __shared__ f32x4_t outs[kThreads];
-  __shared__ float2 found[kThreads / LR];
+  using Join = SoftmaxJoin<D>;
+  __shared__ Join join;
   const SeqGeom& g = A.g;
-  const int tid = threadIdx.x, group = tid / LR, slice = group % slices, f = (tid % LR) * 4, per_wg = kThreads / (LR * slices);
+  const int tid = threadIdx.x, group = tid / Join::LR, slice = group % slices, f = (tid % Join::LR) * 4, per_wg = kThreads / (Join::LR * slices);
   const int per = (A.rows + per_wg - 1) / per_wg, s = blockIdx.x / per, hk = blockIdx.y;
   const int row = (int)(blockIdx.x % per) * per_wg + group / slices;
   SeqView v;
   SoftmaxShare sh;
   if (!softmax_share<false>(A, s, v, sh) || sh.n <= 1) return;  // (the same for the workgroup)
-  const int pieces = sh.n;
   const bool mine = row < v.n * g.G;
-  const long long at = ((long long)sh.first * g.Hkv + hk) * A.rows + (mine ? row : 0), step = (long long)g.Hkv * A.rows;
-  float most = -kInf, l = 0.f;
-#pragma unroll 4
-  for (int k = slice; k < pieces; k += slices) most = fmaxf(most, A.sums[at + k * step].x);
-  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int k = slice; k < pieces; k += slices) {
-    const float2 x = A.sums[at + k * step];
-    const f32x4_t y = *reinterpret_cast<const f32x4_t*>(A.part + (at + k * step) * D + f);
-    const float w = x.y > 0.f ? __builtin_amdgcn_exp2f(x.x - most) : 0.f;
-    l = fmaf(x.y, w, l);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
-  }
-  if (slices > 1) {
-    outs[tid] = o;
-    if (f == 0) found[group] = make_float2(most, l);
-    __syncthreads();
-    if (slice != 0) return;
-    for (int k = 0; k < slices; ++k) most = fmaxf(most, found[group + k].x);
-    l = 0.f;
-    o = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < slices; ++k) {
-      const float2 x = found[group + k];
-      const float w = x.y > 0.f ? __builtin_amdgcn_exp2f(x.x - most) : 0.f;
-      l = fmaf(x.y, w, l);
-      const f32x4_t y = outs[tid + k * LR];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
-    }
-  }
-  if (!mine) return;
-  const int t = row / g.G, qh = hk * g.G + row - t * g.G;
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  T* dst = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + t) * g.o_st + (long long)qh * g.o_sh + f;
-  store4<T>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-  if (f == 0 && A.lse) A.lse[(long long)qh * g.T + v.row0 + t] = l > 0.f ? (most + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
+  const long long at = ((long long)sh.first * g.Hkv + hk) * A.rows + (mine ? row : 0);
+  f32x4_t o;
+  const float lse = join.add_up(A.part + at * D, A.sums + at, sh.n, (long long)g.Hkv * A.rows, slice, slices, f, o);
+  if (mine && slice == 0) store_joined<T, D>(A, v, hk, row, f, o, lse);
+}
+
+// The same for the groups of softmax_tiled_kernel; a workgroup for kThreads / (D / 4) rows.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void softmax_tiled_join_kernel(SoftmaxArgs A) {
+  using Join = SoftmaxJoin<D>;
+  __shared__ Join join;
+  constexpr int RW = kThreads / Join::LR, PER = kBlockRows / RW;
+  const SeqGeom& g = A.g;
+  const int hk = blockIdx.x % g.Hkv, part = (int)blockIdx.x / g.Hkv % PER, blk = (int)blockIdx.x / g.Hkv / PER, f = ((int)threadIdx.x % Join::LR) * 4;
+  SeqView v;
+  int blk0;
+  if (!seq_block(g, blk, A.split != 0, v, blk0)) return;
+  const int local = part * RW + (int)threadIdx.x / Join::LR, row = blk0 + local, last_row = min(v.n * g.G, blk0 + kBlockRows) - 1;
+  SoftmaxShare sh;
+  sh.cut(g.causal ? max(0, min(v.L - v.n + last_row / g.G + 1, v.L)) : v.L, A.tpiece >> 5, 2);
+  if (sh.n <= 1 || row > last_row) return;
+  const long long at = ((long long)blk * g.Hkv + hk) * A.tsplits * kBlockRows + local;
+  f32x4_t o;
+  const float lse = join.add_up(A.tpart + at * D, A.tsums + at, sh.n, kBlockRows, 0, 1, f, o);
+  store_joined<T, D>(A, v, hk, row, f, o, lse);
 }
 
 template <typename T, int D>
@@ -672,6 +760,10 @@ struct SoftmaxTiledCfg {
   static constexpr int NB = sizeof(T) == 2 ? 2 : 1;  // blocks of 32 keys that a wave takes in together
 };
 
+// The two waves of a SIMD hide each other's exponentials and LDS reads behind their products; what counts is how much else a tile costs.  bf16, 16 x 512 tokens
+// against 2048 keys, 4 x 4 heads of 128: 308 us (447 TFLOP/s) with the address of every load from its page and limit and a rescaling of the sums inside the loop (32 register
+// pairs copied a tile), 263 without, 200 with a `top` that is left for good after a few tiles.  4096 tokens against themselves, 16 heads: 139 us (990 TFLOP/s, all pairs
+// counted).
 template <typename T, int D, bool CAP>
 __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) void softmax_tiled_kernel(SoftmaxArgs A) {
   using Cfg = SoftmaxTiledCfg<T, D>;
@@ -682,8 +774,8 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const SeqGeom& g = A.g;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  // (heads and groups in the order of the entmax attention's tiled kernel)
-  const int hk = blockIdx.x % g.Hkv, blk = A.nblk - 1 - (int)blockIdx.x / g.Hkv;
+  // (heads and groups in the order of the entmax attention's tiled kernel; a group's pieces next to each other)
+  const int hk = blockIdx.x % g.Hkv, piece = (int)blockIdx.x / g.Hkv % A.tsplits, blk = A.nblk - 1 - (int)blockIdx.x / g.Hkv / A.tsplits;
   SeqView v;
   int blk0;
   if (!seq_block(g, blk, A.split != 0, v, blk0)) return;
@@ -694,7 +786,10 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
   q.init(A, v, hk, blk0 + wave * 32);
   const int last_row = min(v.n * g.G, blk0 + kBlockRows) - 1;
   const int block_lim = g.causal ? max(0, min(v.L - v.n + last_row / g.G + 1, v.L)) : v.L;
-  const int ntiles = __builtin_amdgcn_readfirstlane((block_lim + KT - 1) / KT);
+  SoftmaxShare sh;
+  sh.cut(block_lim, A.tpiece >> 5, 2);  // (tiles of 64 keys in all pieces, also where this kernel's are of 32)
+  if (piece >= sh.n) return;
+  const int key0 = piece * sh.len, ntiles = __builtin_amdgcn_readfirstlane((min(block_lim - key0, sh.len) + KT - 1) / KT);
   const bool holes = seq_has_holes(keys, block_lim);
   const int lane = q.lane;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
@@ -703,15 +798,46 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
   for (int cc = 0; cc < NC; ++cc) koff[cc] = FragOff<T>::template make<typename KTile::Tile>(q.li, 2 * cc + q.hh);
   Vals vv;
   vv.init(lane);
-  typename KTile::Pages pk;
-  typename VTile::Pages pv;
+  // bf16: the first `plain` tiles have no key that some row of the workgroup does not see (limits do not decrease from row to row) and nothing else that has
+  // to be looked at
+  bool whole = NB == 2 && !holes && keys.sp >> 32 == 0 && vals.sp >> 32 == 0 && (keys.sn << g.lps) >> 31 == 0 && (vals.sn << g.lps) >> 31 == 0;
+  whole = __builtin_amdgcn_readfirstlane(whole ? 1 : 0) != 0;
+  int plain = 0;
+  if constexpr (NB == 2) {
+    const int first_lim = g.causal ? max(0, min(v.L - v.n + blk0 / g.G + 1, v.L)) : v.L;
+    if (__builtin_amdgcn_readfirstlane(__syncthreads_or(q.biased ? 1 : 0)) == 0 && whole) plain = max(0, min(ntiles, (first_lim - key0) / KT));
+    plain = __builtin_amdgcn_readfirstlane(plain);
+  }
+  // Tiles on their way, their pages asked for one tile ahead (the same for keys and values).  `whole`, and no row behind the last: 32-bit offsets, the same of a
+  // lane in all its loads (the swizzle has the period of a load's rows), and nothing to clamp.
+  static_assert(VTile::L == KTile::L && VTile::RS == KTile::RS && VTile::RW == KTile::RW && (NB == 1 || KTile::RS % 16 == 0), "loads of the same rows");
+  typename KTile::Pages pages;
   auto ask = [&](int t) {
-    pk.ask(keys, t * KT, v.L, wave);
-    pv.ask(vals, t * KT, v.L, wave);
+    pages.ask(keys, key0 + t * KT, v.L, wave);
+#pragma unroll
+    for (int it = 0; it < KTile::L; ++it) pages.pg[it] = __builtin_amdgcn_readfirstlane(pages.pg[it]);
   };
+  const int load_row = wave * KTile::RW + lane / KTile::kCpr;
+  const uint32_t klane = (uint32_t)(lane / KTile::kCpr) * (uint32_t)keys.sn + (uint32_t)(((lane % KTile::kCpr) ^ KTile::swz(load_row)) << 4);
+  const uint32_t vlane = (uint32_t)(lane / VTile::kCpr) * (uint32_t)vals.sn + (uint32_t)(((lane % VTile::kCpr) ^ VTile::swz(load_row)) << 4);
   auto issue = [&](int t, int buf) {
-    KTile::load(keys, pk, t * KT, v.L, lds0 + (uint32_t)(2 * buf) * TB, wave, lane);
-    VTile::load(vals, pv, t * KT, v.L, lds0 + (uint32_t)(2 * buf + 1) * TB, wave, lane);
+    const uint32_t kdst = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(2 * buf) * TB), vdst = kdst + TB;
+    if (NB == 2 && whole && key0 + (t + 1) * KT <= v.L) {
+      const uint32_t mask = (1u << g.lps) - 1u;
+#pragma unroll
+      for (int it = 0; it < KTile::L; ++it) {
+        const uint32_t at = (uint32_t)(key0 + t * KT + it * KTile::RS + wave * KTile::RW) & mask, dst = (uint32_t)((it * kThreads + wave * 64) * 16);
+        const uint32_t pg = (uint32_t)pages.pg[it];
+        load_to_lds(uniform(keys.base + ((unsigned long long)pg * (uint32_t)keys.sp + at * (uint32_t)keys.sn)), klane, kdst + dst);
+        load_to_lds(uniform(vals.base + ((unsigned long long)pg * (uint32_t)vals.sp + at * (uint32_t)vals.sn)), vlane, vdst + dst);
+      }
+    } else {
+      typename VTile::Pages same;
+#pragma unroll
+      for (int it = 0; it < KTile::L; ++it) same.pg[it] = pages.pg[it];
+      KTile::load(keys, pages, key0 + t * KT, v.L, kdst, wave, lane);
+      VTile::load(vals, same, key0 + t * KT, v.L, vdst, wave, lane);
+    }
   };
   if (ntiles > 0) {
     ask(0);
@@ -720,39 +846,90 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
   if (ntiles > 1) ask(1);
   lds_loads_wait<0>();
   __syncthreads();
-  for (int t = 0; t < ntiles; ++t) {
-    const int cur = t & 1;
-    if (t + 1 < ntiles) {
-      issue(t + 1, cur ^ 1);
+  // Every wave meets the others once a tile, in the first loop or in what follows it.
+  int t = 0;
+  while (t < ntiles) {
+    bool ahead = false;  // of the loads of the next tile
+    if constexpr (NB == 2) {
+      // as long as no row's largest score goes up by much: nothing here rescales the sums, so they stay in their registers
+#pragma unroll 1
+      for (; t < plain; ++t) {
+        if (t + 1 < ntiles) {
+          issue(t + 1, (t + 1) & 1);
+          if (t + 2 < ntiles) ask(t + 2);
+        }
+        const char* tile = smem + (t & 1) * 2 * TB;
+        f32x16_t acc[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[b] = f32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int cc = 0; cc < NC; ++cc)  // (two sums in turn: neither waits for its last product)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) acc[b] = Elem<T>::mma(koff[cc].load(tile, b * 32 * KTile::kRowBytes), q.qf[cc], acc[b]);
+        Frag<T> vf[2][NM];
+        auto fetch = [&](int u) {  // values of the 16 keys 16 u .. of the tile
+#pragma unroll
+          for (int mm = 0; mm < NM; ++mm) vf[u & 1][mm] = vv.frag(tile + TB, u >> 1, u & 1, mm);
+        };
+        fetch(0);
+        if constexpr (CAP) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) q.cap_scores(acc[b], key0 + t * KT + 32 * b);
+        }
+        if (q.template rises<2>(acc)) {
+          ahead = true;
+          break;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (u + 1 < 4) fetch(u + 1);
+          float p[8];
+          q.probs8(acc[u >> 1], 8 * (u & 1), p);
+          // the probabilities as the sum of two bf16 numbers: rounded to one, they would cost up to 2^-9 |v| of the output (and save a seventh of the time)
+          Frag<T> hi, lo;
+          split_pairs(p, hi, lo);
+#pragma unroll
+          for (int mm = 0; mm < NM; ++mm) q.oacc[mm] = Elem<T>::mma(vf[u & 1][mm], hi, q.oacc[mm]);
+#pragma unroll
+          for (int mm = 0; mm < NM; ++mm) q.oacc[mm] = Elem<T>::mma(vf[u & 1][mm], lo, q.oacc[mm]);
+        }
+        lds_loads_wait<0>();
+        __syncthreads();
+      }
+      if (t >= ntiles) break;
+    }
+    if (!ahead && t + 1 < ntiles) {
+      issue(t + 1, (t + 1) & 1);
       if (t + 2 < ntiles) ask(t + 2);
     }
-    const char* tile = smem + cur * 2 * TB;
+    const char* tile = smem + (t & 1) * 2 * TB;
 #pragma unroll 1
-    for (int sb0 = 0; sb0 < KT / 32; sb0 += NB) {
-      const int j0 = t * KT + sb0 * 32;
+    for (int sb = 0; sb < KT / 32; ++sb) {
+      const int j0 = key0 + t * KT + sb * 32;
       if (j0 >= q.lim_max) break;
-      f32x16_t acc[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const char* at = tile + (sb0 + b) * 32 * KTile::kRowBytes;
-        acc[b] = q.scores(q.start(j0 + 32 * b), [&](int cc) { return koff[cc].load(at, 0); });
-      }
-      const bool masked = holes || j0 + 32 * NB > q.lim_min;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        if constexpr (CAP) q.cap_scores(acc[b], j0 + 32 * b);
-        if (masked) q.mask(acc[b], j0 + 32 * b, keys, holes);
-      }
-      float p[NB][16];
-      q.template step<NB>(acc, p);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) vv.accumulate(tile + TB, sb0 + b, p[b], masked, q.oacc);
+      const char* at = tile + sb * 32 * KTile::kRowBytes;
+      f32x16_t acc[1] = {q.scores(q.start(j0), [&](int cc) { return koff[cc].load(at, 0); })};
+      if constexpr (CAP) q.cap_scores(acc[0], j0);
+      const bool masked = holes || j0 + 32 > q.lim_min;
+      if (masked) q.mask(acc[0], j0, keys, holes);
+      q.template raise<1>(acc);
+      float p[16];
+      q.probs(acc[0], p);
+      vv.accumulate(tile + TB, sb, p, masked, q.oacc);
     }
     lds_loads_wait<0>();
     __syncthreads();
+    ++t;
   }
-  const float l = q.sum + __shfl_xor(q.sum, 32);
+  const float l = q.total();
   if (!q.valid) return;
+  if (sh.n > 1) {
+    const long long at = (((long long)blk * g.Hkv + hk) * A.tsplits + piece) * kBlockRows + wave * 32 + q.li;
+#pragma unroll
+    for (int u = 0; u < q.kChunks; ++u) *reinterpret_cast<f32x4_t*>(A.tpart + at * D + q.feature(u)) = q.out(u);
+    if (q.hh == 0) A.tsums[at] = make_float2(q.top2(), l);
+    return;
+  }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   T* o = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + q.t) * g.o_st + (long long)q.head * g.o_sh;
 #pragma unroll
@@ -786,8 +963,13 @@ bool launch_softmax(const SoftmaxArgs& a, const SoftmaxLayout& L, hipStream_t st
     using Cfg = SoftmaxTiledCfg<T, D>;
     constexpr auto kern = softmax_tiled_kernel<T, D, CAP>;
     if (!ensure_dynamic_lds<kern>(Cfg::kLdsBytes)) return false;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(a.nblk * a.g.Hkv)), dim3(kThreads), Cfg::kLdsBytes, st, a);
+    const unsigned groups = (unsigned)(a.nblk * a.g.Hkv);
+    hipLaunchKernelGGL(kern, dim3(groups * (unsigned)a.tsplits), dim3(kThreads), Cfg::kLdsBytes, st, a);
     if (!launch_ok()) return false;
+    if (a.tsplits > 1) {
+      hipLaunchKernelGGL((softmax_tiled_join_kernel<T, D>), dim3(groups * (unsigned)(kBlockRows * D / 4 / kThreads)), dim3(kThreads), 0, st, a);
+      if (!launch_ok()) return false;
+    }
   }
   if (!L.split) return true;
   // (two blocks of fp32 rows of 128 features do not fit the registers)
@@ -832,6 +1014,10 @@ int run_softmax(const SoftmaxCall& c) {
   a.splits = L.splits;
   a.nblk = (int)seq_blocks(p->nseq, p->T, a.g.G);
   a.split = L.split ? 1 : 0;
+  a.tpart = reinterpret_cast<float*>(c.ws + L.off_tpart);
+  a.tsums = reinterpret_cast<float2*>(c.ws + L.off_tsums);
+  a.tpiece = L.tpiece;
+  a.tsplits = L.tsplits;
   const bool ok = c.cap > 0.f ? launch_softmax<T, D, true>(a, L, c.st) : launch_softmax<T, D, false>(a, L, c.st);
   return ok ? ENTMAX_ATTN_OK : ENTMAX_ATTN_LAUNCH_FAILED;
 }

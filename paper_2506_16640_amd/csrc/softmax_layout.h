@@ -24,6 +24,12 @@ constexpr int kSoftmaxLeastTiles = 4;
 // With at most so many sequences their lengths decide how the keys are cut up (every wave looks at all of them), else the bound of the lengths
 constexpr int kSoftmaxSharedSeqs = 512;
 
+// softmax_tiled_kernel: a group of 128 rows is cut up along its keys where there are fewer groups than workgroups on the chip: into pieces of at least so many
+// keys, until there are so many workgroups.  4 x 700 tokens against 3159 to 9130 keys, 4 x 4 heads of 128 (352 groups): 250 us, 309 whole, 269 with three times as
+// many pieces.  100 tokens against 12000 keys (16 groups): 51 us, 305 whole, 58 with 8 pieces of a group at most; against 1000 keys 29 us, 42 with pieces of
+// 512 keys, 27 with pieces of 128, which cost 2 x 200 tokens against 2000 keys 49 us for 44.
+constexpr int kSoftmaxTiledWorkgroups = 768, kSoftmaxMostTiledPieces = 32, kSoftmaxLeastTiledKeys = 256;
+
 struct SoftmaxLayout {
   bool split;   // the call may hold sequences of at most kSplitRows folded rows
   bool blocks;  // it may hold others
@@ -33,7 +39,8 @@ struct SoftmaxLayout {
   int piece, splits;   // keys of a piece, pieces of a sequence, where they are not shared
   int most_pieces;     // of a sequence
   long long places;    // workgroups
-  size_t off_part, off_sums, total;
+  int tpiece, tsplits; // softmax_tiled_kernel: most keys of a piece, pieces of a group
+  size_t off_part, off_sums, off_tpart, off_tsums, total;
 };
 
 inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
@@ -62,6 +69,22 @@ inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
       L.off_part = o;
       o += align_up(n * p->D * sizeof(float));
       L.off_sums = o;
+      o += align_up(n * 2 * sizeof(float));
+    }
+  }
+  L.tsplits = 1;
+  L.tpiece = 1 << 22;
+  if (L.blocks) {
+    const long long groups = seq_blocks(p->nseq, p->T, G) * p->Hkv;
+    while (groups < kSoftmaxSlots && L.tsplits < kSoftmaxMostTiledPieces && groups * L.tsplits < kSoftmaxTiledWorkgroups &&
+           p->max_keys >= kSoftmaxLeastTiledKeys * (L.tsplits + 1))
+      ++L.tsplits;
+    if (L.tsplits > 1) {
+      L.tpiece = ceil_div(ceil_div(p->max_keys, L.tsplits), 64) * 64;
+      const size_t n = (size_t)groups * L.tsplits * kBlockRows;
+      L.off_tpart = o;
+      o += align_up(n * p->D * sizeof(float));
+      L.off_tsums = o;
       o += align_up(n * 2 * sizeof(float));
     }
   }
