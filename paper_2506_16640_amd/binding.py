@@ -461,10 +461,12 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def _array(name, t, ref, dtype, want):
-    """A contiguous tensor of one dimension of `want` elements on ref's device."""
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != want or not t.is_contiguous() or t.get_device() != ref.get_device():
-        raise ValueError("%s must be a contiguous %s tensor of %d elements on the device of the others" % (name, str(dtype)[6:], want))
+def _arrays(ref, dtype, *named):
+    """named: (name, tensor or None, elements) of contiguous tensors of one dimension on ref's device."""
+    device = ref.get_device()
+    for name, t, want in named:
+        if t is not None and (t.dtype is not dtype or t.dim() != 1 or t.numel() != want or not t.is_contiguous() or t.get_device() != device):
+            raise ValueError("%s must be a contiguous %s tensor of %d elements on the device of the others" % (name, str(dtype)[6:], want))
 
 
 class _DeviceOf:
@@ -690,28 +692,23 @@ def cache_plan(new_len, kv_len, page_table, free_pages, free_count, page_size, p
     get its pages (or whose tokens do not fit the plan's rows) gets no rows; those behind the last sequence have -1 everywhere."""
     nseq, max_pages = _page_table(page_table, new_len)
     i32 = torch.int32
-    for name, t, want in (("new_len", new_len, nseq), ("kv_len", kv_len, nseq), ("release", release, nseq), ("free_count", free_count, 1),
-                          ("plan.cu_seqlens", plan.cu_seqlens, nseq + 1), ("plan.kv_len", plan.kv_len, nseq), ("plan.free_count", plan.free_count, 1)):
-        if t is not None:
-            _array(name, t, new_len, i32, want)
-        elif name != "release":
-            raise ValueError("%s is missing" % name)
-    _array("free_pages", free_pages, new_len, i32, free_pages.shape[0] if free_pages.dim() else -1)
-    rows = None
-    for name, t, dtype in (("plan.slots", plan.slots, torch.int64), ("plan.positions", plan.positions, i32), ("plan.sequences", plan.sequences, i32)):
-        if t is not None:
-            rows = t.shape[0] if rows is None and t.dim() else rows
-            _array(name, t, new_len, dtype, rows)
+    cu_seqlens, slots, positions, sequences = plan.cu_seqlens, plan.slots, plan.positions, plan.sequences
+    rows = slots if slots is not None else positions if positions is not None else sequences
     if rows is None:
         raise ValueError("the plan needs slots, positions or sequences: their length is the number of rows")
+    rows = rows.numel()
+    _arrays(new_len, i32, ("new_len", new_len, nseq), ("kv_len", kv_len, nseq), ("release", release, nseq), ("free_count", free_count, 1),
+            ("free_pages", free_pages, free_pages.numel()), ("plan.cu_seqlens", cu_seqlens, nseq + 1), ("plan.kv_len", plan.kv_len, nseq),
+            ("plan.free_count", plan.free_count, 1), ("plan.positions", positions, rows), ("plan.sequences", sequences, rows))
+    _arrays(new_len, torch.int64, ("plan.slots", slots, rows))
     w = plan.workspace
     if w.dtype != torch.uint8 or not w.is_contiguous() or w.get_device() != new_len.get_device():
         raise ValueError("plan.workspace must be a contiguous uint8 tensor on the device of the others")
-    p = _plan_bytes.pack(nseq, rows, page_size, free_pages.shape[0], max_pages)
+    p = _plan_bytes.pack(nseq, rows, page_size, free_pages.numel(), max_pages)
     with _DeviceOf(new_len) as stream:
         rc = _lib.entmax_cache_plan(p, new_len.data_ptr(), _at(release), kv_len.data_ptr(), free_count.data_ptr(), page_table.data_ptr(),
-                                    free_pages.data_ptr(), plan.kv_len.data_ptr(), plan.free_count.data_ptr(), plan.cu_seqlens.data_ptr(),
-                                    _at(plan.slots), _at(plan.positions), _at(plan.sequences), w.data_ptr(), w.numel(), stream)
+                                    free_pages.data_ptr(), plan.kv_len.data_ptr(), plan.free_count.data_ptr(), cu_seqlens.data_ptr(),
+                                    _at(slots), _at(positions), _at(sequences), w.data_ptr(), w.numel(), stream)
     if rc != 0:
         raise EntmaxAttnError(rc)
     return plan
@@ -786,10 +783,9 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     draw (all -infinity or NaN)."""
     rows, p = _sample_params(logits)
     f32, i32 = torch.float32, torch.int32
-    for name, t, dtype in (("uniform", uniform, f32), ("temperature", temperature, f32), ("top_k", top_k, i32), ("top_p", top_p, f32),
-                           ("min_p", min_p, f32), ("token", token, i32), ("logprob", logprob, f32)):
-        if t is not None:
-            _array(name, t, logits, dtype, rows)
+    _arrays(logits, f32, ("uniform", uniform, rows), ("temperature", temperature, rows), ("top_p", top_p, rows), ("min_p", min_p, rows),
+            ("logprob", logprob, rows))
+    _arrays(logits, i32, ("top_k", top_k, rows), ("token", token, rows))
     with _DeviceOf(logits) as stream:
         if token is None:
             token = torch.empty(rows, dtype=i32, device=logits.device)
