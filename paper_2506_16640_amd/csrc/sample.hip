@@ -2,7 +2,7 @@
 // largest and w = exp((x - m) / temperature), every filter keeps the first tokens of the row's falling order (x, then lower index first), so that
 // what is left is "rank >= cut" for a cut that is found without sorting the row:
 //   sample_slices_kernel   a workgroup per slice of a row: its largest logit, its sum of w, and, for rows with top-k or top-p, how many tokens
-//                          (top-k) or how much w (top-p) lie in each of 256 bins of equal width below its largest.  Bins lie on one
+//                          (top-k) or how much w (top-p) lie in each of 512 bins of equal width below its largest.  Bins lie on one
 //                          grid of logits, so that those of a row's slices can be added up.
 //   sample_bracket_kernel  the row's bins, and with them the bin in which the filter's cut must lie: tokens above it are surely kept and only their w
 //                          is summed, tokens below are dropped, those of the bin are listed
@@ -70,9 +70,10 @@ struct RowAsk {
     p = has_p ? fmax((double)pp, 0.0) : 1.0;
     has_m = !nan(mm) && mm > 0.f;
     f = has_m ? fmin((double)mm, 1.0) : 0.0;
-    // top-p: bins of 1/24 of the temperature: 256 of them reach down to 2e-5 of the largest w, and the bin of the cut holds a few per cent of the
-    // tokens of a flat row at most.  top-k: 1/12 of it, but not less than 1/12 of a logit, for low temperatures.
-    grid = greedy ? 0.f : (float)fmin(has_k ? fmin(12.0 * inv, 12.0) : 24.0 * inv, 1e30);
+    // top-p: bins of 1/32 of the temperature.  512 of them reach down to 1e-7 of the largest w, below which lies nothing that counts (256 of 1/24 of it reached down
+    // to 2e-5, and where the cut of 131072 tokens, a few of which stood out, was in none of them, all were listed and the call took 500 us for 50), and the bin
+    // of the cut holds a few per cent of the tokens of a flat row at most.  top-k: 1/12 of it, but not less than 1/12 of a logit, for low temperatures.
+    grid = greedy ? 0.f : (float)fmin(has_k ? fmin(12.0 * inv, 12.0) : 32.0 * inv, 1e30);
   }
   // 2^t, t <= 0, to 4e-14 of it and 1 for 0: the whole part goes to the exponent; the rest f, at most 1/2, through 1 + f p(f), p interpolating (2^f - 1) / f at the
   // nine zeros of a Chebyshev polynomial.  (-infinity: undefined)
@@ -302,7 +303,8 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bracket_kernel(Sampl
   using S = Slice<T, NCH>;
   using L = Listed<T>;
   __shared__ double sums[2][S::kBlocks];
-  __shared__ double bins[4][kSampleBins], factor[kSampleMostSlices];
+  constexpr int kParts = NT / kSampleBins;  // threads to a bin
+  __shared__ double bins[kParts][kSampleBins], factor[kSampleMostSlices];
   __shared__ int shift[kSampleMostSlices], listed;
   const int row = blockIdx.x / A.nslices, slice = blockIdx.x - row * A.nslices, tid = threadIdx.x, lane = tid & 63;
   RowAsk ask;
@@ -335,13 +337,13 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bracket_kernel(Sampl
   __syncthreads();
   const RowStat r = stat;
   if (binned) {
-    // the row's bins: four threads to each add it up over a quarter of the slices; what lies in no bin is in the last
+    // the row's bins: two threads to each add it up over half of the slices; what lies in no bin is in the last
     const float* hist = A.hist + (long long)row * A.nslices * kSampleBins;
-    static_assert(NT == 4 * kSampleBins, "a quarter each");
+    static_assert(NT == 2 * kSampleBins, "half of the slices each");
     const int bin = tid & (kSampleBins - 1);
     double mine = 0.0;
 #pragma unroll 4
-    for (int s = tid / kSampleBins; s < A.nslices; s += 4) {
+    for (int s = tid / kSampleBins; s < A.nslices; s += kParts) {
       const int b = bin - shift[s];
       if (b >= 0 && bin < kSampleBins - 1) mine += (double)hist[s * kSampleBins + b] * factor[s];
     }
@@ -351,22 +353,23 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bracket_kernel(Sampl
   if (tid < 64) {
     int b0 = kSampleBins, b1 = -1;
     if (binned) {
-      // where the sum reaches what is to be kept, four bins a lane.  Sums of w: a little less and a little more of it, for the rounding of the bins
+      // where the sum reaches what is to be kept, eight bins a lane.  Sums of w: a little less and a little more of it, for the rounding of the bins
       const double least = ask.has_k ? (double)ask.k : ask.p * r.sum * (1.0 - 1e-5), most = ask.has_k ? (double)ask.k : ask.p * r.sum * (1.0 + 1e-5);
-      double v[4], upto = 0.0;
+      constexpr int PL = kSampleBins / 64;
+      double v[PL], upto = 0.0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int b = 4 * lane + j;
-        v[j] = (bins[0][b] + bins[1][b]) + (bins[2][b] + bins[3][b]);
+      for (int j = 0; j < PL; ++j) {
+        const int b = PL * lane + j;
+        v[j] = bins[0][b] + bins[1][b];
         upto += v[j];
       }
       const double mine = upto;
       upto = wave_scan(upto, 0.0, Add()) - mine;
       int n0 = 0, n1 = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < PL; ++j) {
         upto += v[j];
-        const bool in = 4 * lane + j < kSampleBins - 1;
+        const bool in = PL * lane + j < kSampleBins - 1;
         n0 += (int)__popcll(__ballot(in && upto < least));
         n1 += (int)__popcll(__ballot(in && upto < most));
       }
@@ -431,11 +434,12 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bracket_kernel(Sampl
   }
 }
 
+constexpr int kPickBins = 256;     // of a round of the selection
 constexpr int kPickList = 7680;    // listed tokens that stay in LDS; longer lists are looked up again for every pass
 
 struct PickLds {
   u64 buf[kSampleWaves];
-  u64 bins[2][kSampleBins];        // in use, and cleared meanwhile: these four
+  u64 bins[2][kPickBins];        // in use, and cleared meanwhile: these four
   uint32_t least_key[2], most_key[2];
   int few[2];
   ulonglong2 few_of[64];           // (rank, amount)
@@ -480,7 +484,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs 
       lds.most_key[tid] = 0;
       lds.few[tid] = 0;
     }
-    for (int b = tid; b < 2 * kSampleBins; b += NT) (&lds.bins[0][0])[b] = 0;
+    for (int b = tid; b < 2 * kPickBins; b += NT) (&lds.bins[0][0])[b] = 0;
     if (tid == 0) lds.first[0] = 0, lds.total = 0;
   }
   __shared__ RowStat stat;
@@ -574,7 +578,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs 
         each([&](u64 k, u64 w, int) {
           if (k >= lo && k <= hi && k >= least) atomicAdd(&lds.bins[turn][(k >> shift) & 255], amount(w));
         });
-        if (tid < kSampleBins) lds.bins[turn ^ 1][tid] = 0;
+        if (tid < kPickBins) lds.bins[turn ^ 1][tid] = 0;
         if (tid == 0) {
           lds.least_key[turn ^ 1] = ~0u;
           lds.most_key[turn ^ 1] = 0;

@@ -5,7 +5,7 @@
 namespace entmax {
 
 constexpr int kSampleMostVocab = 1 << 22;   // (an index has 22 bits of a token's rank)
-constexpr int kSampleBins = 256;
+constexpr int kSampleBins = 512;
 // Logits of a workgroup: a row is cut into slices of so many (the first one may begin up to 16 bytes in front of the row, where addresses are round)
 constexpr int kSampleSmallSlice = 8192, kSampleLargeSlice = 16384;
 // small ones where large ones would not give most of the chip's 512 places for workgroups something to do
