@@ -37,6 +37,7 @@ struct SoftmaxArgs {
   float cap;
   float* part;    // [places][rows][D], a place for every piece: see SoftmaxShare
   float2* sums;   // [places][rows] (largest score in units of log 2, sum)
+  int2* shares;   // (shared) [nseq] first and n of the sequences' SoftmaxShare
   int rows;
   int shared;     // pieces from the lengths of all sequences (else of `piece` keys, `splits` to a sequence)
   int budget;     // shared: tiles are dealt out to about so many workgroups
@@ -61,16 +62,15 @@ struct SoftmaxShare {
   }
 };
 
-// The share of sequence x, or (BY_PLACE) of the sequence that has place x, with what it is; false: there is none.
+// The share of the sequence that has place x, with what it is; false: there is none.
 // Memory delivers as much as it can when all compute units ask for equal parts of it at the same time, and the host knows only a bound of the lengths: so
 // every wave adds up the tiles of all sequences (64 at a time, a lane each), divides them by the number of workgroups that fit the chip, and
 // numbers the pieces that come of it.  (48 sequences of 150 to 9000 keys, 2 heads of 128: 41 us with pieces by the bound, 27 so.)  With many
 // sequences that would take longer than it gives: pieces by the bound.
-template <bool BY_PLACE>
 __device__ __forceinline__ bool softmax_share(const SoftmaxArgs& A, int x, SeqView& v, SoftmaxShare& sh) {
   const SeqGeom& g = A.g;
   if (!A.shared) {
-    const int s = BY_PLACE ? x / A.splits : x;
+    const int s = x / A.splits;
     if (s >= g.nseq || !load_seq(g, s, v) || !split_seq(g, v)) return false;
     sh.cut(v.L, A.piece >> 5);
     sh.first = s * A.splits;
@@ -103,7 +103,7 @@ __device__ __forceinline__ bool softmax_share(const SoftmaxArgs& A, int x, SeqVi
       const int y = __shfl_up(upto, off);
       if (lane >= off) upto += y;
     }
-    const unsigned long long here = __ballot(BY_PLACE ? first + upto > x : s0 + lane == x);
+    const unsigned long long here = __ballot(first + upto > x);
     if (here) {
       const int l = __builtin_ctzll(here);
       v.s = s0 + l;
@@ -228,6 +228,10 @@ struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
   __device__ __forceinline__ void cap_scores(f32x16_t& acc, int j0) const {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = this->capped(acc[e], this->pos - j0 - this->key_of(e));
+  }
+  __device__ __forceinline__ void add_bias(f32x16_t& acc, int j0) const {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = fmaf(this->w, (float)max(this->pos - j0 - this->key_of(e), 0), acc[e]);
   }
   // Moves `top` to 2^24 times the largest score if some score x = acc (masked ones -inf) is above it.  No probability is above 1 then, so nothing overflows
   // that the formula does not, the largest is 2^-24 at least, so none that counts is lost at 2^-126, and the sums are rarely scaled anew.
@@ -504,10 +508,9 @@ struct SoftmaxSplitCfg {
   static constexpr size_t kLdsBytes = (size_t)NW * kWaveBytes;
 };
 
-// Rows: SoftmaxRows or SoftmaxRows16; NQB: blocks of them
+// A workgroup's piece: place `place`, of sequence v, cut up as sh says.  Rows: SoftmaxRows or SoftmaxRows16; NQB: blocks of them, from row rbase on
 template <typename T, int D, class Rows, int NQB>
-__global__ __launch_bounds__((SoftmaxSplitCfg<T, D>::NW * 64), (NQB == 1 && (sizeof(T) == 2 || Rows::kRows == 16) ? 2 : 1)) void softmax_split_kernel(
-    SoftmaxArgs A) {
+__device__ __forceinline__ void softmax_split_piece(const SoftmaxArgs& A, int place, int rbase, const SeqView& v, const SoftmaxShare& sh) {
   using Cfg = SoftmaxSplitCfg<T, D>;
   constexpr int NW = Cfg::NW, ST = Cfg::ST, TB = Cfg::kTileBytes, RB = Rows::kRows, CH = Rows::kChunks;
   using KTile = typename Rows::KTile;
@@ -517,15 +520,13 @@ __global__ __launch_bounds__((SoftmaxSplitCfg<T, D>::NW * 64), (NQB == 1 && (siz
   __shared__ float tops[NW][NQB * RB], parts[NW][NQB * RB];
   const SeqGeom& g = A.g;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int hk = blockIdx.x % g.Hkv;
-  SeqView v;
-  SoftmaxShare sh;
-  if (!softmax_share<true>(A, (int)blockIdx.x / g.Hkv, v, sh)) return;
-  const int split = (int)blockIdx.x / g.Hkv - sh.first;
+  const int hk = place % g.Hkv;
+  const int split = place / g.Hkv - sh.first;
   if (split >= sh.n) return;
   const int from = split * sh.len, to = min(v.L, from + sh.len);
-  const int rbase = blockIdx.z * NQB * RB, R = v.n * g.G - rbase;  // first row, rows from there on
+  const int R = v.n * g.G - rbase;  // rows from there on
   if (R <= 0) return;
+  if (A.shared && A.shares && split == 0 && hk == 0 && rbase == 0 && tid == 0) A.shares[v.s] = make_int2(sh.first, sh.n);
   SeqKeys keys, vals;
   keys.init(g, v, A.K, hk, false, sizeof(T));
   vals.init(g, v, A.V, hk, true, sizeof(T));
@@ -642,7 +643,7 @@ __global__ __launch_bounds__((SoftmaxSplitCfg<T, D>::NW * 64), (NQB == 1 && (siz
       if (row >= R) continue;
       const int feature = q[qb].feature(u);
       if (pieces > 1) {
-        *reinterpret_cast<f32x4_t*>(A.part + ((long long)blockIdx.x * A.rows + rbase + row) * D + feature) = o;
+        *reinterpret_cast<f32x4_t*>(A.part + ((long long)place * A.rows + rbase + row) * D + feature) = o;
       } else {
         T* dst = reinterpret_cast<T*>(A.O) + (long long)(v.row0 + q[qb].t) * g.o_st + (long long)q[qb].head * g.o_sh + feature;
         store4<T>(dst, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
@@ -650,11 +651,19 @@ __global__ __launch_bounds__((SoftmaxSplitCfg<T, D>::NW * 64), (NQB == 1 && (siz
     }
     if (wave == 0 && q[qb].first_lane() && row < R) {
       if (pieces > 1)
-        A.sums[(long long)blockIdx.x * A.rows + rbase + row] = make_float2(most, l);
+        A.sums[(long long)place * A.rows + rbase + row] = make_float2(most, l);
       else if (A.lse)
         A.lse[(long long)q[qb].head * g.T + v.row0 + q[qb].t] = l > 0.f ? (most + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
     }
   }
+}
+
+template <typename T, int D, class Rows, int NQB>
+__global__ __launch_bounds__((SoftmaxSplitCfg<T, D>::NW * 64), (NQB == 1 && (sizeof(T) == 2 || Rows::kRows == 16) ? 2 : 1)) void softmax_split_kernel(
+    SoftmaxArgs A) {
+  SeqView v;
+  SoftmaxShare sh;
+  if (softmax_share(A, (int)blockIdx.x / A.g.Hkv, v, sh)) softmax_split_piece<T, D, Rows, NQB>(A, blockIdx.x, blockIdx.z * NQB * Rows::kRows, v, sh);
 }
 
 // Adds up the pieces of a row: piece k's output at part + k step D, its (largest score, sum) at sums[k step].  `slices` groups of D / 4 threads share them, each
@@ -712,43 +721,45 @@ __device__ __forceinline__ void store_joined(const SoftmaxArgs& A, const SeqView
   if (f == 0 && A.lse) A.lse[(long long)qh * g.T + v.row0 + t] = lse;
 }
 
+// Both kinds of pieces: workgroups 0 .. tiled - 1 for those of groups, kThreads / (D / 4) rows each, the others for those of softmax_split_piece()
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void softmax_join_kernel(SoftmaxArgs A, int slices) {
+__global__ __launch_bounds__(kThreads) void softmax_join_kernel(SoftmaxArgs A, int tiled, int slices) {
   using Join = SoftmaxJoin<D>;
   __shared__ Join join;
   const SeqGeom& g = A.g;
-  const int tid = threadIdx.x, group = tid / Join::LR, slice = group % slices, f = (tid % Join::LR) * 4, per_wg = kThreads / (Join::LR * slices);
-  const int per = (A.rows + per_wg - 1) / per_wg, s = blockIdx.x / per, hk = blockIdx.y;
-  const int row = (int)(blockIdx.x % per) * per_wg + group / slices;
+  const int tid = threadIdx.x, group = tid / Join::LR, f = (tid % Join::LR) * 4, hk = blockIdx.x % g.Hkv;
   SeqView v;
   SoftmaxShare sh;
-  if (!softmax_share<false>(A, s, v, sh) || sh.n <= 1) return;  // (the same for the workgroup)
+  f32x4_t o;
+  if ((int)blockIdx.x < tiled) {
+    constexpr int RW = kThreads / Join::LR, PER = kBlockRows / RW;
+    const int x = (int)blockIdx.x / g.Hkv, blk = x / PER;
+    int blk0;
+    if (!seq_block(g, blk, A.split != 0, v, blk0)) return;
+    const int local = x % PER * RW + group, row = blk0 + local, last_row = min(v.n * g.G, blk0 + kBlockRows) - 1;
+    sh.cut(g.causal ? max(0, min(v.L - v.n + last_row / g.G + 1, v.L)) : v.L, A.tpiece >> 5, 2);
+    if (sh.n <= 1 || row > last_row) return;
+    const long long at = ((long long)blk * g.Hkv + hk) * A.tsplits * kBlockRows + local;
+    const float lse = join.add_up(A.tpart + at * D, A.tsums + at, sh.n, kBlockRows, 0, 1, f, o);
+    store_joined<T, D>(A, v, hk, row, f, o, lse);
+    return;
+  }
+  const int x = ((int)blockIdx.x - tiled) / g.Hkv, per_wg = kThreads / (Join::LR * slices), per = (A.rows + per_wg - 1) / per_wg;
+  const int s = x / per, slice = group % slices, row0 = x % per * per_wg, row = row0 + group / slices;
+  if (!load_seq(g, s, v) || !split_seq(g, v) || row0 >= v.n * g.G) return;
+  if (A.shared) {
+    const int2 share = A.shares[s];
+    sh.first = share.x;
+    sh.n = share.y;
+  } else {
+    sh.cut(v.L, A.piece >> 5);
+    sh.first = s * A.splits;
+  }
+  if (sh.n <= 1) return;  // (the same for the workgroup)
   const bool mine = row < v.n * g.G;
   const long long at = ((long long)sh.first * g.Hkv + hk) * A.rows + (mine ? row : 0);
-  f32x4_t o;
   const float lse = join.add_up(A.part + at * D, A.sums + at, sh.n, (long long)g.Hkv * A.rows, slice, slices, f, o);
   if (mine && slice == 0) store_joined<T, D>(A, v, hk, row, f, o, lse);
-}
-
-// The same for the groups of softmax_tiled_kernel; a workgroup for kThreads / (D / 4) rows.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void softmax_tiled_join_kernel(SoftmaxArgs A) {
-  using Join = SoftmaxJoin<D>;
-  __shared__ Join join;
-  constexpr int RW = kThreads / Join::LR, PER = kBlockRows / RW;
-  const SeqGeom& g = A.g;
-  const int hk = blockIdx.x % g.Hkv, part = (int)blockIdx.x / g.Hkv % PER, blk = (int)blockIdx.x / g.Hkv / PER, f = ((int)threadIdx.x % Join::LR) * 4;
-  SeqView v;
-  int blk0;
-  if (!seq_block(g, blk, A.split != 0, v, blk0)) return;
-  const int local = part * RW + (int)threadIdx.x / Join::LR, row = blk0 + local, last_row = min(v.n * g.G, blk0 + kBlockRows) - 1;
-  SoftmaxShare sh;
-  sh.cut(g.causal ? max(0, min(v.L - v.n + last_row / g.G + 1, v.L)) : v.L, A.tpiece >> 5, 2);
-  if (sh.n <= 1 || row > last_row) return;
-  const long long at = ((long long)blk * g.Hkv + hk) * A.tsplits * kBlockRows + local;
-  f32x4_t o;
-  const float lse = join.add_up(A.tpart + at * D, A.tsums + at, sh.n, kBlockRows, 0, 1, f, o);
-  store_joined<T, D>(A, v, hk, row, f, o, lse);
 }
 
 template <typename T, int D>
@@ -765,7 +776,7 @@ struct SoftmaxTiledCfg {
 // pairs copied a tile), 263 without, 200 with a `top` that is left for good after a few tiles.  4096 tokens against themselves, 16 heads: 139 us (990 TFLOP/s, all pairs
 // counted).
 template <typename T, int D, bool CAP>
-__global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) void softmax_tiled_kernel(SoftmaxArgs A) {
+__device__ __forceinline__ void softmax_tiled_piece(const SoftmaxArgs& A, int wg) {
   using Cfg = SoftmaxTiledCfg<T, D>;
   constexpr int KT = Cfg::KT, NB = Cfg::NB, NC = D / 16, NM = D / 32, TB = Cfg::kTileBytes;
   using KTile = SeqTile<T, D, KT, false>;
@@ -775,7 +786,7 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
   const SeqGeom& g = A.g;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   // (heads and groups in the order of the entmax attention's tiled kernel; a group's pieces next to each other)
-  const int hk = blockIdx.x % g.Hkv, piece = (int)blockIdx.x / g.Hkv % A.tsplits, blk = A.nblk - 1 - (int)blockIdx.x / g.Hkv / A.tsplits;
+  const int hk = wg % g.Hkv, piece = wg / g.Hkv % A.tsplits, blk = A.nblk - 1 - wg / g.Hkv / A.tsplits;
   SeqView v;
   int blk0;
   if (!seq_block(g, blk, A.split != 0, v, blk0)) return;
@@ -798,22 +809,23 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
   for (int cc = 0; cc < NC; ++cc) koff[cc] = FragOff<T>::template make<typename KTile::Tile>(q.li, 2 * cc + q.hh);
   Vals vv;
   vv.init(lane);
-  // bf16: the first `plain` tiles have no key that some row of the workgroup does not see (limits do not decrease from row to row) and nothing else that has
-  // to be looked at
+  // bf16: the first `plain` tiles have no key that some row of the workgroup does not see (limits do not decrease from row to row)
   bool whole = NB == 2 && !holes && keys.sp >> 32 == 0 && vals.sp >> 32 == 0 && (keys.sn << g.lps) >> 31 == 0 && (vals.sn << g.lps) >> 31 == 0;
   whole = __builtin_amdgcn_readfirstlane(whole ? 1 : 0) != 0;
   int plain = 0;
   if constexpr (NB == 2) {
     const int first_lim = g.causal ? max(0, min(v.L - v.n + blk0 / g.G + 1, v.L)) : v.L;
-    if (__builtin_amdgcn_readfirstlane(__syncthreads_or(q.biased ? 1 : 0)) == 0 && whole) plain = max(0, min(ntiles, (first_lim - key0) / KT));
-    plain = __builtin_amdgcn_readfirstlane(plain);
+    plain = __builtin_amdgcn_readfirstlane(whole ? max(0, min(ntiles, (first_lim - key0) / KT)) : 0);
   }
   // Tiles on their way, their pages asked for one tile ahead (the same for keys and values).  `whole`, and no row behind the last: 32-bit offsets, the same of a
   // lane in all its loads (the swizzle has the period of a load's rows), and nothing to clamp.
   static_assert(VTile::L == KTile::L && VTile::RS == KTile::RS && VTile::RW == KTile::RW && (NB == 1 || KTile::RS % 16 == 0), "loads of the same rows");
+  // From the last tile to the first: where the bias or the model prefers near keys, the largest scores come first and `top` stays.  (8 biased heads of 16, 5 sequences of
+  // 100 to 187 tokens against 564 to 4930 keys: 69 us from the first, 56 so; without a bias within 3 % of each other.)
+  auto key_of = [&](int t) { return key0 + (ntiles - 1 - t) * KT; };
   typename KTile::Pages pages;
   auto ask = [&](int t) {
-    pages.ask(keys, key0 + t * KT, v.L, wave);
+    pages.ask(keys, key_of(t), v.L, wave);
 #pragma unroll
     for (int it = 0; it < KTile::L; ++it) pages.pg[it] = __builtin_amdgcn_readfirstlane(pages.pg[it]);
   };
@@ -822,11 +834,11 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
   const uint32_t vlane = (uint32_t)(lane / VTile::kCpr) * (uint32_t)vals.sn + (uint32_t)(((lane % VTile::kCpr) ^ VTile::swz(load_row)) << 4);
   auto issue = [&](int t, int buf) {
     const uint32_t kdst = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(2 * buf) * TB), vdst = kdst + TB;
-    if (NB == 2 && whole && key0 + (t + 1) * KT <= v.L) {
+    if (NB == 2 && whole && key_of(t) + KT <= v.L) {
       const uint32_t mask = (1u << g.lps) - 1u;
 #pragma unroll
       for (int it = 0; it < KTile::L; ++it) {
-        const uint32_t at = (uint32_t)(key0 + t * KT + it * KTile::RS + wave * KTile::RW) & mask, dst = (uint32_t)((it * kThreads + wave * 64) * 16);
+        const uint32_t at = (uint32_t)(key_of(t) + it * KTile::RS + wave * KTile::RW) & mask, dst = (uint32_t)((it * kThreads + wave * 64) * 16);
         const uint32_t pg = (uint32_t)pages.pg[it];
         load_to_lds(uniform(keys.base + ((unsigned long long)pg * (uint32_t)keys.sp + at * (uint32_t)keys.sn)), klane, kdst + dst);
         load_to_lds(uniform(vals.base + ((unsigned long long)pg * (uint32_t)vals.sp + at * (uint32_t)vals.sn)), vlane, vdst + dst);
@@ -835,8 +847,8 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
       typename VTile::Pages same;
 #pragma unroll
       for (int it = 0; it < KTile::L; ++it) same.pg[it] = pages.pg[it];
-      KTile::load(keys, pages, key0 + t * KT, v.L, kdst, wave, lane);
-      VTile::load(vals, same, key0 + t * KT, v.L, vdst, wave, lane);
+      KTile::load(keys, pages, key_of(t), v.L, kdst, wave, lane);
+      VTile::load(vals, same, key_of(t), v.L, vdst, wave, lane);
     }
   };
   if (ntiles > 0) {
@@ -853,7 +865,7 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
     if constexpr (NB == 2) {
       // as long as no row's largest score goes up by much: nothing here rescales the sums, so they stay in their registers
 #pragma unroll 1
-      for (; t < plain; ++t) {
+      for (; t >= ntiles - plain && t < ntiles; ++t) {
         if (t + 1 < ntiles) {
           issue(t + 1, (t + 1) & 1);
           if (t + 2 < ntiles) ask(t + 2);
@@ -861,7 +873,8 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
         const char* tile = smem + (t & 1) * 2 * TB;
         f32x16_t acc[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) acc[b] = f32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int b = 0; b < 2; ++b)
+          acc[b] = CAP ? q.start(key_of(t) + 32 * b) : f32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int cc = 0; cc < NC; ++cc)  // (two sums in turn: neither waits for its last product)
 #pragma unroll
@@ -872,9 +885,13 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
           for (int mm = 0; mm < NM; ++mm) vf[u & 1][mm] = vv.frag(tile + TB, u >> 1, u & 1, mm);
         };
         fetch(0);
+        if (!CAP && q.biased) {  // (afterwards: a start for it would be 32 registers to clear in each tile; with a cap they do not count and the code would spill)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) q.add_bias(acc[b], key_of(t) + 32 * b);
+        }
         if constexpr (CAP) {
 #pragma unroll
-          for (int b = 0; b < 2; ++b) q.cap_scores(acc[b], key0 + t * KT + 32 * b);
+          for (int b = 0; b < 2; ++b) q.cap_scores(acc[b], key_of(t) + 32 * b);
         }
         if (q.template rises<2>(acc)) {
           ahead = true;
@@ -905,7 +922,7 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
     const char* tile = smem + (t & 1) * 2 * TB;
 #pragma unroll 1
     for (int sb = 0; sb < KT / 32; ++sb) {
-      const int j0 = key0 + t * KT + sb * 32;
+      const int j0 = key_of(t) + sb * 32;
       if (j0 >= q.lim_max) break;
       const char* at = tile + sb * 32 * KTile::kRowBytes;
       f32x16_t acc[1] = {q.scores(q.start(j0), [&](int cc) { return koff[cc].load(at, 0); })};
@@ -942,6 +959,37 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
 }
 
 // Enqueues the call for checked parameters; returns an entmax_attn_status.
+template <typename T, int D, bool CAP>
+__global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) void softmax_tiled_kernel(SoftmaxArgs A) {
+  softmax_tiled_piece<T, D, CAP>(A, blockIdx.x);
+}
+
+// Prompts and sequences of few rows in one call, at the same time: workgroups 0 .. tiled - 1 for the groups, the others for the pieces.  (bf16, whose two
+// kinds of workgroups are of one size.  18 sequences of one token and one of 20 against up to
+// 4355 keys, 4 x 4 heads of 128, capped and biased: 92 us one after the other, 42 so.)
+template <typename T, int D, bool CAP>
+__global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) void softmax_mixed_kernel(SoftmaxArgs A, int tiled) {
+  static_assert(SoftmaxSplitCfg<T, D>::NW * 64 == kThreads, "one size of workgroups");
+  if ((int)blockIdx.x < tiled) {
+    softmax_tiled_piece<T, D, CAP>(A, blockIdx.x);
+    return;
+  }
+  const int place = (int)blockIdx.x - tiled;
+  SeqView v;
+  SoftmaxShare sh;
+  if (!softmax_share(A, place / A.g.Hkv, v, sh)) return;
+  if (v.n * A.g.G <= 16)
+    softmax_split_piece<T, D, SoftmaxRows16<T, D, CAP>, 1>(A, place, 0, v, sh);
+  else {
+    constexpr int NQB = D == 64 ? 2 : 1;  // (two blocks of 128 features leave no room for a second workgroup on the compute unit)
+#pragma unroll 1
+    for (int rbase = 0; rbase < v.n * A.g.G; rbase += 32 * NQB) {
+      if (rbase) __syncthreads();  // (what the last ones left in LDS has been read)
+      softmax_split_piece<T, D, SoftmaxRows<T, D, CAP>, NQB>(A, place, rbase, v, sh);
+    }
+  }
+}
+
 template <typename T, int D>
 int run_softmax(const SoftmaxCall& c);
 
@@ -959,33 +1007,45 @@ bool launch_softmax_split(const SoftmaxArgs& a, long long places, hipStream_t st
 
 template <typename T, int D, bool CAP>
 bool launch_softmax(const SoftmaxArgs& a, const SoftmaxLayout& L, hipStream_t st) {
+  using Tiled = SoftmaxTiledCfg<T, D>;
+  const unsigned groups = (unsigned)(a.nblk * a.g.Hkv), tiled = L.blocks ? groups * (unsigned)a.tsplits : 0u;
+  bool split = L.split;
   if (L.blocks) {
-    using Cfg = SoftmaxTiledCfg<T, D>;
-    constexpr auto kern = softmax_tiled_kernel<T, D, CAP>;
-    if (!ensure_dynamic_lds<kern>(Cfg::kLdsBytes)) return false;
-    const unsigned groups = (unsigned)(a.nblk * a.g.Hkv);
-    hipLaunchKernelGGL(kern, dim3(groups * (unsigned)a.tsplits), dim3(kThreads), Cfg::kLdsBytes, st, a);
-    if (!launch_ok()) return false;
-    if (a.tsplits > 1) {
-      hipLaunchKernelGGL((softmax_tiled_join_kernel<T, D>), dim3(groups * (unsigned)(kBlockRows * D / 4 / kThreads)), dim3(kThreads), 0, st, a);
+    if constexpr (sizeof(T) == 2) {
+      if (split) {
+        constexpr auto kern = softmax_mixed_kernel<T, D, CAP>;
+        constexpr size_t lds = Tiled::kLdsBytes > SoftmaxSplitCfg<T, D>::kLdsBytes ? Tiled::kLdsBytes : SoftmaxSplitCfg<T, D>::kLdsBytes;
+        if (!ensure_dynamic_lds<kern>(lds)) return false;
+        hipLaunchKernelGGL(kern, dim3(tiled + (unsigned)L.places), dim3(kThreads), lds, st, a, (int)tiled);
+        if (!launch_ok()) return false;
+      }
+    }
+    if (sizeof(T) == 4 || !split) {
+      constexpr auto kern = softmax_tiled_kernel<T, D, CAP>;
+      if (!ensure_dynamic_lds<kern>(Tiled::kLdsBytes)) return false;
+      hipLaunchKernelGGL(kern, dim3(tiled), dim3(kThreads), Tiled::kLdsBytes, st, a);
       if (!launch_ok()) return false;
     }
+    if (sizeof(T) == 2) split = false;  // (done)
   }
-  if (!L.split) return true;
-  // (two blocks of fp32 rows of 128 features do not fit the registers)
-  constexpr int kMostBlocks = sizeof(T) == 4 && D == 128 ? 1 : 2;
-  const bool ok = a.rows <= 16   ? launch_softmax_split<T, D, SoftmaxRows16<T, D, CAP>, 1>(a, L.places, st)
-                  : a.rows <= 32 ? launch_softmax_split<T, D, SoftmaxRows<T, D, CAP>, 1>(a, L.places, st)
-                                 : launch_softmax_split<T, D, SoftmaxRows<T, D, CAP>, kMostBlocks>(a, L.places, st);
-  if (!ok) return false;
-  if (L.most_pieces > 1) {
-    int slices = 1;  // (a power of two: two pieces or more to each)
+  if (split) {
+    // (two blocks of fp32 rows of 128 features do not fit the registers)
+    constexpr int kMostBlocks = sizeof(T) == 4 && D == 128 ? 1 : 2;
+    const bool ok = a.rows <= 16   ? launch_softmax_split<T, D, SoftmaxRows16<T, D, CAP>, 1>(a, L.places, st)
+                    : a.rows <= 32 ? launch_softmax_split<T, D, SoftmaxRows<T, D, CAP>, 1>(a, L.places, st)
+                                   : launch_softmax_split<T, D, SoftmaxRows<T, D, CAP>, kMostBlocks>(a, L.places, st);
+    if (!ok) return false;
+  }
+  const unsigned of_groups = L.blocks && a.tsplits > 1 ? groups * (unsigned)(kBlockRows * D / 4 / kThreads) : 0u;
+  unsigned of_pieces = 0;
+  int slices = 1;  // (a power of two: two pieces or more to each)
+  if (L.split && L.most_pieces > 1) {
     while (2 * slices <= kThreads / (D / 4) && 4 * slices <= L.most_pieces) slices *= 2;
-    const int per = ceil_div(a.rows, kThreads / (D / 4) / slices);
-    hipLaunchKernelGGL((softmax_join_kernel<T, D>), dim3((unsigned)(a.g.nseq * per), (unsigned)a.g.Hkv), dim3(kThreads), 0, st, a, slices);
-    return launch_ok();
+    of_pieces = (unsigned)(a.g.nseq * a.g.Hkv) * (unsigned)ceil_div(a.rows, kThreads / (D / 4) / slices);
   }
-  return true;
+  if (of_groups + of_pieces == 0) return true;
+  hipLaunchKernelGGL((softmax_join_kernel<T, D>), dim3(of_groups + of_pieces), dim3(kThreads), 0, st, a, (int)of_groups, slices);
+  return launch_ok();
 }
 
 }  // namespace
@@ -1007,6 +1067,7 @@ int run_softmax(const SoftmaxCall& c) {
   a.cap = c.cap;
   a.part = reinterpret_cast<float*>(c.ws + L.off_part);
   a.sums = reinterpret_cast<float2*>(c.ws + L.off_sums);
+  a.shares = L.most_pieces > 1 ? reinterpret_cast<int2*>(c.ws + L.off_shares) : nullptr;
   a.rows = L.rows;
   a.shared = L.shared ? 1 : 0;
   a.budget = L.budget;

@@ -40,7 +40,7 @@ struct SoftmaxLayout {
   int most_pieces;     // of a sequence
   long long places;    // workgroups
   int tpiece, tsplits; // softmax_tiled_kernel: most keys of a piece, pieces of a group
-  size_t off_part, off_sums, off_tpart, off_tsums, total;
+  size_t off_part, off_sums, off_shares, off_tpart, off_tsums, total;
 };
 
 inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
@@ -70,6 +70,8 @@ inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
       o += align_up(n * p->D * sizeof(float));
       L.off_sums = o;
       o += align_up(n * 2 * sizeof(float));
+      L.off_shares = o;
+      if (L.shared) o += align_up((size_t)p->nseq * 2 * sizeof(int));
     }
   }
   L.tsplits = 1;

@@ -99,7 +99,8 @@ static int softmax(long& accepted) {
     if (L.most_pieces > 1) {
       const size_t n = (size_t)L.places * L.rows;
       MUST(L.off_part == 0 && L.off_sums % kAlign == 0 && L.off_sums >= n * p.D * 4);
-      end = L.off_sums + n * 8;
+      MUST(L.off_shares % kAlign == 0 && L.off_shares >= L.off_sums + n * 8);
+      end = L.off_shares + (L.shared ? (size_t)p.nseq * 8 : 0);
       MUST(end <= L.total);
     }
   }
