@@ -24,11 +24,12 @@ constexpr int kSoftmaxLeastTiles = 4;
 // With at most so many sequences their lengths decide how the keys are cut up (every wave looks at all of them), else the bound of the lengths
 constexpr int kSoftmaxSharedSeqs = 512;
 
-// softmax_tiled_kernel: a group of 128 rows is cut up along its keys where there are fewer groups than workgroups on the chip: into pieces of at least so many
-// keys, until there are so many workgroups.  4 x 700 tokens against 3159 to 9130 keys, 4 x 4 heads of 128 (352 groups): 250 us, 309 whole, 269 with three times as
-// many pieces.  100 tokens against 12000 keys (16 groups): 51 us, 305 whole, 58 with 8 pieces of a group at most; against 1000 keys 29 us, 42 with pieces of
-// 512 keys, 27 with pieces of 128, which cost 2 x 200 tokens against 2000 keys 49 us for 44.
-constexpr int kSoftmaxTiledWorkgroups = 768, kSoftmaxMostTiledPieces = 32, kSoftmaxLeastTiledKeys = 256;
+// softmax_tiled_piece(): a group of 128 rows is cut up along its keys where there are fewer groups than workgroups on the chip: into pieces of at least so many
+// keys (bf16, fp32), until there are so many workgroups.  4 x 700 tokens against 3159 to 9130 keys, 4 x 4 heads of 128 (352 groups): 250 us, 309 whole, 269 with
+// three times as many pieces.  100 tokens against 12000 keys (16 groups): 51 us, 305 whole, 58 with 8 pieces of a group at most; against 1000 keys 29 us, 42 with
+// pieces of 512 keys, 27 with pieces of 128, which cost 2 x 200 tokens against 2000 keys 49 us for 44.  fp32, where a tile takes four times as long: 411 tokens of 4 x 2
+// heads of 64 against themselves 26 us, 50 with pieces of 256 keys, 31 with pieces of 128; 20 x 60 tokens against 1000 keys 93 us, 84, 95.
+constexpr int kSoftmaxTiledWorkgroups = 768, kSoftmaxMostTiledPieces = 32, kSoftmaxLeastTiledKeys[2] = {256, 64};
 
 struct SoftmaxLayout {
   bool split;   // the call may hold sequences of at most kSplitRows folded rows
@@ -79,7 +80,7 @@ inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
   if (L.blocks) {
     const long long groups = seq_blocks(p->nseq, p->T, G) * p->Hkv;
     while (groups < kSoftmaxSlots && L.tsplits < kSoftmaxMostTiledPieces && groups * L.tsplits < kSoftmaxTiledWorkgroups &&
-           p->max_keys >= kSoftmaxLeastTiledKeys * (L.tsplits + 1))
+           p->max_keys >= kSoftmaxLeastTiledKeys[p->dtype == ENTMAX_ATTN_FP32] * (L.tsplits + 1))
       ++L.tsplits;
     if (L.tsplits > 1) {
       L.tpiece = ceil_div(ceil_div(p->max_keys, L.tsplits), 64) * 64;
