@@ -450,11 +450,12 @@ struct SoftmaxRows16 : SeqRow, SoftmaxScale<T, CAP> {
   // oacc += V^T P^T; as in SeqValues::accumulate() where some row does not see some key
   __device__ __forceinline__ void take_values(const Places& at, const char* tile, const float (&p)[kProbs], bool masked) {
     if (masked) {
-      bool bad = false;
-#pragma unroll 1
-      for (int e = 0; e < 32 * D / 64; ++e) {
-        const float x = value(tile, (64 * e + lane) / D, (64 * e + lane) % D);
-        bad = bad || (opaque_bits(x) & 0x7f800000u) == 0x7f800000u;
+      bool bad = false;  // (of the tile's bytes as they lie there; one value after the other took 4 us)
+#pragma unroll
+      for (int e = 0; e < VTile::kBytes / 1024; ++e) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(tile + 1024 * e + 16 * lane);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bad = bad || (x[k] & 0x7f800000u) == 0x7f800000u || (sizeof(T) == 2 && (x[k] & 0x7f80u) == 0x7f80u);
       }
       if (__ballot(bad) != 0ull) {
         one_by_one(tile, p);
