@@ -40,7 +40,7 @@ struct SoftmaxArgs {
   int2* shares;   // (shared) [nseq] first and n of the sequences' SoftmaxShare
   int rows;
   int shared;     // pieces from the lengths of all sequences (else of `piece` keys, `splits` to a sequence)
-  int budget;     // shared: tiles are dealt out to about so many workgroups
+  int budget, least;  // shared: tiles are dealt out to about so many workgroups, at least so many to each
   int piece, splits;
   int nblk;
   int split;      // sequences with few rows are left to softmax_split_kernel
@@ -90,7 +90,7 @@ __device__ __forceinline__ bool softmax_share(const SoftmaxArgs& A, int x, SeqVi
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) all += __shfl_xor(all, off);
-  const int most = max(kSoftmaxLeastTiles, (int)((all * g.Hkv + A.budget - 1) / A.budget));
+  const int most = max(A.least, (int)((all * g.Hkv + A.budget - 1) / A.budget));
   int first = 0;
   for (int s0 = 0; s0 < g.nseq; s0 += 64) {
     if (s0) tiles = load(s0 + lane, t);
@@ -233,8 +233,8 @@ struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = fmaf(this->w, (float)max(this->pos - j0 - this->key_of(e), 0), acc[e]);
   }
-  // Moves `top` to 2^24 times the largest score if some score x = acc (masked ones -inf) is above it.  No probability is above 1 then, so nothing overflows
-  // that the formula does not, the largest is 2^-24 at least, so none that counts is lost at 2^-126, and the sums are rarely scaled anew.
+  // Moves `top` to 2^24 times the largest score if some score x = acc (masked ones -inf) is above it.  No probability is above 1 then, so that the sums overflow
+  // no sooner than those of exp(s - max) v would; the largest is 2^-24 at least, so that none that counts is lost at 2^-126; and the sums are rarely scaled anew.
   template <int NB>
   __device__ __forceinline__ void raise(const f32x16_t (&acc)[NB]) {
     const float m = other_half_max(most(acc));
@@ -1072,6 +1072,7 @@ int run_softmax(const SoftmaxCall& c) {
   a.rows = L.rows;
   a.shared = L.shared ? 1 : 0;
   a.budget = L.budget;
+  a.least = L.least;
   a.piece = L.piece;
   a.splits = L.splits;
   a.nblk = (int)seq_blocks(p->nseq, p->T, a.g.G);

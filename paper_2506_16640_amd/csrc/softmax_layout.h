@@ -19,10 +19,14 @@ constexpr int kSoftmaxWaves = ES == 4 && D == 128 ? 2 : 4;
 
 // Workgroups of that kernel that are on the chip at a time: two on each compute unit
 constexpr int kSoftmaxSlots = 512;
-// Fewest 32-key tiles of a piece
+// Fewest 32-key tiles of a piece.  (48 sequences of 150 to 300 keys, 2 heads of 128: 20.1 us, 22.4 with 2, 21.7 with 8.)
 constexpr int kSoftmaxLeastTiles = 4;
-// With at most so many sequences their lengths decide how the keys are cut up (every wave looks at all of them), else the bound of the lengths
-constexpr int kSoftmaxSharedSeqs = 512;
+// With so many heads of all sequences, most of which have a workgroup each in any case, only the long ones are cut.  (256
+// sequences of 150 to 2000 keys, 2 heads of 128: 53 us, 70 with the rule for few; to 8000 keys: 132 and 160; to 500 keys: 27, 44 with pieces of 4 tiles.)
+constexpr int kSoftmaxManyHeads = 3 * kSoftmaxSlots / 4, kSoftmaxManyLeastTiles = 16;
+// With at most so many sequences their lengths decide how the keys are cut up (every wave looks at all of them), else the bound of the lengths.  (2 heads of 128, keys
+// 150 to 2000: 100 sequences 29 us and 42, 256 sequences 53 and 64, 512 sequences 113 and 98.)
+constexpr int kSoftmaxSharedSeqs = 384;
 
 // softmax_tiled_piece(): a group of 128 rows is cut up along its keys where there are fewer groups than workgroups on the chip: into pieces of at least so many
 // keys (bf16, fp32), until there are so many workgroups.  4 x 700 tokens against 3159 to 9130 keys, 4 x 4 heads of 128 (352 groups): 250 us, 309 whole, 269 with
@@ -36,7 +40,7 @@ struct SoftmaxLayout {
   bool blocks;  // it may hold others
   int rows;     // rows of a head there is room for
   bool shared;  // see softmax_share()
-  int budget;
+  int budget, least;
   int piece, splits;   // keys of a piece, pieces of a sequence, where they are not shared
   int most_pieces;     // of a sequence
   long long places;    // workgroups
@@ -57,11 +61,13 @@ inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
     L.rows = (int)(most_rows < kSplitRows ? most_rows : kSplitRows);
     L.shared = p->nseq <= kSoftmaxSharedSeqs;
     // (pieces are rounded up, by half a piece a head on average)
-    L.budget = heads < kSoftmaxSlots ? (int)(kSoftmaxSlots - heads / 2) : kSoftmaxSlots / 2;
+    const bool many = heads >= kSoftmaxManyHeads;
+    L.budget = many ? 2 * kSoftmaxSlots : (int)(kSoftmaxSlots - heads / 2);
+    L.least = many ? kSoftmaxManyLeastTiles : kSoftmaxLeastTiles;
     L.piece = kSoftmaxLeastTiles * 32;
     while (L.piece < (1 << 22) && heads * ceil_div(tiles, L.piece / 32) > 2 * kSoftmaxSlots) L.piece *= 2;
     L.splits = ceil_div(tiles, L.piece / 32);
-    L.most_pieces = L.shared ? ceil_div(tiles, kSoftmaxLeastTiles) : L.splits;
+    L.most_pieces = L.shared ? ceil_div(tiles, L.least) : L.splits;
     L.places = heads * L.most_pieces;
     // (shared: the sum of tiles / piece over the heads is at most the budget, and each of them is rounded up)
     if (L.shared && L.places > L.budget + heads) L.places = L.budget + heads;

@@ -38,7 +38,7 @@ static int cut(int keys, int most, int step) {
 static int softmax(long& accepted) {
   entmax_seq_params p;
   memset(&p, 0, sizeof(p));
-  p.nseq = PICK(0, 1, 3, 64, 512, 513, 4000, 1 << 20, -1, 0x7fffffff);
+  p.nseq = PICK(0, 1, 3, 64, 200, 384, 385, 4000, 1 << 20, -1, 0x7fffffff);
   p.T = PICK(0, 1, 5, 4096, 1 << 20, 1 << 26, -3, 0x7fffffff);
   p.Hkv = PICK(1, 1, 2, 4, 8, 0, -2, 4096);
   p.Hq = p.Hkv * PICK(1, 1, 2, 3, 8, 64, 100) + (rnd() % 50 == 0);
@@ -88,7 +88,7 @@ static int softmax(long& accepted) {
         all += keys[s] ? (keys[s] + 31) / 32 : 1;
       }
       const long long share = (all * p.Hkv + L.budget - 1) / L.budget;
-      const int most = (int)(share > kSoftmaxLeastTiles ? share : kSoftmaxLeastTiles);
+      const int most = (int)(share > L.least ? share : L.least);
       for (int s = 0; s < p.nseq; ++s) {
         const int n = cut(keys[s], most, 1);
         MUST(n <= L.most_pieces);

@@ -1,0 +1,56 @@
+"""GPU tests of the softmax attention on batches: many sequences, prompts beside single tokens, prompts whose keys are cut into pieces."""
+import random
+
+import pytest
+
+from tests.serving_util import BF16, FP32, Problem
+from tests.test_gpu_softmax import TYPES, _check, binding  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("nseq", [191, 192, 384, 385])
+@pytest.mark.parametrize("new", [(1, 1), (0, 3)])
+@pytest.mark.parametrize("D,dtype", [(64, BF16), (128, FP32)])
+def test_many_sequences(binding, nseq, new, D, dtype):  # noqa: F811
+    """Lengths of all sequences decide about the pieces, or the bound of the lengths does; most are short, some are long, some empty."""
+    rng = random.Random(nseq)
+    lens = []
+    for s in range(nseq):
+        n = rng.randint(*new)
+        lens.append((n, max(n, rng.choice([0, 1, 31, 32, 33, 90, 90, rng.randint(1, 300), 1500 if s % 60 == 7 else 40]))))
+    _check(binding, Problem(lens, Hq=2, Hkv=2, D=D, dtype=dtype, page=32, seed=70, pad=2), "many")
+
+
+MIXED = [(1, 700), (90, 300), (0, 0), (1, 1), (5, 260), (8, 513), (9, 40), (12, 333), (16, 1000), (17, 1000), (1, 2000), (40, 1800)]
+
+
+@pytest.mark.parametrize("D,dtype", TYPES)
+@pytest.mark.parametrize("cap", [0.0, 4.0])
+@pytest.mark.parametrize("slopes", [False, True])
+def test_prompts_beside_single_tokens(binding, D, dtype, cap, slopes):  # noqa: F811
+    """4 heads to a key/value head: sequences of 4 to 64 rows beside those of more."""
+    _check(binding, Problem(MIXED, Hq=4, Hkv=1, D=D, dtype=dtype, seed=71, pad=1, slopes=slopes), "mixed", cap)
+
+
+@pytest.mark.parametrize("D,dtype", TYPES)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("slopes,bias_mode", [(False, 0), (True, 0), (True, 1)])
+def test_prompts_in_pieces(binding, D, dtype, causal, slopes, bias_mode):  # noqa: F811
+    _check(binding, Problem([(100, 5000), (64, 64), (70, 2601), (33, 1023)], Hq=2, Hkv=1, D=D, dtype=dtype, seed=72, causal=causal, slopes=slopes,
+                            bias_mode=bias_mode, page=64), "pieces")
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_prompts_with_sharp_scores(binding, dtype):  # noqa: F811
+    """Scores of hundreds: a row's largest goes up again and again, and its sums are scaled anew."""
+    _check(binding, Problem([(130, 1400), (1, 1400)], Hq=2, Hkv=1, D=128, dtype=dtype, seed=73, scale="none", q_factor=30.0), "sharp")
+
+
+def test_holes_in_prompts(binding):  # noqa: F811
+    p = Problem([(80, 900), (1, 300), (20, 700)], Hq=4, Hkv=1, D=64, dtype=BF16, seed=74)
+    p.table[0, 3:9] = -1
+    p.table[0, 40] = p.pages
+    p.table[1, 0] = -5
+    p.table[2, 30:] = 1 << 30
+    _check(binding, p, "holes")
