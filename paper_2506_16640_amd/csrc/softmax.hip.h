@@ -802,7 +802,7 @@ __device__ __forceinline__ void softmax_tiled_piece(const SoftmaxArgs& A, int wg
   sh.cut(block_lim, A.tpiece >> 5, 2);  // (tiles of 64 keys in all pieces, also where this kernel's are of 32)
   if (piece >= sh.n) return;
   const int key0 = piece * sh.len, ntiles = __builtin_amdgcn_readfirstlane((min(block_lim - key0, sh.len) + KT - 1) / KT);
-  const bool holes = seq_has_holes(keys, block_lim);
+  const bool holes = seq_has_holes(keys, min(v.L, (block_lim + KT - 1) / KT * KT));  // (whole tiles are loaded, also behind the last key that a row sees)
   const int lane = q.lane;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   FragOff<T> koff[NC];

@@ -4,15 +4,6 @@
 
 namespace entmax {
 
-inline int check_softmax_params(const entmax_seq_params* p) {
-  if (!p || p->alpha != 1.0f || p->path != 0) return ENTMAX_ATTN_INVALID_ARG;
-  entmax_seq_params q = *p;
-  q.alpha = 2.0f;  // (everything else is as in the entmax attention)
-  const int rc = check_seq_params(&q);
-  if (rc != ENTMAX_ATTN_OK) return rc;
-  return p->page_size == 0 ? ENTMAX_ATTN_INVALID_ARG : ENTMAX_ATTN_OK;
-}
-
 // Waves of a workgroup of the kernel that splits the keys (element size, head dimension)
 template <int ES, int D>
 constexpr int kSoftmaxWaves = ES == 4 && D == 128 ? 2 : 4;
@@ -99,6 +90,19 @@ inline SoftmaxLayout make_softmax_layout(const entmax_seq_params* p) {
   }
   L.total = o < kAlign ? kAlign : o;
   return L;
+}
+
+inline int check_softmax_params(const entmax_seq_params* p) {
+  if (!p || p->alpha != 1.0f || p->path != 0) return ENTMAX_ATTN_INVALID_ARG;
+  entmax_seq_params q = *p;
+  q.alpha = 2.0f;  // (everything else is as in the entmax attention)
+  const int rc = check_seq_params(&q);
+  if (rc != ENTMAX_ATTN_OK) return rc;
+  if (p->page_size == 0) return ENTMAX_ATTN_INVALID_ARG;
+  // (one launch for both kinds of sequences: fewer than 2^32 threads together)
+  const SoftmaxLayout L = make_softmax_layout(p);
+  const long long tiled = L.blocks ? seq_blocks(p->nseq, p->T, p->Hq / p->Hkv) * p->Hkv * L.tsplits : 0;
+  return (tiled + (L.split ? L.places : 0)) * kThreads < 1ll << 32 ? ENTMAX_ATTN_OK : ENTMAX_ATTN_UNSUPPORTED_SHAPE;
 }
 
 inline size_t softmax_workspace_bytes_of(const entmax_seq_params* p) {

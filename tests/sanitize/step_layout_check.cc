@@ -104,6 +104,7 @@ static int softmax(long& accepted) {
       MUST(end <= L.total);
     }
   }
+  MUST(((L.blocks ? groups * L.tsplits : 0) + (L.split ? L.places : 0)) * 256 < (1ll << 32));
   MUST(L.tsplits >= 1 && L.tsplits <= kSoftmaxMostTiledPieces && L.tpiece % 64 == 0);
   if (L.blocks) {
     MUST(groups * L.tsplits * 256 < (1ll << 32));

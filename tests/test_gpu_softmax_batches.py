@@ -54,3 +54,13 @@ def test_holes_in_prompts(binding):  # noqa: F811
     p.table[1, 0] = -5
     p.table[2, 30:] = 1 << 30
     _check(binding, p, "holes")
+
+
+@pytest.mark.parametrize("D,dtype", TYPES)
+@pytest.mark.parametrize("what", [-1, -(1 << 31), (1 << 31) - 1])
+def test_holes_behind_the_last_key_of_a_block(binding, D, dtype, what):  # noqa: F811
+    """A tile's pages that no row of its block sees, though later rows would: nothing is read where they point."""
+    p = Problem([(96, 96), (100, 1100)], Hq=4, Hkv=1, D=D, dtype=dtype, seed=75)
+    p.table[0, 2:5] = what  # (32 tokens to a block: its first one sees keys 0 .. 31, in a tile of 64)
+    p.table[1, 65:67] = what
+    _check(binding, p, "holes")
