@@ -5,7 +5,7 @@
 namespace entmax {
 
 // One workgroup does all of a step of at most so many sequences and rows (sequences and what they got stay in LDS); larger ones take two
-// launches, the sequences by one workgroup, the rows by many.
+// launches, the sequences by one workgroup, the rows by many.  (In a graph: 2000 sequences of 2 tokens 10.5 us, 17.7 in two launches; 64 sequences of one, 4.0 and 7.7.)
 constexpr int kPlanOneSeqs = 2048;
 constexpr int kPlanOneRows = 4096;
 constexpr int kPlanRowsPerWorkgroup = 1024;

@@ -10,7 +10,8 @@
 //                          falls into, and the token in it
 // A token is right or wrong, and with 10^5 tokens to a row sums of 32 bits would put one row in a hundred on the neighbour of the right one: w and all sums
 // are of 64 bits.  Sums that atomics make are sums of integers (w in steps of a power of two), the others are formed in a fixed order: the same call gives the same tokens.
-// Bound: one read of the logits, and 64-bit exponentials.
+// Bound: one read of the logits and 64-bit exponentials (256 plain rows of 32768 in fp32: 15.5 us of 21, 7 of them reading); with filters, three dependent
+// launches of round trips (64 rows of 131072: 16 + 22 + 18 us).
 #include "entmax_attn.h"
 
 #include <hip/hip_runtime.h>
@@ -435,7 +436,7 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bracket_kernel(Sampl
 }
 
 constexpr int kPickBins = 256;     // of a round of the selection
-constexpr int kPickList = 7680;    // listed tokens that stay in LDS; longer lists are looked up again for every pass
+constexpr int kPickList = 7680;    // listed tokens that stay in LDS; longer lists are looked up again for every pass (4 rows of 7680 equal logits 72 us, of 9000 102)
 
 struct PickLds {
   u64 buf[kSampleWaves];

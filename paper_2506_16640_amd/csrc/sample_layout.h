@@ -8,7 +8,8 @@ constexpr int kSampleMostVocab = 1 << 22;   // (an index has 22 bits of a token'
 constexpr int kSampleBins = 512;
 // Logits of a workgroup: a row is cut into slices of so many (the first one may begin up to 16 bytes in front of the row, where addresses are round)
 constexpr int kSampleSmallSlice = 8192, kSampleLargeSlice = 16384;
-// small ones where large ones would not give most of the chip's 512 places for workgroups something to do
+// small ones where large ones would not give most of the chip's 512 places for workgroups something to do.  (top-p, rows of 131072: 16 of them 31 us, 38 with large ones;
+// 64 of them 52 with large ones, 57 with small ones.)
 inline int sample_slice(int rows, int vocab) {
   return (long long)rows * ceil_div(vocab, kSampleLargeSlice) < 384 && vocab <= kSampleMostVocab / 2 ? kSampleSmallSlice : kSampleLargeSlice;
 }

@@ -1,14 +1,14 @@
 // Softmax attention of new tokens over a paged cache: o_i = sum_j p_ij v_j, p_ij = exp(s_ij - lse_i), with the scales, bias and masks of the entmax
 // attention and, if asked for, scores capped by a tanh.  One pass over keys and values: a row's largest score and sum so far, its output so far
-// scaled down whenever a larger score comes.  Scores as in the tiled kernel there, S^T = K Q^T with a lane pair for each of 32 folded rows (token, head of the
+// scaled down whenever a much larger score comes.  Scores as in the tiled kernel there, S^T = K Q^T with a lane pair for each of 32 folded rows (token, head of the
 // group), whose probabilities are the second operand of O^T = V^T P^T as they are.
-//   softmax_split_kernel  sequences of at most kSplitRows folded rows (decode steps): the keys are cut into pieces, a workgroup each.  A wave
-//                         goes through 32-key tiles of its own, brought to LDS by loads that it alone waits for; the waves meet at the end.
-//                         Bound by the one read of K and V.
-//   softmax_join_kernel   adds up the pieces' outputs, each in units of its own largest score
-//   softmax_tiled_kernel  others: a workgroup per 128 folded rows and piece of the keys, tiles of keys and values shared by its waves; bound by the matrix
-//                         products, of which the one with V is made twice in bf16
-//   softmax_tiled_join_kernel  adds up such pieces
+//   softmax_split_piece()  sequences of at most kSplitRows folded rows (decode steps): the keys are cut into pieces, a workgroup each.  A wave
+//                          goes through 32-key tiles of its own, brought to LDS by loads that it alone waits for; the waves meet at the end.
+//                          Bound by the one read of K and V: 48 sequences of 150 to 9000 keys, 2 heads of 128, 23 us (4.1 TB/s); one of 65536 keys, 4 heads, 50 us (5.4 TB/s).
+//   softmax_tiled_piece()  others: a workgroup per 128 folded rows and piece of the keys, tiles of keys and values shared by its waves; bound by the matrix
+//                          products, of which the one with V is made twice in bf16
+//   softmax_join_kernel    adds up the pieces' outputs, each in units of its own reference score
+// Both kinds of pieces have a kernel of their own and one for calls that have both.
 #pragma once
 #include "launch.hip.h"
 #include "seq.hip.h"
@@ -65,7 +65,7 @@ struct SoftmaxShare {
 // The share of the sequence that has place x, with what it is; false: there is none.
 // Memory delivers as much as it can when all compute units ask for equal parts of it at the same time, and the host knows only a bound of the lengths: so
 // every wave adds up the tiles of all sequences (64 at a time, a lane each), divides them by the number of workgroups that fit the chip, and
-// numbers the pieces that come of it.  (48 sequences of 150 to 9000 keys, 2 heads of 128: 41 us with pieces by the bound, 27 so.)  With many
+// numbers the pieces that come of it.  (48 sequences of 150 to 9000 keys, 2 heads of 128: 41 us with pieces by the bound, 31 so.)  With many
 // sequences that would take longer than it gives: pieces by the bound.
 __device__ __forceinline__ bool softmax_share(const SoftmaxArgs& A, int x, SeqView& v, SoftmaxShare& sh) {
   const SeqGeom& g = A.g;
@@ -308,7 +308,8 @@ struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
   }
 };
 
-// A wave's 16 rows, four lanes each, on the matrix instructions of 16 x 16: half the work of SoftmaxRows where there are not more rows.
+// A wave's 16 rows, four lanes each, on the matrix instructions of 16 x 16: half the work of SoftmaxRows where there are not more rows.  (48 sequences of 150 to
+// 9000 keys: 31 us, 33 with 32 rows; 256 to 2000 keys: 66 and 77; 12 of three tokens in fp32, capped: 29 and 53.)
 // Lane l has row l % 16; of 32 keys those of 16 (e / 4) + 4 (l / 16) + e % 4, e = 0 .. 7, and of the output features 16 f + 4 (l / 16) + 0 .. 3.
 template <typename T, int D, bool CAP>
 struct SoftmaxRows16 : SeqRow, SoftmaxScale<T, CAP> {

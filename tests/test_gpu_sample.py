@@ -223,3 +223,15 @@ def test_replay_and_workspace(binding):
 
 def test_no_rows(binding):
     assert binding.sample(torch.zeros(0, 10, device="cuda"), torch.zeros(0, device="cuda")).shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_rows_far_apart(binding, dtype):
+    """Rows whose offsets need more than 32 bits."""
+    gen = torch.Generator().manual_seed(21)
+    x = (2 * torch.randn(3, 20000, generator=gen)).to(dtype)
+    u, p = torch.rand(3, generator=gen).cuda(), torch.full((3,), 0.9).cuda()
+    stride = (1 << 31) // x.element_size() + 8
+    far = torch.empty(2 * stride + 20000, dtype=dtype, device="cuda").as_strided((3, 20000), (stride, 1))
+    far.copy_(x)
+    assert torch.equal(binding.sample(far, u, None, None, p), binding.sample(x.cuda(), u, None, None, p))

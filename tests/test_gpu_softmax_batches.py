@@ -2,6 +2,7 @@
 import random
 
 import pytest
+import torch
 
 from tests.serving_util import BF16, FP32, Problem
 from tests.test_gpu_softmax import TYPES, _check, binding  # noqa: F401
@@ -64,3 +65,20 @@ def test_holes_behind_the_last_key_of_a_block(binding, D, dtype, what):  # noqa:
     p.table[0, 2:5] = what  # (32 tokens to a block: its first one sees keys 0 .. 31, in a tile of 64)
     p.table[1, 65:67] = what
     _check(binding, p, "holes")
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_pages_behind_four_gigabytes(binding, dtype):  # noqa: F811
+    """Bytes of pages whose offsets need more than 32 bits: the same as in a small cache."""
+    p = Problem([(1, 900), (70, 300), (12, 77)], Hq=4, Hkv=1, D=64, dtype=dtype, seed=76)
+    cu = torch.tensor(p.cu, dtype=torch.int32).cuda()
+    kv = torch.tensor([L for _, L in p.lens], dtype=torch.int32).cuda()
+    kw = {k: v for k, v in p.gpu_kw().items() if k != "alpha"}
+    small = binding.paged_softmax_fwd(p.q.cuda(), p.kc.cuda(), p.vc.cuda(), cu, kv, p.table.cuda(), **kw)
+    page = p.page * p.D
+    first = (1 << 32) // (2 * page * p.kc.element_size()) - p.pages // 2  # (in the middle of the pages that are used)
+    both = torch.empty(first + p.pages, 2, p.page, p.D, dtype=dtype, device="cuda")
+    both[first:, :1], both[first:, 1:] = p.kc.cuda(), p.vc.cuda()
+    table = torch.where(p.table >= 0, p.table + first, p.table).to(torch.int32).cuda()
+    large = binding.paged_softmax_fwd(p.q.cuda(), both[:, :1], both[:, 1:], cu, kv, table, **kw)
+    assert torch.equal(small, large)
