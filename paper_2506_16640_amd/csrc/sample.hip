@@ -583,9 +583,10 @@ __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs 
         if (tid == 0) {
           lds.least_key[turn ^ 1] = ~0u;
           lds.most_key[turn ^ 1] = 0;
-          lds.few[turn ^ 1] = 0;
         }
         __syncthreads();
+        // (every wave reads it behind the last barrier of a round: cleared sooner, a late one would see none and leave the loop alone)
+        if (tid == 0) lds.few[turn ^ 1] = 0;
         // bins from the highest down: the last one with something in it, before which the sum is below the target
         if (tid < 64) {
           u64 v[4], mine = 0;

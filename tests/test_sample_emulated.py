@@ -1,0 +1,78 @@
+"""Sampling with its kernels run on the CPU, lane by lane, and a workgroup's waves in the orders that depend most on its barriers (tests/emulate)."""
+import ctypes
+import math
+import os
+import subprocess
+
+import pytest
+import torch
+
+from tests.step_util import BF16, FP32, plain_sample
+from tests.test_sanitize_host import ROOT
+
+UNWRITTEN = -12345
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("emulate") / "sample_emulated.so")
+    here = os.path.join(ROOT, "tests", "emulate")
+    clang = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "clang++")
+    subprocess.run([clang, "-x", "c++", "-std=c++17", "-O1", "-fPIC", "-shared", "-w", "-I", here, "-I", os.path.join(ROOT, "include"), "-I",
+                    os.path.join(ROOT, "paper_2506_16640_amd", "csrc"), os.path.join(here, "sample_emulated.cc"), "-o", out], check=True)
+    lib = ctypes.CDLL(out)
+    lib.entmax_sample.argtypes = [ctypes.c_char_p] + [ctypes.c_void_p] * 9 + [ctypes.c_size_t, ctypes.c_void_p]
+    lib.entmax_sample_workspace_bytes.restype = ctypes.c_size_t
+    lib.emulate_end.restype = ctypes.c_char_p
+    return lib
+
+
+def sample(lib, logits, u, order, temperature=None, top_k=None, top_p=None, min_p=None):
+    from paper_2506_16640_amd import binding
+    R, V = logits.shape
+    p = binding._sample_bytes.pack(R, V, 0 if logits.dtype == BF16 else 1, V)
+    token, logprob = torch.full((R,), UNWRITTEN, dtype=torch.int32), torch.full((R,), float(UNWRITTEN))
+    # (a place that a read in front of or behind the workspace meets holds NaN)
+    need = int(lib.entmax_sample_workspace_bytes(p))
+    room = torch.full((need + (2 << 20),), 255, dtype=torch.uint8)
+    at = (room.data_ptr() + (1 << 20) + 255) // 256 * 256
+    lib.emulate_begin(order)
+    rc = lib.entmax_sample(p, logits.data_ptr(), u.data_ptr(), *[None if t is None else t.data_ptr() for t in (temperature, top_k, top_p, min_p)],
+                           token.data_ptr(), logprob.data_ptr(), at, need, None)
+    assert rc == 0
+    error = lib.emulate_end().decode()
+    assert not error, error
+    return token, logprob
+
+
+def check(lib, logits, u, label="", orders=(0, 1, 2), **kw):
+    want, want_lp = plain_sample(logits, u, **kw)
+    for order in orders:
+        token, logprob = sample(lib, logits, u, order, **kw)
+        assert torch.equal(token, want), (label, order, token.tolist(), want.tolist())
+        there = want >= 0
+        assert (logprob[~there] == -math.inf).all()
+        off = (logprob.double() - want_lp).abs()[there]
+        assert (off <= 2.0 ** -24 * want_lp.abs()[there] + 1e-9).all(), (label, order, off.max().item())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_ordinary_rows(lib, dtype):
+    g = torch.Generator().manual_seed(1)
+    x = (2 * torch.randn(4, 9001, generator=g)).to(dtype)
+    u = torch.rand(4, generator=g)
+    check(lib, x, u, "plain", temperature=torch.tensor([1.0, 0.0, 0.3, 5.0]))
+    check(lib, x, u, "filters", temperature=torch.tensor([1.0, 0.0, 0.3, 5.0]), top_k=torch.tensor([50, 3, 0, 4000], dtype=torch.int32),
+          top_p=torch.tensor([0.9, 0.5, 1.0, 0.99]), min_p=torch.tensor([0.0, 0.0, 0.05, 0.01]))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("values", [1, 3])
+def test_selections_of_several_rounds(lib, dtype, values):
+    """Equal logits: the bins of a round hold more tokens than are compared with each other, so that there is another one, in which the first wave clears what
+    the last one may not have read."""
+    g = torch.Generator().manual_seed(values)
+    x = torch.randint(values, (3, 8100), generator=g).to(dtype)
+    u = torch.tensor([0.2, 0.6, 0.99])
+    check(lib, x, u, "top-p", top_p=torch.tensor([0.5, 0.9, 0.3]))
+    check(lib, x, u, "both", top_k=torch.tensor([4000, 7000, 100], dtype=torch.int32), top_p=torch.tensor([0.5, 0.9, 0.99]))
