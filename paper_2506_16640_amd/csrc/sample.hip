@@ -380,7 +380,11 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bracket_kernel(Sampl
     const int cell = ask.cell(r.top);
     float sure = b0 == 0 ? kInf : (b0 == kSampleBins ? -kInf : ask.edge(cell - b0 + 1));
     // min-p without top-p: of what is a little below its bound no w is wanted
-    if (ask.has_m && !ask.has_p && r.top < kInf) sure = fmaxf(sure, RowAsk::next((float)((double)r.top + (log2(ask.f) - 1e-3) / ask.scale), -1));
+    // (at very high temperatures the bound is below all finite numbers, which are then left)
+    if (ask.has_m && !ask.has_p && r.top < kInf) {
+      const double bound = (double)r.top + (log2(ask.f) - 1e-3) / ask.scale;
+      if (bound > -3.4e38) sure = fmaxf(sure, RowAsk::next((float)bound, -1));
+    }
     if (lane == 0) {
       b0_ = b0;
       b1_ = b1;

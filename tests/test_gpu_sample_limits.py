@@ -1,0 +1,36 @@
+"""GPU tests of sampling at the ends of its arguments' ranges; all of them run on the CPU first (test_sample_emulated.py)."""
+import math
+
+import pytest
+import torch
+
+from tests.step_util import BF16, FP32
+from tests.test_gpu_sample import _check, binding  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("V", [300, 8192, 40001])
+def test_selections_of_several_rounds(binding, dtype, V):  # noqa: F811
+    """Lists of equal logits, whose selection goes over its bins more than once."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.randint(3, (40, V), generator=g).to(dtype)
+    x[0] = 1.0
+    u, p = torch.rand(40, generator=g), torch.rand(40, generator=g)
+    k = torch.randint(1, V, (40,), generator=g).to(torch.int32)
+    _check(binding, x, u, "top-p", top_p=p)
+    _check(binding, x, u, "both", top_p=p, top_k=k)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("V", [100, 9001, 40001])
+def test_min_p_at_very_high_temperatures(binding, dtype, V):  # noqa: F811
+    g = torch.Generator().manual_seed(V)
+    x, u = (3 * torch.randn(12, V, generator=g)).to(dtype), torch.rand(12, generator=g)
+    t = torch.tensor([1e30, 3e35, 3e36, 1e38, 3e38, math.inf] * 2)
+    k = torch.randint(1, V, (12,), generator=g).to(torch.int32)
+    for f in (1e-30, 0.2, 1.0):
+        _check(binding, x, u, "min-p", temperature=t, min_p=torch.full((12,), f))
+        _check(binding, x, u, "min-p and top-k", temperature=t, min_p=torch.full((12,), f), top_k=k)
+        _check(binding, x, u, "min-p and top-p", temperature=t, min_p=torch.full((12,), f), top_p=torch.full((12,), 0.7))

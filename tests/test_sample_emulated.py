@@ -76,3 +76,16 @@ def test_selections_of_several_rounds(lib, dtype, values):
     u = torch.tensor([0.2, 0.6, 0.99])
     check(lib, x, u, "top-p", top_p=torch.tensor([0.5, 0.9, 0.3]))
     check(lib, x, u, "both", top_k=torch.tensor([4000, 7000, 100], dtype=torch.int32), top_p=torch.tensor([0.5, 0.9, 0.99]))
+
+
+HOT = [3e36, 1e38, 3e38, math.inf]
+
+
+def test_min_p_at_very_high_temperatures(lib):
+    """All tokens are within min-p of the largest: how far below it they may be is more than a float holds."""
+    x = 3 * torch.randn(8, 4001, generator=torch.Generator().manual_seed(5))
+    u, t = torch.tensor([0.0, 0.3, 0.6, 0.99, 0.1, 0.5, 0.9, 0.2]), torch.tensor(2 * HOT)
+    for f in (1e-30, 0.2, 1.0):
+        check(lib, x, u, "min-p", orders=(0,), temperature=t, min_p=torch.full((8,), f))
+    check(lib, x, u, "min-p and top-k", orders=(0,), temperature=t, min_p=torch.full((8,), 0.2), top_k=torch.tensor([5, 400, 4000, 1] * 2, dtype=torch.int32))
+    check(lib, x.bfloat16(), u, "bf16", orders=(0,), temperature=t, min_p=torch.full((8,), 0.2))
