@@ -108,13 +108,14 @@ struct RowAsk {
   __device__ __forceinline__ float edge(int c) const {
     if (c <= -(1 << 29)) return -kInf;
     if (grid == 0.f) return c <= 0 ? -kInf : kInf;
-    float x = fminf(fmaxf((float)c / grid, -3.4e38f), 3.4e38f);
+    constexpr float kMost = 3.40282347e38f;  // (the largest finite number: it and its negative may be logits)
+    float x = fminf(fmaxf((float)c / grid, -kMost), kMost);
     // (the quotient is rounded, and so are products: a few steps of a float away at most; with a step of zero nothing but infinity is left)
-    for (int k = 0; k < 8 && cell(x) >= c && x > -3.4e38f; ++k) x = next(x, -1);
+    for (int k = 0; k < 8 && cell(x) >= c && x > -kMost; ++k) x = next(x, -1);
     for (int k = 0; k < 16 && cell(x) < c; ++k) x = next(x, 1);
     return x;
   }
-  static __device__ __forceinline__ float next(float x, int way) {  // the neighbour of a finite number (3.4e38's: infinity)
+  static __device__ __forceinline__ float next(float x, int way) {  // the neighbour of a finite number (the largest one's: infinity)
     const int b = (int)__float_as_uint(x), order = b < 0 ? (int)(0x80000000u - (uint32_t)b) : b;
     const int n = order + way;
     return __uint_as_float(n < 0 ? 0x80000000u - (uint32_t)n : (uint32_t)n);

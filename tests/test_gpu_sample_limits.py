@@ -34,3 +34,14 @@ def test_min_p_at_very_high_temperatures(binding, dtype, V):  # noqa: F811
         _check(binding, x, u, "min-p", temperature=t, min_p=torch.full((12,), f))
         _check(binding, x, u, "min-p and top-k", temperature=t, min_p=torch.full((12,), f), top_k=k)
         _check(binding, x, u, "min-p and top-p", temperature=t, min_p=torch.full((12,), f), top_p=torch.full((12,), 0.7))
+
+
+@pytest.mark.parametrize("V", [300, 20001])
+def test_lowest_logits_at_very_high_temperatures(binding, V):  # noqa: F811
+    """The lowest finite number is in the bin of the cut: the bin's tokens begin with it."""
+    x = torch.randn(12, V, generator=torch.Generator().manual_seed(6))
+    x[:, V // 3:] = torch.finfo(FP32).min
+    u = torch.linspace(0.01, 0.99, 12)
+    for t in (1e38, 2e38, 3e38):
+        _check(binding, x, u, "low", temperature=torch.full((12,), t), top_p=torch.tensor([0.9, 0.95, 0.99, 0.999] * 3))
+        _check(binding, x, u, "low, top-k", temperature=torch.full((12,), t), top_k=torch.full((12,), V - 50, dtype=torch.int32))

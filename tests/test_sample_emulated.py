@@ -89,3 +89,13 @@ def test_min_p_at_very_high_temperatures(lib):
         check(lib, x, u, "min-p", orders=(0,), temperature=t, min_p=torch.full((8,), f))
     check(lib, x, u, "min-p and top-k", orders=(0,), temperature=t, min_p=torch.full((8,), 0.2), top_k=torch.tensor([5, 400, 4000, 1] * 2, dtype=torch.int32))
     check(lib, x.bfloat16(), u, "bf16", orders=(0,), temperature=t, min_p=torch.full((8,), 0.2))
+
+
+def test_lowest_logits_at_very_high_temperatures(lib):
+    """The lowest finite number is in the bin of the cut: the bin's tokens begin with it."""
+    low = torch.finfo(FP32).min
+    x = torch.randn(4, 300, generator=torch.Generator().manual_seed(6))
+    x[:, 100:] = low
+    u = torch.tensor([0.2, 0.5, 0.8, 0.999])
+    for t in (1e38, 2e38, 3e38):
+        check(lib, x, u, "low", orders=(0,), temperature=torch.full((4,), t), top_p=torch.tensor([0.9, 0.99, 0.95, 0.999]))
