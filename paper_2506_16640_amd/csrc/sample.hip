@@ -536,7 +536,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs 
   }
   const bool held = listed <= kPickList;
   const int from0 = -(int)((reinterpret_cast<uintptr_t>(reinterpret_cast<const T*>(A.logits) + (long long)row * A.stride) & 15u) / sizeof(T));
-  auto in_steps = [&](float x) { return (u64)(ask.weight(x, r.top) * steps + 0.5); };
+  // (rounded up: a token with any w can be drawn, by a random number of 0 if by no other)
+  auto in_steps = [&](float x) { return (u64)ceil(ask.weight(x, r.top) * steps); };
   // every listed token: fn(rank, w in steps, slice)
   auto each = [&](auto fn) {
     if (held) {
@@ -778,31 +779,43 @@ __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs 
   }
   if (cuts) __syncthreads();
   if (tid >= 64) return;
-  double want = left, x = 0.0;
+  const double want = left;
+  double x = 0.0;
   if (lane < S::kBlocks) {
     x = A.blocks[(at + chosen) * S::kBlocks + lane] * (sums ? 1.0 : ask.weight(A.stat[at + chosen].top, r.top));
     if (cuts) x += (double)lds.block[lane] / steps;
   }
   {
     const double upto = wave_scan(x, 0.0, Add());
-    const u64 over = __ballot(x > 0.0 && upto > want), some = __ballot(x > 0.0);
-    const int l = over ? __builtin_ctzll(over) : 63 - __clzll((long long)some);  // (else the sum of the blocks fell just short of the slice's)
-    want -= lane_value(upto - x, l);
-    x = lane_value(x, l);
-    const int i0 = from0 + chosen * S::kSize + l * S::kBlock + lane * S::E;
+    const u64 over = __ballot(x > 0.0 && upto > want);
+    u64 some = __ballot(x > 0.0), past, any;
+    int l = over ? __builtin_ctzll(over) : 63 - __clzll((long long)some);  // (else the sum of the blocks fell just short of the slice's)
     S sl;
     sl.init(A, row, chosen);
+    int i0;
     float v[S::E];
-    sl.load_chunk(i0, v);
-    double w[S::E], sum = 0.0;
+    double w[S::E], sum, to, rest;
+    for (;;) {
+      rest = want - lane_value(upto - x, l);
+      i0 = from0 + chosen * S::kSize + l * S::kBlock + lane * S::E;
+      sl.load_chunk(i0, v);
+      sum = 0.0;
 #pragma unroll
-    for (int e = 0; e < S::E; ++e) {
-      w[e] = ask.weight(v[e], r.top);
-      if (!(w[e] >= ask.f) || Rank<T>::of(v[e], i0 + e) < cut) w[e] = 0.0;
-      sum += w[e];
+      for (int e = 0; e < S::E; ++e) {
+        w[e] = ask.weight(v[e], r.top);
+        if (!(w[e] >= ask.f) || Rank<T>::of(v[e], i0 + e) < cut) w[e] = 0.0;
+        sum += w[e];
+      }
+      to = wave_scan(sum, 0.0, Add());
+      past = __ballot(sum > 0.0 && to > rest);
+      any = __ballot(sum > 0.0);
+      // A block's sum next to the slice's largest may be a number where w next to the row's largest is less than 2^-1074 for each of its tokens: the next block,
+      // or else the one before.  (The block with the slice's largest has a token; the random number is 0 or 1 where this counts.)
+      some &= ~(1ull << l);
+      if (any || some == 0) break;
+      const u64 behind = some & (~0ull << l);
+      l = behind ? __builtin_ctzll(behind) : 63 - __clzll((long long)some);
     }
-    const double to = wave_scan(sum, 0.0, Add());
-    const u64 past = __ballot(sum > 0.0 && to > want), any = __ballot(sum > 0.0);
     const int mine = past ? __builtin_ctzll(past) : 63 - __clzll((long long)any);
     if (lane == mine) {
       double t = to - sum, drawn = 0.0;
@@ -814,7 +827,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_pick_kernel(SampleArgs 
         if (w[e] > 0.0 && !done) {
           token = i0 + e;
           drawn = w[e];
-          done = t > want;
+          done = t > rest;
         }
       }
       A.token[row] = token;

@@ -45,3 +45,21 @@ def test_lowest_logits_at_very_high_temperatures(binding, V):  # noqa: F811
     for t in (1e38, 2e38, 3e38):
         _check(binding, x, u, "low", temperature=torch.full((12,), t), top_p=torch.tensor([0.9, 0.95, 0.99, 0.999] * 3))
         _check(binding, x, u, "low, top-k", temperature=torch.full((12,), t), top_k=torch.full((12,), V - 50, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_random_number_zero(binding, dtype):  # noqa: F811
+    """The first token with any probability, however small: those that are 2^-1074 of the largest as well."""
+    u = torch.tensor([0.0, 1.0])
+    x = torch.full((2, 20000), -800.0)
+    x[:, 12000] = 0.0
+    for at in (-500.0, -744.0, -744.4, -744.9) if dtype == FP32 else (-500.0, -744.0):
+        x[:, 300:900] = at - (1.0 if dtype == FP32 else 4.0)
+        x[:, 5000:5300] = at
+        x[0, 15000:15600] = at - 4.0
+        _check(binding, x.to(dtype), u, "plain %g" % at)
+        _check(binding, x.to(dtype), u, "min-p %g" % at, min_p=torch.full((2,), 1e-38))
+    x = torch.randn(2, 9000, generator=torch.Generator().manual_seed(7)).to(dtype)
+    k = torch.tensor([5, 700], dtype=torch.int32)
+    _check(binding, x, u, "top-k", temperature=torch.full((2,), 0.01), top_k=k)
+    _check(binding, x, u, "top-k and top-p", temperature=torch.full((2,), 0.01), top_k=k, top_p=torch.tensor([0.9999, 1.0]))

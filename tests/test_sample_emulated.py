@@ -99,3 +99,21 @@ def test_lowest_logits_at_very_high_temperatures(lib):
     u = torch.tensor([0.2, 0.5, 0.8, 0.999])
     for t in (1e38, 2e38, 3e38):
         check(lib, x, u, "low", orders=(0,), temperature=torch.full((4,), t), top_p=torch.tensor([0.9, 0.99, 0.95, 0.999]))
+
+
+def test_random_number_zero(lib):
+    """The first token with any probability, however small: those that are 2^-1074 of the largest as well."""
+    u = torch.tensor([0.0, 1.0])
+    x = torch.full((2, 20000), -800.0)
+    x[:, 12000] = 0.0
+    for at in (-500.0, -744.4, -744.9, -745.0, -745.13):
+        # (two slices, the first of which holds nothing but these; tokens whose own w is none next to others of their block and slice that have some)
+        x[:, 300:900] = at - 1.0
+        x[:, 5000:5300] = at
+        x[0, 15000:15600] = at - 1.0
+        check(lib, x, u, "plain %g" % at, orders=(0,))
+        check(lib, x, u, "min-p %g" % at, orders=(0,), min_p=torch.full((2,), 1e-38))
+    x = torch.randn(2, 9000, generator=torch.Generator().manual_seed(7))
+    k = torch.tensor([5, 700], dtype=torch.int32)
+    check(lib, x, u, "top-k", orders=(0,), temperature=torch.full((2,), 0.01), top_k=k)
+    check(lib, x, u, "top-k and top-p", orders=(0,), temperature=torch.full((2,), 0.01), top_k=k, top_p=torch.tensor([0.9999, 1.0]))
