@@ -381,7 +381,8 @@ size_t entmax_plan_workspace_bytes(const entmax_plan_params* p);
  * p->path = 0.  cap: 0, or c > 0 for scores c tanh(s / c); with bias_mode 1 the bias is added after that (c tanh(scale z / c) + b), with bias_mode 0 it
  * is part of s.
  *   lse: NULL, or [Hq, T] fp32: the rows' lse (-infinity where a row sees no key); rows that no sequence owns are left as they are.
- * Keys that a row does not see do not influence it whatever they hold; O, lse must not meet each other or what is read (INVALID_ARG).
+ * Keys that a row does not see do not influence it whatever they hold.  O, lse must not meet each other, what is read (lengths, page table, scales
+ * and slopes included) or the workspace, nor the workspace Q, K, V, beta, gamma or alibi_slopes (INVALID_ARG).
  * Calls need entmax_softmax_workspace_bytes(p) bytes of 256-byte aligned workspace; calls that may overlap in time need one each.
  */
 int entmax_paged_softmax_fwd(const entmax_seq_params* p, float cap, const void* Q, const void* K, const void* V, const int32_t* cu_seqlens,

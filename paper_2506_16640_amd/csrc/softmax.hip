@@ -37,7 +37,7 @@ int entmax_paged_softmax_fwd(const entmax_seq_params* p, float cap, const void* 
   if (off4(cu_seqlens) || off4(kv_len) || off4(page_table) || off4(beta) || off4(gamma) || off4(alibi_slopes) || off4(lse))
     return ENTMAX_ATTN_MISALIGNED;
   if (workspace_bytes < softmax_workspace_bytes_of(p)) return ENTMAX_ATTN_WORKSPACE_TOO_SMALL;
-  if (!softmax_outputs_apart(p, Q, K, V, O, lse)) return ENTMAX_ATTN_INVALID_ARG;
+  if (!softmax_outputs_apart(p, SoftmaxArrays{Q, K, V, cu_seqlens, kv_len, page_table, beta, gamma, alibi_slopes, O, lse, workspace})) return ENTMAX_ATTN_INVALID_ARG;
   const SoftmaxCall c{p, cap, Q, K, V, cu_seqlens, kv_len, page_table, beta, gamma, alibi_slopes, O, lse, reinterpret_cast<char*>(workspace),
                       reinterpret_cast<hipStream_t>(hip_stream)};
   if (p->dtype == ENTMAX_ATTN_BF16) return p->D == 64 ? run_softmax<bf16_t, 64>(c) : run_softmax<bf16_t, 128>(c);

@@ -109,17 +109,30 @@ inline size_t softmax_workspace_bytes_of(const entmax_seq_params* p) {
   return check_softmax_params(p) == ENTMAX_ATTN_OK ? make_softmax_layout(p).total : 0;
 }
 
-// Whether O and lse are apart from each other and from what is read
-inline bool softmax_outputs_apart(const entmax_seq_params* p, const void* Q, const void* K, const void* V, const void* O, const void* lse) {
-  if (!seq_output_apart(p, Q, K, V, O)) return false;
+// Whether O and lse are apart from each other, from what is read (every workgroup may read all of it at any time) and from the workspace, and the workspace from
+// tensors of floats that are read.
+struct SoftmaxArrays {
+  const void *Q, *K, *V, *cu, *kv_len, *table, *beta, *gamma, *slopes;  // read
+  const void *O, *lse, *workspace;
+};
+inline bool softmax_outputs_apart(const entmax_seq_params* p, const SoftmaxArrays& x) {
+  if (!seq_output_apart(p, x.Q, x.K, x.V, x.O)) return false;
   const int64_t es = p->dtype == ENTMAX_ATTN_BF16 ? 2 : 4, row = p->D * es;
-  const RowSet l{lse, {1, 1, 1}, {0, 0, 0}, 4ll * p->Hq * p->T};
-  const RowSet x[4] = {RowSet{O, {p->T, p->Hq, 1}, {p->o_stride_t * es, p->o_stride_h * es, 0}, row},
-                       RowSet{Q, {p->T, p->Hq, 1}, {p->q_stride_t * es, p->q_stride_h * es, 0}, row},
-                       RowSet{K, {p->num_pages, p->Hkv, p->page_size}, {p->k_stride_p * es, p->k_stride_h * es, p->k_stride_n * es}, row},
-                       RowSet{V, {p->num_pages, p->Hkv, p->page_size}, {p->v_stride_p * es, p->v_stride_h * es, p->v_stride_n * es}, row}};
-  for (int k = 0; k < 4; ++k)
-    if (rows_meet(l, x[k])) return false;
+  auto one = [](const void* at, long long bytes) { return RowSet{bytes > 0 ? at : nullptr, {1, 1, 1}, {0, 0, 0}, bytes}; };
+  const long long scales = p->scale_layout == 0 ? 0 : 4ll * p->Hq * (p->scale_layout == 1 ? 1 : p->T);
+  const RowSet out[3] = {RowSet{x.O, {p->T, p->Hq, 1}, {p->o_stride_t * es, p->o_stride_h * es, 0}, row}, one(x.lse, 4ll * p->Hq * p->T),
+                         one(x.workspace, (long long)make_softmax_layout(p).total)};
+  const RowSet in[9] = {RowSet{x.Q, {p->T, p->Hq, 1}, {p->q_stride_t * es, p->q_stride_h * es, 0}, row},
+                        RowSet{x.K, {p->num_pages, p->Hkv, p->page_size}, {p->k_stride_p * es, p->k_stride_h * es, p->k_stride_n * es}, row},
+                        RowSet{x.V, {p->num_pages, p->Hkv, p->page_size}, {p->v_stride_p * es, p->v_stride_h * es, p->v_stride_n * es}, row},
+                        one(x.beta, scales), one(x.gamma, scales), one(x.slopes, 4ll * p->Hq),
+                        one(x.cu, 4ll * p->nseq + 4), one(x.kv_len, 4ll * p->nseq), one(x.table, 4ll * p->nseq * p->max_pages)};
+  for (int a = 0; a < 3; ++a) {
+    for (int c = a + 1; c < 3; ++c)
+      if (rows_meet(out[a], out[c])) return false;
+    for (int c = 0; c < (a == 2 ? 6 : 9); ++c)
+      if (rows_meet(out[a], in[c])) return false;
+  }
   return true;
 }
 
