@@ -98,16 +98,17 @@ struct RowAsk {
     const double w = power(((double)x - (double)m) * scale);
     return x == -kInf ? 0.0 : w;
   }
-  // The logit's place on the row's grid of bins.  (That it never falls as x rises is all that matters: bins of a row's slices are the same ones.)
+  // The logit's place on the row's grid of bins.  (That it never falls as x rises is all that matters: bins of a row's slices are the same ones.  Negative logits
+  // are below 0 also where their product is none: edge() could not find the end of those otherwise.)
   __device__ __forceinline__ int cell(float x) const {
     if (x == kInf) return 1 << 29;
     if (x == -kInf) return -(1 << 29);
-    return (int)fminf(fmaxf(floorf(x * grid), -(float)(1 << 29)), (float)(1 << 29));
+    return (int)fminf(fmaxf(floorf(x * grid), -(float)(1 << 29)), x < 0.f ? -1.f : (float)(1 << 29));
   }
   // The smallest logit of cell c or above (-inf: all of them are)
   __device__ __forceinline__ float edge(int c) const {
     if (c <= -(1 << 29)) return -kInf;
-    if (grid == 0.f) return c <= 0 ? -kInf : kInf;
+    if (grid == 0.f) return c < 0 ? -kInf : c == 0 ? 0.f : kInf;
     constexpr float kMost = 3.40282347e38f;  // (the largest finite number: it and its negative may be logits)
     float x = fminf(fmaxf((float)c / grid, -kMost), kMost);
     // (the quotient is rounded, and so are products: a few steps of a float away at most; with a step of zero nothing but infinity is left)

@@ -63,3 +63,17 @@ def test_random_number_zero(binding, dtype):  # noqa: F811
     k = torch.tensor([5, 700], dtype=torch.int32)
     _check(binding, x, u, "top-k", temperature=torch.full((2,), 0.01), top_k=k)
     _check(binding, x, u, "top-k and top-p", temperature=torch.full((2,), 0.01), top_k=k, top_p=torch.tensor([0.9999, 1.0]))
+
+
+def test_tiny_logits_at_very_high_temperatures(binding):  # noqa: F811
+    """Logits times the bins' grid that no float holds: negative ones stay below zero's bin."""
+    g = torch.Generator().manual_seed(3)
+    u = torch.tensor([0.0, 0.3, 0.7, 0.98])
+    for scale, t in ((1e-30, 1e20), (1e-30, 3e38), (1e-38, 1e30), (1.0, 3e38), (1e-44, math.inf), (1.0, math.inf)):
+        for V in (700, 9001):
+            x, T = scale * torch.randn(4, V, generator=g), torch.full((4,), t)
+            x[0, ::7] = 0.0
+            x[1, ::9] = -0.0
+            _check(binding, x, u, "top-p %g" % scale, temperature=T, top_p=torch.tensor([0.9, 0.99, 1e-30, 0.3]))
+            _check(binding, x, u, "top-k %g" % scale, temperature=T, top_k=torch.tensor([3, 400, 20, 699], dtype=torch.int32))
+            _check(binding, -x.abs(), u, "negative %g" % scale, temperature=T, top_p=torch.tensor([0.9, 0.99, 1e-30, 0.3]))

@@ -117,3 +117,16 @@ def test_random_number_zero(lib):
     k = torch.tensor([5, 700], dtype=torch.int32)
     check(lib, x, u, "top-k", orders=(0,), temperature=torch.full((2,), 0.01), top_k=k)
     check(lib, x, u, "top-k and top-p", orders=(0,), temperature=torch.full((2,), 0.01), top_k=k, top_p=torch.tensor([0.9999, 1.0]))
+
+
+def test_tiny_logits_at_very_high_temperatures(lib):
+    """Logits times the bins' grid that no float holds: negative ones stay below zero's bin."""
+    g = torch.Generator().manual_seed(3)
+    u = torch.tensor([0.0, 0.3, 0.7, 0.98])
+    for scale, t in ((1e-30, 1e20), (1e-30, 3e38), (1e-38, 1e30), (1.0, 3e38), (1e-44, math.inf), (1.0, math.inf)):
+        x, t = scale * torch.randn(4, 700, generator=g), torch.full((4,), t)
+        x[0, ::7] = 0.0
+        x[1, ::9] = -0.0
+        check(lib, x, u, "top-p %g" % scale, orders=(0,), temperature=t, top_p=torch.tensor([0.9, 0.99, 1e-30, 0.3]))
+        check(lib, x, u, "top-k %g" % scale, orders=(0,), temperature=t, top_k=torch.tensor([3, 400, 20, 699], dtype=torch.int32))
+        check(lib, -x.abs(), u, "negative %g" % scale, orders=(0,), temperature=t, top_p=torch.tensor([0.9, 0.99, 1e-30, 0.3]))
