@@ -122,36 +122,58 @@ __device__ __forceinline__ bool softmax_share(const SoftmaxArgs& A, int x, SeqVi
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// A cap above this is none: c tanh(s / c) is s to a step of a float up to c / 4096, 2^52, and exponentials of numbers of that size are 0 or 1 either way.  (From
+// 2e38 on the cap itself would leave the range of a float in units of log 2, and s / c that of whole ones.)
+constexpr float kSoftmaxMostCap = 18446744073709551616.f;
+// bf16: up to this cap 1.2e-7 of it is no more than the 2^-17 or so that probabilities as two bf16 numbers are off by, and tanh needs no series near zero.  (4 x 700 tokens against
+// 6000 keys, 4 x 4 heads of 128, cap 30: 333 us, 387 with the series.)
+constexpr float kSoftmaxPlainCap = 64.f;
+
 // From accumulators of the dot products to scores in units of log 2: score = unit * x, x the accumulator or, with a cap, what capped() makes of it.
 template <typename T, bool CAP>
 struct SoftmaxScale {
   float unit, slack;      // slack: x of a factor of 2^24
   float cap2, in2, late;  // CAP: cap in units of log 2; s / cap = in2 * accumulator; slope of a bias outside the cap
+  bool series;            // CAP: the same in all lanes
   // a, w: as in SeqRow; w is zero afterwards if the bias is added late
   __device__ __forceinline__ void init_scale(const SoftmaxArgs& A, float a, float& w) {
     unit = CAP ? 1.f : a * kLog2e;
     slack = fminf(24.f / unit, 1e30f);
     if (CAP) {
       cap2 = A.cap * kLog2e;
-      in2 = a / A.cap;
+      in2 = fminf(a / A.cap, 3e38f);  // (no infinity that a product of 0 would meet)
       late = 0.f;
+      series = A.cap > kSoftmaxPlainCap;
       if (A.g.bias_mode == 1) {
         late = a * w * kLog2e;
         w = 0.f;
       }
     }
   }
+  // SERIES: see kSoftmaxPlainCap
+  template <bool SERIES>
   __device__ __forceinline__ float capped(float acc, int dist) const {
-    // 1 - 2 / (1 + exp(2 x)): off by some 1.2e-7, of the cap.  fp32: near zero, where that is much of the value, the first five terms of the series
-    // (the sixth is 1e-8 of it at 1/4)
+    // 1 - 2 / (1 + exp(2 x)): off by some 1.2e-7, of the cap.  SERIES: near zero, where that is much of the value (all of it with a cap far above the scores), the
+    // first five terms of the series (the sixth is 1e-8 of it at 1/4)
     const float x = acc * in2;
     float t = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * (2.f * kLog2e)));
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (SERIES) {
       const float x2 = x * x;
       const float near = x * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
       t = x2 < 0.0625f ? near : t;
     }
     return fmaf(late, (float)max(dist, 0), cap2 * t);
+  }
+  // N scores, dist(e) the distance of the e-th
+  template <int N, typename V, class F>
+  __device__ __forceinline__ void cap_all(V& x, F dist) const {
+    if (sizeof(T) == 4 || series) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = capped<true>(x[e], dist(e));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = capped<false>(x[e], dist(e));
+    }
   }
 };
 
@@ -226,8 +248,7 @@ struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
     }
   }
   __device__ __forceinline__ void cap_scores(f32x16_t& acc, int j0) const {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = this->capped(acc[e], this->pos - j0 - this->key_of(e));
+    this->template cap_all<16>(acc, [&](int e) { return this->pos - j0 - this->key_of(e); });
   }
   __device__ __forceinline__ void add_bias(f32x16_t& acc, int j0) const {
 #pragma unroll
@@ -403,8 +424,9 @@ struct SoftmaxRows16 : SeqRow, SoftmaxScale<T, CAP> {
         for (int e = 0; e < 4; ++e) acc[e] = w * (float)max(pos - j0 - key_of(4 * b + e), 0);
       }
       acc = scores(at, tile, b, acc);
+      if constexpr (CAP) this->template cap_all<4>(acc, [&](int e) { return pos - j0 - key_of(4 * b + e); });
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * b + e] = CAP ? this->capped(acc[e], pos - j0 - key_of(4 * b + e)) : acc[e];
+      for (int e = 0; e < 4; ++e) x[4 * b + e] = acc[e];
     }
     const bool masked = hole || j0 + 32 > lim_min;
     if (masked) {
@@ -1082,7 +1104,7 @@ int run_softmax(const SoftmaxCall& c) {
   a.tsums = reinterpret_cast<float2*>(c.ws + L.off_tsums);
   a.tpiece = L.tpiece;
   a.tsplits = L.tsplits;
-  const bool ok = c.cap > 0.f ? launch_softmax<T, D, true>(a, L, c.st) : launch_softmax<T, D, false>(a, L, c.st);
+  const bool ok = c.cap > 0.f && c.cap <= kSoftmaxMostCap ? launch_softmax<T, D, true>(a, L, c.st) : launch_softmax<T, D, false>(a, L, c.st);
   return ok ? ENTMAX_ATTN_OK : ENTMAX_ATTN_LAUNCH_FAILED;
 }
 
