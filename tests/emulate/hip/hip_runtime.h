@@ -19,7 +19,8 @@
 #define __forceinline__ inline
 #define __launch_bounds__(...)
 #define __shared__ static
-#define asm(...)  // (only to hide values from the compiler)
+#define asm(...)           // (only to hide values from the compiler)
+#define volatile(...) ("")  // (of asm volatile: loads to LDS, which nothing here runs)
 
 struct dim3 {
   unsigned x, y, z;
@@ -67,7 +68,7 @@ inline World& world() {
   return w;
 }
 struct Index { unsigned x, y, z; };
-inline Index thread_index, block_index, block_dim;
+inline Index thread_index, block_index, block_dim, grid_dim;
 
 inline void fail(const char* text, int a, int b) {
   if (!world().error[0]) snprintf(world().error, sizeof(world().error), "%s (%d, %d)", text, a, b);
@@ -185,6 +186,7 @@ void launch(K kernel, dim3 grid, dim3 block, A... args) {
   w.waves.resize((w.threads + 63) / 64);
   w.stacks.resize((size_t)w.threads * kStack);
   block_dim = {block.x, 1, 1};
+  grid_dim = {grid.x, 1, 1};
   w.body = [=] { kernel(args...); };
   for (unsigned x = 0; x < grid.x && !w.error[0]; ++x) {
     block_index = {x, 0, 0};
@@ -197,6 +199,7 @@ void launch(K kernel, dim3 grid, dim3 block, A... args) {
 #define threadIdx emulate::thread_index
 #define blockIdx emulate::block_index
 #define blockDim emulate::block_dim
+#define gridDim emulate::grid_dim
 #define __syncthreads() emulate::barrier(__LINE__)
 #define hipLaunchKernelGGL(kernel, grid, block, lds, stream, ...) emulate::launch(kernel, grid, block, __VA_ARGS__)
 
@@ -218,6 +221,17 @@ inline int __builtin_amdgcn_readlane(int x, int lane) {
   const emulate::Wave& w = emulate::meet(3, (unsigned)x);
   return (int)w.values[lane & 63];
 }
+template <class V>
+inline V __shfl(V x, int lane) {
+  unsigned bits;
+  static_assert(sizeof(V) == 4, "");
+  memcpy(&bits, &x, 4);
+  bits = (unsigned)emulate::meet(2048, bits).values[lane & 63];
+  memcpy(&x, &bits, 4);
+  return x;
+}
+template <class V>
+inline V __shfl_xor(V x, int mask) { return __shfl(x, emulate_lane() ^ mask); }
 inline int __builtin_amdgcn_update_dpp(int old, int x, int ctrl, int rows, int banks, bool) {
   const int me = emulate_lane(), row = me >> 4;
   const emulate::Wave& w = emulate::meet(4 + ctrl, (unsigned)x);
@@ -266,7 +280,12 @@ inline float emulate_min(float a, float b) { return emulate_signals(a) || emulat
 #define fmaxf emulate_max
 #define fminf emulate_min
 
-// (the matrix products of the headers, which nothing here runs)
+// (matrix products and others of the headers, which nothing here runs)
+inline int __syncthreads_or(int x) {
+  emulate::fail("not here", __LINE__, x);
+  return x;
+}
+#define __builtin_amdgcn_sched_group_barrier(...)
 #define __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, ...) (c)
 #define __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, ...) (c)
 #define __builtin_amdgcn_exp2f exp2f
