@@ -63,7 +63,7 @@ struct RowAsk {
     const float t = A.temperature ? A.temperature[row] : 1.f;
     greedy = nan(t) || !(t > 0.f);
     const double inv = greedy ? 1.0 : 1.0 / (double)t;
-    scale = inv * 1.4426950408889634;
+    scale = fmax(inv * 1.4426950408889634, 1e-300);  // (more than zero, so that -infinity stays what it is; 1e-300 of a logit is nothing)
     k = A.top_k ? A.top_k[row] : 0;
     has_k = k > 0 && k < A.vocab;
     const float pp = A.top_p ? A.top_p[row] : 1.f, mm = A.min_p ? A.min_p[row] : 0.f;
@@ -77,7 +77,7 @@ struct RowAsk {
     grid = greedy ? 0.f : (float)fmin(has_k ? fmin(12.0 * inv, 12.0) : 32.0 * inv, 1e30);
   }
   // 2^t, t <= 0, to 4e-14 of it and 1 for 0: the whole part goes to the exponent; the rest f, at most 1/2, through 1 + f p(f), p interpolating (2^f - 1) / f at the
-  // nine zeros of a Chebyshev polynomial.  (-infinity: undefined)
+  // nine zeros of a Chebyshev polynomial.  (From -1100 on: the whole part is one of 32 bits)
   static __device__ __forceinline__ double power(double t) {
     const double k = rint(t), f = t - k;
     double p = 1.0203121172135084e-07;
@@ -95,8 +95,8 @@ struct RowAsk {
   // w of a logit x next to the largest, m
   __device__ __forceinline__ double weight(float x, float m) const {
     if (m == kInf || m == -kInf) return x == m && x > 0.f ? 1.0 : 0.0;  // (uniform)
-    const double w = power(((double)x - (double)m) * scale);
-    return x == -kInf ? 0.0 : w;
+    // (below 2^-1074 all are 0.  Unbounded, t - k would be formed from the product before it is rounded, which beyond 2^53 is a number of any size)
+    return power(fmax(((double)x - (double)m) * scale, -1100.0));
   }
   // The logit's place on the row's grid of bins.  (That it never falls as x rises is all that matters: bins of a row's slices are the same ones.  Negative logits
   // are below 0 also where their product is none: edge() could not find the end of those otherwise.)

@@ -77,3 +77,19 @@ def test_tiny_logits_at_very_high_temperatures(binding):  # noqa: F811
             _check(binding, x, u, "top-p %g" % scale, temperature=T, top_p=torch.tensor([0.9, 0.99, 1e-30, 0.3]))
             _check(binding, x, u, "top-k %g" % scale, temperature=T, top_k=torch.tensor([3, 400, 20, 699], dtype=torch.int32))
             _check(binding, -x.abs(), u, "negative %g" % scale, temperature=T, top_p=torch.tensor([0.9, 0.99, 1e-30, 0.3]))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("V", [3, 9001, 40001])
+def test_lowest_logits_at_very_low_temperatures(binding, dtype, V):  # noqa: F811
+    """Masks of the lowest finite number: exponents that are far beyond the whole numbers of 64-bit floats."""
+    g = torch.Generator().manual_seed(V)
+    x, u = (3 * torch.randn(12, V, generator=g)).to(dtype), torch.rand(12, generator=g)
+    u[0], u[1] = 0.0, 1.0
+    x[:, ::2] = torch.finfo(dtype).min
+    x[6:, :V - 3] = torch.finfo(dtype).min
+    for t in (1e-6, 1e-12, 1e-13, 1e-20, 1e-38, 1e-40, 1e-45):
+        t = torch.full((12,), t)
+        _check(binding, x, u, "plain", temperature=t)
+        _check(binding, x, u, "top-p", temperature=t, top_p=torch.tensor([0.5, 0.9, 0.0] * 4))
+        _check(binding, x, u, "top-k, min-p", temperature=t, min_p=torch.tensor([0.0, 0.1, 1.0] * 4), top_k=torch.tensor([5, 0, 4000, 1] * 3, dtype=torch.int32))

@@ -130,3 +130,18 @@ def test_tiny_logits_at_very_high_temperatures(lib):
         check(lib, x, u, "top-p %g" % scale, orders=(0,), temperature=t, top_p=torch.tensor([0.9, 0.99, 1e-30, 0.3]))
         check(lib, x, u, "top-k %g" % scale, orders=(0,), temperature=t, top_k=torch.tensor([3, 400, 20, 699], dtype=torch.int32))
         check(lib, -x.abs(), u, "negative %g" % scale, orders=(0,), temperature=t, top_p=torch.tensor([0.9, 0.99, 1e-30, 0.3]))
+
+
+def test_lowest_logits_at_very_low_temperatures(lib):
+    """Masks of the lowest finite number: exponents that are far beyond the whole numbers of 64-bit floats."""
+    g = torch.Generator().manual_seed(8)
+    u = torch.tensor([0.0, 0.3, 0.9, 1.0])
+    for dtype in (BF16, FP32):
+        x = (3 * torch.randn(4, 9001, generator=g)).to(dtype)
+        x[:, ::2] = torch.finfo(dtype).min
+        x[2:, :8500] = torch.finfo(dtype).min
+        for t in (1e-6, 1e-13, 1e-40):
+            t = torch.full((4,), t)
+            check(lib, x, u, "plain", orders=(0,), temperature=t)
+            check(lib, x, u, "filters", orders=(0,), temperature=t, top_p=torch.tensor([0.5, 0.9, 1.0, 0.0]), min_p=torch.tensor([0.0, 0.1, 0.1, 0.0]),
+                  top_k=torch.tensor([0, 0, 5, 4000], dtype=torch.int32))
