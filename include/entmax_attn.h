@@ -399,12 +399,14 @@ size_t entmax_softmax_workspace_bytes(const entmax_seq_params* p);
  *      w of all that step 1 left; the first stays in any case
  *   3. min_p = f > 0: those with w_i >= min(f, 1) stay
  *   4. the token is the first, by index, up to and with which the w that are left add up to more than uniform times their sum
- * Sums and w are of 64 bits.  temperature <= 0 (or NaN): the largest logit, of equal ones the first, whatever the filters; logprob 0.
+ * Sums and w are of 64 bits; sums that differ by less than 2.3e-13 of themselves count as equal.
+ * temperature <= 0 (or NaN): the largest logit, of equal ones the first, whatever the filters; logprob 0.
  *   temperature, top_p, min_p fp32 [rows], top_k int32 [rows]: NULL where not wanted (temperature 1).  A top_k <= 0 or >= vocab, top_p >= 1 or
  *   NaN, min_p <= 0 or NaN leave all; top_p <= 0 leaves the first.  uniform: fp32 [rows] in [0, 1); others count as the nearest (NaN as 0).
  *   token: int32 [rows].  logprob: NULL, or fp32 [rows]: log of the probability with which the token was drawn.
  * Logits of -infinity and NaN are never drawn; those of +infinity share all the probability.  A row without any other: token -1, logprob -infinity.
- * entmax_sample_workspace_bytes(p) bytes of 256-byte aligned workspace; contents do not matter; calls that may overlap in time need one each.
+ * entmax_sample_workspace_bytes(p) bytes of 256-byte aligned workspace; contents do not matter; calls that may overlap in time need one each.  It has room to
+ * list every token, 4 bytes each for bf16 and 8 for fp32, of rows rounded up to 8192 or 16384 logits, whatever the filters: 100 MB for 256 x 32768 fp32.
  */
 typedef struct {
   int32_t rows, vocab; /* at most 2^20, 2^22 */

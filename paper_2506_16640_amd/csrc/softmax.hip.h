@@ -4,7 +4,7 @@
 // group), whose probabilities are the second operand of O^T = V^T P^T as they are.
 //   softmax_split_piece()  sequences of at most kSplitRows folded rows (decode steps): the keys are cut into pieces, a workgroup each.  A wave
 //                          goes through 32-key tiles of its own, brought to LDS by loads that it alone waits for; the waves meet at the end.
-//                          Bound by the one read of K and V: 48 sequences of 150 to 9000 keys, 2 heads of 128, 23 us (4.1 TB/s); one of 65536 keys, 4 heads, 50 us (5.4 TB/s).
+//                          Bound by the one read of K and V: 48 sequences of 150 to 9000 keys, 2 heads of 128, 23 us (4.1 TB/s); two of 65536 keys, 4 heads, 50 us (5.4 TB/s).
 //   softmax_tiled_piece()  others: a workgroup per 128 folded rows and piece of the keys, tiles of keys and values shared by its waves; bound by the matrix
 //                          products, of which the one with V is made twice in bf16
 //   softmax_join_kernel    adds up the pieces' outputs, each in units of its own reference score
@@ -255,7 +255,8 @@ struct SoftmaxRows : SeqRows<T, D>, SoftmaxScale<T, CAP> {
     for (int e = 0; e < 16; ++e) acc[e] = fmaf(this->w, (float)max(this->pos - j0 - this->key_of(e), 0), acc[e]);
   }
   // Moves `top` to 2^24 times the largest score if some score x = acc (masked ones -inf) is above it.  No probability is above 1 then, so that the sums overflow
-  // no sooner than those of exp(s - max) v would; the largest is 2^-24 at least, so that none that counts is lost at 2^-126; and the sums are rarely scaled anew.
+  // no sooner than those of exp(s - max) v would; the largest is 2^-24 at least, so that none that counts is lost at 2^-126; and the sums are rarely scaled anew.  It
+  // costs accuracy: exponents near -24 are rounded to 2^-20, probabilities to 6.6e-7 of them instead of 6e-8.
   template <int NB>
   __device__ __forceinline__ void raise(const f32x16_t (&acc)[NB]) {
     const float m = other_half_max(most(acc));
@@ -797,8 +798,8 @@ struct SoftmaxTiledCfg {
 
 // The two waves of a SIMD hide each other's exponentials and LDS reads behind their products; what counts is how much else a tile costs.  bf16, 16 x 512 tokens
 // against 2048 keys, 4 x 4 heads of 128: 308 us (447 TFLOP/s) with the address of every load from its page and limit and a rescaling of the sums inside the loop (32 register
-// pairs copied a tile), 263 without, 200 with a `top` that is left for good after a few tiles.  4096 tokens against themselves, 16 heads: 139 us (990 TFLOP/s, all pairs
-// counted).
+// pairs copied a tile), 263 without, 200 with a `top` that is left for good after a few tiles.  4096 tokens against themselves, 16 heads: 139 us (495 TFLOP/s of the pairs
+// that rows see, half of all; with the product of V made twice 740 are done).
 template <typename T, int D, bool CAP>
 __device__ __forceinline__ void softmax_tiled_piece(const SoftmaxArgs& A, int wg) {
   using Cfg = SoftmaxTiledCfg<T, D>;
@@ -982,7 +983,6 @@ __device__ __forceinline__ void softmax_tiled_piece(const SoftmaxArgs& A, int wg
   if (A.lse && q.hh == 0) A.lse[(long long)q.head * g.T + v.row0 + q.t] = l > 0.f ? (q.top2() + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
 }
 
-// Enqueues the call for checked parameters; returns an entmax_attn_status.
 template <typename T, int D, bool CAP>
 __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) void softmax_tiled_kernel(SoftmaxArgs A) {
   softmax_tiled_piece<T, D, CAP>(A, blockIdx.x);
@@ -1014,6 +1014,7 @@ __global__ __launch_bounds__(kThreads, (SoftmaxTiledCfg<T, D>::kWavesPerSimd)) v
   }
 }
 
+// Enqueues the call for checked parameters; returns an entmax_attn_status.
 template <typename T, int D>
 int run_softmax(const SoftmaxCall& c);
 
